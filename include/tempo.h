@@ -43,7 +43,7 @@
  *    not finite may show in steps of the call that do not see it (fp32: it does not).
  *
  * Supported shapes: head_dim in {64, 128}; block_size a power of two, >= 32
- * for bf16 and >= 4 for f32; num_q_heads a multiple of num_kv_heads with a
+ * for bf16 and e4m3 and >= 4 for f32; num_q_heads a multiple of num_kv_heads with a
  * group of at most 128 query heads per key/value head (bf16: a group of up to
  * 16 heads is served by the single-step kernel, which can write the step's
  * key/value itself; a larger group by the kernels for wide blocks of the block entry
@@ -59,7 +59,7 @@
 extern "C" {
 #endif
 
-typedef enum { TEMPO_BF16 = 0, TEMPO_F32 = 1 } tempo_dtype;
+typedef enum { TEMPO_BF16 = 0, TEMPO_F32 = 1, TEMPO_E4M3 = 2 } tempo_dtype;
 
 typedef enum {
   TEMPO_OK = 0,
@@ -87,6 +87,19 @@ typedef enum {
  *               x 32 dims per unit group; V: 32 slots x 16 dims).  A decode step
  *               therefore streams K and V with contiguous 1 KiB loads and no
  *               transposition; the price is paid once per token at append time.
+ *   TEMPO_E4M3  8 bits an element, half the bytes of a bf16 store: q, k_new, v_new and out are bf16 as
+ *               in a bf16 store, and rows are quantised as they are written.  A row (a step's key, after
+ *               rotation, or value of one head) x gets the scale 2^e with the least whole e >= -111 for
+ *               which max |x_d| <= 448 * 2^e (over the finite x_d), and codes x_d * 2^-e rounded to the
+ *               nearest e4m3 value (4 exponent bits, 3 mantissa bits, largest 448, no infinities), ties
+ *               to even (with the largest e, 120, codes end at 240, as bf16 does not hold 2^128); elements that
+ *               are not finite become NaN.  Everything that reads the store works
+ *               with code * 2^e, which bf16 holds exactly.  Relative error of an element: at most 2^-4
+ *               down to 2^(e-6), below that at most 2^(e-10) absolute.  The pool holds the codes of all
+ *               (block, kv head) tiles, operand-major too (tempo_kv_element_offset()), and behind them a
+ *               scale byte e + 127 for every slot (tempo_kv_scale_offset()); its size is
+ *               tempo_kv_pool_bytes().  Not on an 8-bit store (TEMPO_ERR_DTYPE): the padded baseline and
+ *               work lists.
  *
  * The pools are opaque to the caller: write them with tempo_kv_append, read
  * them back with tempo_kv_gather.  Slots that were never appended may hold
@@ -101,7 +114,8 @@ typedef struct tempo_kv {
   int32_t block_size;         /* Z, the static tile size of Section 4.3 */
   int32_t num_kv_heads;       /* Hkv */
   int32_t head_dim;           /* D */
-  int32_t dtype;              /* tempo_dtype of pools, q, k_new, v_new and out */
+  int32_t dtype;              /* tempo_dtype of pools, q, k_new, v_new and out (TEMPO_E4M3: of the
+                                 pools; the others are bf16) */
   int32_t ring_blocks;        /* 0: linear store, tile n -> block_table[b][n].
                                  R > 0 (a power of two, <= max_blocks_per_seq): window store,
                                  tile n -> block_table[b][n mod R]; see below */
@@ -183,6 +197,10 @@ int tempo_ring_blocks(int32_t window, int32_t Z, int32_t queries, int32_t* ring_
 int64_t tempo_kv_element_offset(const tempo_kv* kv, int32_t which, int32_t block, int32_t head,
                                 int32_t slot, int32_t d);
 
+/* TEMPO_E4M3: byte offset, from the start of the pool, of the scale byte of slot `slot`; the scale is
+ * 2^(byte - 127).  Returns -1 for other stores and for arguments out of range. */
+int64_t tempo_kv_scale_offset(const tempo_kv* kv, int32_t which, int32_t block, int32_t head, int32_t slot);
+
 /* Bytes of one pool (k_pool or v_pool); 0 if the layout fields are invalid. */
 size_t tempo_kv_pool_bytes(const tempo_kv* kv);
 
@@ -219,7 +237,7 @@ int tempo_kv_append(const tempo_kv* kv, const void* k_new, const void* v_new, in
 /*
  * Read keys/values of steps j0 .. j0+count-1 of every sequence back out of the
  * block store into flat arrays k_out, v_out (device, [batch][count][Hkv][D] of
- * dtype; either may be NULL).  The "slice read" of the block store; used by
+ * dtype, of an 8-bit store the bf16 values that its codes stand for; either may be NULL).  The "slice read" of the block store; used by
  * tests and for inspection, not by the decode path.
  */
 int tempo_kv_gather(const tempo_kv* kv, void* k_out, void* v_out, int32_t batch, int32_t j0,
@@ -551,7 +569,7 @@ int tempo_kv_append_block(const tempo_kv* kv, const void* k_new, const void* v_n
  * kernel that produces the keys writes them into the store): row c of k_raw arrives
  * unrotated and is turned to its own position t + c (t_per_seq[b] + c) on the way in;
  * the store then holds the bits tempo_rope_kv_append would have written step by step.
- * bf16 stores only (TEMPO_ERR_DTYPE otherwise); rope as in tempo_rope_kv_append, its
+ * Not fp32 stores (TEMPO_ERR_DTYPE); rope as in tempo_rope_kv_append, its
  * tables must reach position t + count - 1.  Other errors as tempo_kv_append_block.
  */
 int tempo_rope_kv_append_block(const tempo_kv* kv, const tempo_rope* rope, const void* k_raw,
@@ -586,6 +604,70 @@ int tempo_attn_decode_combine(const tempo_kv* kv, void* out, int32_t batch, int3
 /* Workspace bytes for an explicit plan. */
 size_t tempo_attn_plan_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads,
                                        const tempo_plan* plan);
+
+/*
+ * Sparse decode attention: a step attends over `count` of its sequence's blocks instead of all of
+ * them, chosen for each (sequence, kv head) by a score that reads 4 bytes a block and dimension where
+ * attention reads block_size keys and values.  (The block is Section 4.3's static tile; which tiles a
+ * step depends on is then a dynamic dependence of its own, computed from the query.)
+ *
+ *   bounds    of a complete block n, per kv head and dimension: the smallest and the largest key element,
+ *             lo_d and hi_d, as the store holds the keys.  NaN if a key element is NaN.
+ *   score     S_n = max over the group's query heads g of sum_d max(q_gd * lo_d, q_gd * hi_d): no key of
+ *             the block has a larger product with any of the group's queries.  Taken in 64 bits, in which
+ *             products of bf16 values are exact, so the choice does not hang on rounding.
+ *   choice    the first `first` blocks, the `last` newest ones (last >= 1: the newest block is being filled
+ *             and has no bounds) and, of the others, those with the largest scores; of equal scores the
+ *             earlier block.  A score of NaN counts as the largest, so what is NaN shows in the answer.
+ *
+ * bf16 and e4m3 stores (TEMPO_ERR_DTYPE otherwise), linear ones (TEMPO_ERR_SHAPE on rings); query
+ * groups as for the attention.  t and t_per_seq as for tempo_attn_decode_causal.
+ *
+ * tempo_block_bounds_bytes  bytes of the bounds of a store (host only): bf16 [num_blocks][Hkv][2][D], by
+ *                           physical block.  16-byte aligned device memory, owned by the caller, without
+ *                           initialisation.
+ * tempo_block_bounds        writes the bounds of every block that steps t .. t+count-1 (t_per_seq[b] ..; only
+ *                           its first count_per_seq[b] ones, if given, as of a prompt) complete; to be
+ *                           called after the steps have been written, in any order with their attention.
+ *                           Bounds of other blocks are left as they are.  No launch if a uniform call
+ *                           completes no block.
+ * tempo_select_blocks       selected (device, int32 [batch][Hkv][count]): the chosen blocks of step t in
+ *                           ascending order; a sequence of fewer than `count` blocks has all of them, then -1.
+ *                           first + last <= count (TEMPO_ERR_RANGE otherwise).  Workspace: 256-byte aligned,
+ *                           tempo_select_workspace_bytes (which grows with max_t; 0 on bad arguments).
+ * tempo_attn_selected       out[b][h][:] = attention of q[b][h][:] over the keys 0 .. t of the listed blocks
+ *                           (any order; entries outside 0 .. t div block_size name no block; a block listed
+ *                           twice counts twice); 0 if that is no key.  Blocks not listed are not read.
+ *                           count * block_size <= 2^30 (TEMPO_ERR_SHAPE otherwise, here and above).
+ *                           Workspace: 256-byte aligned, tempo_attn_selected_workspace_bytes.
+ * tempo_decode_step_selected  a whole step: tempo_kv_append, tempo_block_bounds, tempo_select_blocks and
+ *                           tempo_attn_selected with these arguments; `selected` returns the choice.
+ *                           Workspace: 256-byte aligned, tempo_step_selected_workspace_bytes.
+ */
+size_t tempo_block_bounds_bytes(const tempo_kv* kv);
+
+int tempo_block_bounds(const tempo_kv* kv, void* bounds, int32_t batch, int32_t t, const int32_t* t_per_seq,
+                       int32_t count, const int32_t* count_per_seq, void* stream);
+
+size_t tempo_select_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t);
+
+int tempo_select_blocks(const tempo_kv* kv, const void* bounds, const void* q, int32_t* selected, int32_t count,
+                        int32_t first, int32_t last, int32_t batch, int32_t num_q_heads, int32_t t,
+                        const int32_t* t_per_seq, void* workspace, size_t workspace_bytes, void* stream);
+
+size_t tempo_attn_selected_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t count);
+
+int tempo_attn_selected(const tempo_kv* kv, const void* q, void* out, const int32_t* selected, int32_t count,
+                        int32_t batch, int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+size_t tempo_step_selected_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t,
+                                           int32_t count);
+
+int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, const void* k_new, const void* v_new,
+                               void* out, int32_t* selected, int32_t count, int32_t first, int32_t last, int32_t batch,
+                               int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, float scale, void* workspace,
+                               size_t workspace_bytes, void* stream);
 
 /*
  * Anti-causal window reduction (Section 3, Algorithm 1: the returns of the paper's

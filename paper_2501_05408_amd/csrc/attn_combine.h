@@ -23,7 +23,8 @@ __host__ __device__ inline int combine_lds_floats(int threads, int /*D*/) { retu
 // its splits in batches of 8 independent loads (one memory round trip per batch,
 // which is what the cost of this routine is made of), folds each batch into a
 // running (max, sum, accumulator), and the R lanes are merged through LDS.
-template <int D, bool kBf16>
+// kEmpty: a row may have seen no key at all; its output is 0.
+template <int D, bool kBf16, bool kEmpty = false>
 __device__ inline void combine_heads(const float* ml, const float* acc, int S, int n, int G,
                                      void* out, float* smem) {
   constexpr int C4 = D / 4;
@@ -80,6 +81,7 @@ __device__ inline void combine_heads(const float* ml, const float* acc, int S, i
     if (r == 0 && g < G) {
       float M = mr;
       for (int i = 1; i < R; ++i) M = fmaxf(M, smem[(i * cols + col) * 6]);
+      if (kEmpty && M == -INFINITY) M = 0.f;
       float L = 0.f;
       float4 A = {0.f, 0.f, 0.f, 0.f};
       for (int i = 0; i < R; ++i) {
@@ -89,7 +91,7 @@ __device__ inline void combine_heads(const float* ml, const float* acc, int S, i
         A.x = fmaf(w, slot[2], A.x); A.y = fmaf(w, slot[3], A.y);
         A.z = fmaf(w, slot[4], A.z); A.w = fmaf(w, slot[5], A.w);
       }
-      const float inv = 1.0f / L;
+      const float inv = kEmpty && L == 0.f ? 0.f : 1.0f / L;
       if (kBf16) {
         typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
         bf16x4 o;

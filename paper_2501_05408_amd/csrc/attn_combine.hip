@@ -8,11 +8,12 @@
 //                     latency chain (launch, one memory round trip, store), so this is
 //                     what the common case (1-8 long splits) uses.
 #include "attn_combine.h"
+#include "attn_units.h"
 
 namespace tempo {
 namespace {
 
-template <int D, bool kBf16>
+template <int D, bool kBf16, bool kEmpty = false>
 __global__ __launch_bounds__(256) void attn_combine(AttnParams p) {
   extern __shared__ float smem[];
   const int b = blockIdx.y;  // blockIdx.x runs over the sequence's (query step, query head) rows
@@ -23,12 +24,12 @@ __global__ __launch_bounds__(256) void attn_combine(AttnParams p) {
   const int64_t row = (int64_t)b * gridDim.x + blockIdx.x;
   const int64_t orow = (int64_t)b * p.io_steps * p.Hq + blockIdx.x;  // rows of `out` may be strided per sequence
   const int esz = kBf16 ? 2 : 4;
-  combine_heads<D, kBf16>(p.ws_ml + row * p.num_splits * 2, p.ws_acc + row * p.num_splits * D,
+  combine_heads<D, kBf16, kEmpty>(p.ws_ml + row * p.num_splits * 2, p.ws_acc + row * p.num_splits * D,
                                  p.num_splits, n, 1, static_cast<char*>(p.out) + orow * D * esz, smem);
 }
 
 // One float4 column of a row per thread; block_columns > 0: ranges by blocks of a prompt's columns.
-template <int D, bool kBf16>
+template <int D, bool kBf16, bool kEmpty = false>
 __device__ __forceinline__ void combine_few(const AttnParams& p, int rows, int block_columns) {
   constexpr int C4 = D / 4;
   constexpr int U = 8;
@@ -67,6 +68,7 @@ __device__ __forceinline__ void combine_few(const AttnParams& p, int rows, int b
   float M = m[0];
 #pragma unroll
   for (int u = 1; u < U; ++u) M = fmaxf(M, m[u]);
+  if (kEmpty && M == -INFINITY) M = 0.f;
   float L = 0.f;
   float4 A = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -76,7 +78,7 @@ __device__ __forceinline__ void combine_few(const AttnParams& p, int rows, int b
     A.x = fmaf(w, a[u].x, A.x); A.y = fmaf(w, a[u].y, A.y);
     A.z = fmaf(w, a[u].z, A.z); A.w = fmaf(w, a[u].w, A.w);
   }
-  const float inv = 1.0f / L;
+  const float inv = kEmpty && L == 0.f ? 0.f : 1.0f / L;
   if (kBf16) {
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     bf16x4 o;
@@ -89,9 +91,9 @@ __device__ __forceinline__ void combine_few(const AttnParams& p, int rows, int b
   }
 }
 
-template <int D, bool kBf16>
+template <int D, bool kBf16, bool kEmpty = false>
 __global__ __launch_bounds__(256) void attn_combine_few(AttnParams p, int rows) {
-  combine_few<D, kBf16>(p, rows, 0);
+  combine_few<D, kBf16, kEmpty>(p, rows, 0);
 }
 
 // A prompt: every block of p.block_columns columns has split its own key range.
@@ -123,6 +125,21 @@ hipError_t launch_combine(const AttnParams& p, int batch, int D, int dtype, hipS
     if (D == 128) return launch((attn_combine<128, false>), grid, block, lds, stream, p);
     else return launch((attn_combine<64, false>), grid, block, lds, stream, p);
   }
+}
+
+// Partials of lists of blocks, which may name no key of a row.
+hipError_t launch_combine_selected(const AttnParams& p, int batch, int D, hipStream_t stream) {
+  const dim3 block(256);
+  if (p.num_splits <= 8) {
+    const int rows = batch * p.Hq;
+    const dim3 few((unsigned)(((int64_t)rows * (D / 4) + 255) / 256));
+    if (D == 128) return launch((attn_combine_few<128, true, true>), few, block, 0, stream, p, rows);
+    return launch((attn_combine_few<64, true, true>), few, block, 0, stream, p, rows);
+  }
+  const dim3 grid(p.Hq, batch);
+  const size_t lds = (size_t)combine_lds_floats(256, D) * sizeof(float);
+  if (D == 128) return launch((attn_combine<128, true, true>), grid, block, lds, stream, p);
+  return launch((attn_combine<64, true, true>), grid, block, lds, stream, p);
 }
 
 // bf16, at most 8 splits.

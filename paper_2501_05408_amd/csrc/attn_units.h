@@ -1,0 +1,47 @@
+// What the launches of attn_units.hip and select_blocks.hip take, on top of tempo_internal.h.
+#pragma once
+
+#include "tempo_internal.h"
+
+namespace tempo {
+
+// Attention over a list of blocks: t and t_per_seq are the step's, window and count are not used, one query step.
+struct SelectParams : AttnParams {
+  const int32_t* selected;  // [B][Hkv][pick] block numbers
+  int32_t pick;
+};
+
+// Dynamic LDS of a launch of attn_units.
+inline size_t units_lds_bytes(int waves, int columns, int D) {
+  return (size_t)waves * (32 + (size_t)(columns < 16 ? columns : 16) * D) * sizeof(float);
+}
+
+// Score and choice of blocks.
+struct ChooseParams {
+  const void* bounds;         // [num_blocks][Hkv][2][D] bf16
+  const void* q;              // [B][Hq][D] bf16
+  const int32_t* block_table;
+  const int32_t* t_per_seq;   // may be null
+  uint64_t* scores;           // [B][Hkv][tiles]: order-preserving bits of the scores
+  int32_t* selected;          // [B][Hkv][pick]
+  int32_t t;
+  int32_t z_log2;
+  int32_t max_blocks_per_seq;
+  int32_t num_blocks;
+  int32_t Hkv, Hq, G;
+  int32_t tiles;              // t / Z + 1
+  int32_t pick, first, last;
+};
+
+// Weak: the host side can be built without the kernels (its tests record the launches).
+#define TEMPO_LAUNCHER __attribute__((weak)) hipError_t
+TEMPO_LAUNCHER launch_append_e4m3(const StoreParams& p, const void* k_new, const void* v_new, int D, hipStream_t stream);
+TEMPO_LAUNCHER launch_gather_e4m3(const StoreParams& p, void* k_out, void* v_out, int D, int j0, int count, hipStream_t stream);
+TEMPO_LAUNCHER launch_partial_e4m3(const AttnParams& p, int batch, int D, int grid_splits, int waves, hipStream_t stream);
+TEMPO_LAUNCHER launch_partial_selected(const SelectParams& p, int batch, int D, int dtype, int grid_splits, int waves, hipStream_t stream);
+TEMPO_LAUNCHER launch_combine_selected(const AttnParams& p, int batch, int D, hipStream_t stream);
+TEMPO_LAUNCHER launch_block_bounds(const StoreParams& p, void* bounds, int D, int dtype, hipStream_t stream);
+TEMPO_LAUNCHER launch_select_blocks(const ChooseParams& p, int batch, int D, hipStream_t stream);
+#undef TEMPO_LAUNCHER
+
+}  // namespace tempo

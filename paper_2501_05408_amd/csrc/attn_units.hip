@@ -1,0 +1,340 @@
+// Partial attention of one split over an 8-bit block store, and over a list of selected blocks of either kind of store;
+// MFMA on gfx950.
+//
+// What is computed, and how a wavefront computes it, is as in attn_partial_bf16.hip: Eq. 1 over one split's key
+// positions with a running maximum and sum in fp32; S^T tile = K (16 slots x 32 dims) * Q^T, acc tile = P * V, both
+// operands as they lie in the store, streamed by 1 KiB loads without LDS.  What differs:
+//   8-bit codes (k8).  A 1 KiB unit holds the operands of two MFMAs.  Keys are turned into bf16 with their row's scale
+//     (v_cvt_scalef32_pk_bf16_fp8: exact), so logits need no further factor.  Values are turned into bf16 without a
+//     scale and the weight of a slot is multiplied by the slot's scale, a power of two, after it has been rounded to
+//     bf16: the products are those of the weights and the values that the codes stand for, and the sum of the weights
+//     is that of the rounded ones.  Rounding the weights to bf16 costs as much as rounding the result does.
+//   Lists (kSelect).  The positions of a split run over the blocks of a list, [batch][Hkv][pick] block numbers, not over
+//     the sequence: position v is slot v mod Z of block list[v div Z].  Entries that name no block at or before the
+//     step's are passed over.
+// More than 16 (step, head) columns: further workgroups along grid.x take the next 16 over the same keys, next to
+// each other in dispatch order, so that all but one of them read from a die's L2.
+#include "attn_bf16_common.h"
+#include "attn_units.h"
+#include "store_e4m3.h"
+
+namespace tempo {
+namespace {
+
+// The register image of a 32-slot group: keys, values, and in an 8-bit store the lane's scale bytes.
+template <int D, bool k8>
+struct Image {
+  static constexpr int UNITS = k8 ? D / 32 : D / 16;  // 1 KiB units of keys, and of values
+  u32x4 k[UNITS], v[UNITS];
+  uint32_t k_scales;   // slots row, 16 + row
+  uint2 v_scales;      // slots 4c..4c+3; 16+4c..16+4c+3
+};
+
+template <int D, bool k8>
+__device__ __forceinline__ void load_image_keys(const AttnParams& p, int64_t slot, int64_t slots, int lane, Image<D, k8>& g) {
+  const char* const at = static_cast<const char*>(p.k_pool) + slot * (k8 ? D : 2 * D) + lane * 16;
+#pragma unroll
+  for (int i = 0; i < Image<D, k8>::UNITS; ++i) g.k[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at + i * 1024));
+  if constexpr (k8) g.k_scales = *reinterpret_cast<const uint16_t*>(static_cast<const char*>(p.k_pool) + slots * D + slot + 2 * (lane & 15));
+}
+
+template <int D, bool k8>
+__device__ __forceinline__ void load_image_values(const AttnParams& p, int64_t slot, int64_t slots, int lane, Image<D, k8>& g) {
+  const char* const at = static_cast<const char*>(p.v_pool) + slot * (k8 ? D : 2 * D) + lane * 16;
+#pragma unroll
+  for (int i = 0; i < Image<D, k8>::UNITS; ++i) g.v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at + i * 1024));
+  if constexpr (k8) g.v_scales = *reinterpret_cast<const uint2*>(static_cast<const char*>(p.v_pool) + slots * D + slot + 8 * (lane >> 4));
+}
+
+// 8 codes (two words) as a bf16 operand.
+__device__ __forceinline__ bf16x8 operand_of(uint32_t a, uint32_t b, float scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true)};
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// Logits of the group's two row tiles, in base-2 units.
+template <int D, bool k8>
+__device__ __forceinline__ void image_logits(const AttnParams& p, const u32x4* qreg, const Image<D, k8>& g, float* x) {
+  constexpr int KS = D / 32;
+  f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
+  if constexpr (k8) {
+    const float ka = scale_of(g.k_scales & 0xFFu), kb = scale_of(g.k_scales >> 8);
+#pragma unroll
+    for (int w = 0; w < KS / 2; ++w) {
+      const u32x4 a = g.k[w], b = g.k[KS / 2 + w];
+      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(a.x, a.y, ka), as_bf16x8(qreg[2 * w]), sa, 0, 0, 0);
+      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(b.x, b.y, kb), as_bf16x8(qreg[2 * w]), sb, 0, 0, 0);
+      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(a.z, a.w, ka), as_bf16x8(qreg[2 * w + 1]), sa, 0, 0, 0);
+      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(b.z, b.w, kb), as_bf16x8(qreg[2 * w + 1]), sb, 0, 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(g.k[s]), as_bf16x8(qreg[s]), sa, 0, 0, 0);
+      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(g.k[KS + s]), as_bf16x8(qreg[s]), sb, 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    x[r] = sa[r] * p.scale_log2e;
+    x[4 + r] = sb[r] * p.scale_log2e;
+  }
+}
+
+// Which slots of a group this lane's values may be seen of, as masks of their bytes: x of slots 4c..4c+3, y of the others.
+__device__ __forceinline__ uint2 seen_bytes(int key0, int v_lo, int v_hi, int lane) {
+  const int c = lane >> 4;
+  uint2 keep = {0u, 0u};
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int ja = key0 + 4 * c + r, jb = ja + 16;
+    keep.x |= ja >= v_lo && ja <= v_hi ? 0xFFu << (8 * r) : 0u;
+    keep.y |= jb >= v_lo && jb <= v_hi ? 0xFFu << (8 * r) : 0u;
+  }
+  return keep;
+}
+
+// The weights of a group's slots, times the scales of their values.
+__device__ __forceinline__ bf16x8 scaled_weights(bf16x8 pa, uint2 scales) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    pa[r] = (__bf16)((float)pa[r] * scale_of((scales.x >> (8 * r)) & 0xFFu));
+    pa[4 + r] = (__bf16)((float)pa[4 + r] * scale_of((scales.y >> (8 * r)) & 0xFFu));
+  }
+  return pa;
+}
+
+// Merge of the workgroup's wavefronts, as in attn_partial_bf16.hip; column j is column first_col + j of the call.
+template <int D, int NW, bool kSelect>
+__device__ __forceinline__ void merge_units(const AttnParams& p, const float* smem, int first_col, int ncols, int b, int hkv, int split) {
+  const float* sm_m = smem;
+  const float* sm_l = smem + NW * 16;
+  const float* sm_acc = smem + NW * 32;
+  for (int idx = threadIdx.x; idx < ncols * D; idx += 64 * NW) {
+    const int j = idx / D, d = idx - j * D;
+    float mw[NW], lw[NW], aw[NW];
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      mw[w] = sm_m[w * 16 + j];
+      lw[w] = sm_l[w * 16 + j];
+      aw[w] = sm_acc[(w * ncols + j) * D + d];
+    }
+    float M = mw[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, mw[w]);
+    const float ref = M == -INFINITY ? 0.f : M;  // nothing seen, or nothing but NaN, which has to show
+    float num = 0.f, den = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const bool seen = lw[w] != 0.f;  // (a column's largest weight is 1)
+      const float wgt = fast_exp2(mw[w] - ref);
+      num += seen ? wgt * aw[w] : 0.f;
+      den += seen ? wgt * lw[w] : 0.f;
+    }
+    const int jc = (first_col + j) / p.G, jg = first_col + j - jc * p.G;
+    if (p.direct) {
+      const int64_t orow = ((int64_t)b * p.io_steps + jc) * p.Hq + (int64_t)hkv * p.G + jg;
+      const float o = kSelect && den == 0.f ? 0.f : num / den;  // a list may name no key of this step
+      static_cast<__bf16*>(p.out)[orow * D + d] = (__bf16)o;
+    } else {
+      const int64_t row = ((int64_t)b * p.queries + jc) * p.Hq + (int64_t)hkv * p.G + jg;
+      const int64_t part = row * p.num_splits + split;
+      p.ws_acc[part * D + d] = num;
+      if (d == 0) {
+        p.ws_ml[part * 2] = M;
+        p.ws_ml[part * 2 + 1] = den;
+      }
+    }
+  }
+}
+
+template <int D, bool k8, bool kSelect, bool kRope>
+__global__ __launch_bounds__(512) void attn_units(SelectParams p) {
+  constexpr int KS = D / 32, DT = D / 16;
+  extern __shared__ float smem[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nwaves = blockDim.x >> 6;
+  const int hkv = (int)(blockIdx.x % (unsigned)p.Hkv), first_col = 16 * (int)(blockIdx.x / (unsigned)p.Hkv);
+  const int b = blockIdx.y;
+  int t_b = p.t_per_seq ? ((const_i32_ptr)p.t_per_seq)[b] : p.t;
+  t_b = t_b > p.t ? p.t : (t_b < 0 ? 0 : t_b);
+  int split, start, end;  // positions: keys, or places in the list's blocks
+  if constexpr (kSelect) {
+    split = blockIdx.z;
+    start = split << p.tps_log2;
+    const int last = (p.pick << p.z_log2) - 1, ce = split_end(split, p.tps_log2);
+    end = last < ce ? last : ce;
+  } else {
+    const SeqRange rg = seq_range(t_b, p.window, p.tps_log2, p.queries);
+    if ((int)blockIdx.z >= rg.nchunks) return;  // uniform over the workgroup
+    split = rg.nchunks - 1 - (int)blockIdx.z;   // newest first, as in attn_partial_bf16.hip
+    const int chunk = rg.chunk0 + split, cs = chunk << p.tps_log2, ce = split_end(chunk, p.tps_log2);
+    start = rg.lo > cs ? rg.lo : cs;
+    end = rg.hi < ce ? rg.hi : ce;
+  }
+  const int g_last = end >> 5;
+  const int64_t slots = ((int64_t)p.num_blocks * p.Hkv) << p.z_log2;  // of the store
+  const_i32_ptr const table = (const_i32_ptr)p.block_table + (int64_t)b * p.max_blocks_per_seq;
+  const_i32_ptr const list = kSelect ? (const_i32_ptr)p.selected + ((int64_t)b * p.Hkv + hkv) * p.pick : nullptr;
+
+  // First key of the group at position group `at`; negative: none that step t_b sees.
+  auto key_of = [&](int at) __attribute__((always_inline)) {
+    if constexpr (!kSelect) return at << 5;
+    const int pos = at << 5, n = list[pos >> p.z_log2];
+    if (n < 0 || n > (t_b >> p.z_log2)) return -1;
+    const int key = (n << p.z_log2) + (pos & ((1 << p.z_log2) - 1));
+    return key <= t_b ? key : -1;
+  };
+  // From position group `at` on, in this wavefront's turn, the first one with keys.
+  auto next_of = [&](int at, int& key) __attribute__((always_inline)) {
+    for (; at <= g_last; at += nwaves) {
+      key = key_of(at);
+      if (!kSelect || key >= 0) break;
+    }
+    return at;
+  };
+  auto slot_of = [&](int key) __attribute__((always_inline)) {
+    const int phys = clamp_block(table[(key >> p.z_log2) & p.tile_mask], p.num_blocks);
+    return (((int64_t)phys * p.Hkv + hkv) << p.z_log2) + (key & ((1 << p.z_log2) - 1));
+  };
+
+  Image<D, k8> g;
+  int key = 0;
+  int grp = next_of((start >> 5) + wave, key);
+  if (grp <= g_last) {
+    const int64_t slot = slot_of(key);
+    load_image_keys<D, k8>(p, slot, slots, lane, g);
+    load_image_values<D, k8>(p, slot, slots, lane, g);
+  }
+
+  // Columns and their ranges, as in attn_partial_bf16.hip.
+  const int all_cols = p.queries * p.G - first_col, ncols = all_cols < 16 ? all_cols : 16;
+  const int t_end = t_b + p.queries - 1;
+  const int from = kSelect ? 0 : start, upto = kSelect ? t_b : end;  // keys
+  const int lo_last = (p.window > 0 && t_end - p.window + 1 > 0) ? t_end - p.window + 1 : 0;
+  const int all_lo = lo_last > from ? lo_last : from;
+  const int all_hi = t_b < upto ? t_b : upto;
+  const int seen_hi = t_end < upto ? t_end : upto;
+  const int col = lane & 15;
+  const int cq = col < ncols ? (first_col + col) / p.G : p.queries - 1;
+  const int gq = col < ncols ? first_col + col - cq * p.G : 0;
+  const int hi_col = (t_b + cq) < upto ? (t_b + cq) : upto;
+  const int lo_q = (p.window > 0 && t_b + cq - p.window + 1 > 0) ? t_b + cq - p.window + 1 : 0;
+  const int lo_col = lo_q > from ? lo_q : from;
+  u32x4 qreg[KS];
+  {
+    const int c = lane >> 4;
+    const uint16_t* qp = static_cast<const uint16_t*>(p.q) +
+                         (((int64_t)b * p.io_steps + cq) * p.Hq + (int64_t)hkv * p.G + gq) * D + 8 * c;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const u32x4 zero = {0u, 0u, 0u, 0u};
+      const u32x4 v = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+      qreg[s] = col < ncols ? v : zero;
+    }
+  }
+  if (kRope) rotate_query<D>(p, t_b + cq, lane, qreg);
+
+  WaveState<D> st;
+  st.m = -INFINITY;
+  st.l = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) st.acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  while (grp <= g_last) {
+    int key_nxt = 0;
+    const int nxt = next_of(grp + nwaves, key_nxt);
+    const bool more = nxt <= g_last;
+    const int64_t slot_nxt = more ? slot_of(key_nxt) : 0;
+
+    float x[8];
+    image_logits<D, k8>(p, qreg, g, x);
+    if (more) load_image_keys<D, k8>(p, slot_nxt, slots, lane, g);
+
+    const bool cut = key < all_lo || key + 31 > all_hi;  // wave-uniform
+    uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};             // bf16 values: masks of the lane's 8 slots
+    uint2 keep8 = {~0u, ~0u};
+    if (cut) {
+      mask_logits(key >> 5, lo_col, hi_col, lane, x);
+      if constexpr (k8) keep8 = seen_bytes(key, from, seen_hi, lane);
+      else value_masks(key >> 5, from, seen_hi, lane, keep);
+    }
+    bf16x8 pa = softmax_update<D>(x, lane, st);
+
+    // Slots that no step of the call sees may be unwritten: codes and scales of 0 under the weight of 0.
+    if constexpr (k8) {
+      pa = scaled_weights(pa, uint2{g.v_scales.x & keep8.x, g.v_scales.y & keep8.y});
+#pragma unroll
+      for (int w = 0; w < DT / 2; ++w) {
+        const u32x4 v = g.v[w];
+        st.acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, operand_of(v.x & keep8.x, v.y & keep8.y, 1.f), st.acc[2 * w], 0, 0, 0);
+        st.acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, operand_of(v.z & keep8.x, v.w & keep8.y, 1.f), st.acc[2 * w + 1], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        u32x4 v = g.v[dt];
+        v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
+        st.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, as_bf16x8(v), st.acc[dt], 0, 0, 0);
+      }
+    }
+    if (more) load_image_values<D, k8>(p, slot_nxt, slots, lane, g);
+    grp = nxt;
+    key = key_nxt;
+  }
+
+  const float l_tot = column_sum(st.l);
+  float* sm_m = smem;                  // [nwaves][16]
+  float* sm_l = smem + nwaves * 16;    // [nwaves][16]
+  float* sm_acc = smem + nwaves * 32;  // [nwaves][ncols][D]
+  if (lane < 16) {
+    sm_m[wave * 16 + lane] = st.m;
+    sm_l[wave * 16 + lane] = l_tot;
+  }
+  {
+    const int n = lane & 15, c = lane >> 4;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int j = 4 * c + r;
+      if (j < ncols) {
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) sm_acc[(wave * ncols + j) * D + 16 * dt + n] = st.acc[dt][r];
+      }
+    }
+  }
+  __syncthreads();
+  if (nwaves == 8) merge_units<D, 8, kSelect>(p, smem, first_col, ncols, b, hkv, split);
+  else if (nwaves == 4) merge_units<D, 4, kSelect>(p, smem, first_col, ncols, b, hkv, split);
+  else if (nwaves == 2) merge_units<D, 2, kSelect>(p, smem, first_col, ncols, b, hkv, split);
+  else merge_units<D, 1, kSelect>(p, smem, first_col, ncols, b, hkv, split);
+}
+
+template <bool k8, bool kSelect, bool kRope>
+hipError_t launch_units(const SelectParams& p, int batch, int D, int grid_splits, int waves, hipStream_t stream) {
+  const int columns = p.queries * p.G;
+  const dim3 grid((unsigned)(p.Hkv * ((columns + 15) / 16)), (unsigned)batch, (unsigned)grid_splits), block(64 * waves);
+  const size_t lds = units_lds_bytes(waves, columns, D);
+  if (D == 128) return launch((attn_units<128, k8, kSelect, kRope>), grid, block, lds, stream, p);
+  return launch((attn_units<64, k8, kSelect, kRope>), grid, block, lds, stream, p);
+}
+
+}  // namespace
+
+hipError_t launch_partial_e4m3(const AttnParams& p, int batch, int D, int grid_splits, int waves, hipStream_t stream) {
+  SelectParams s;
+  static_cast<AttnParams&>(s) = p;
+  s.selected = nullptr;
+  s.pick = 0;
+  if (p.rope_cos) return launch_units<true, false, true>(s, batch, D, grid_splits, waves, stream);
+  return launch_units<true, false, false>(s, batch, D, grid_splits, waves, stream);
+}
+
+hipError_t launch_partial_selected(const SelectParams& p, int batch, int D, int dtype, int grid_splits, int waves, hipStream_t stream) {
+  if (dtype == TEMPO_E4M3) return launch_units<true, true, false>(p, batch, D, grid_splits, waves, stream);
+  return launch_units<false, true, false>(p, batch, D, grid_splits, waves, stream);
+}
+
+}  // namespace tempo

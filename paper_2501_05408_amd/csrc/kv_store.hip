@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "attn_bf16_common.h"
+#include "attn_units.h"
 
 namespace tempo {
 namespace {
@@ -250,6 +251,7 @@ hipError_t launch_elements_bf16(const StoreParams& p, const uint16_t* k, const u
 
 hipError_t launch_append(const StoreParams& p, const void* k_new, const void* v_new, int D,
                          int dtype, hipStream_t stream) {
+  if (dtype == TEMPO_E4M3) return launch_append_e4m3(p, k_new, v_new, D, stream);
   // bf16, uniform first step, at least one whole 32-slot group: the group kernel (4096 rows of 16
   // sequences in 8 heads: 86 us, element-wise 315 us).  Rows that fill no group go element by
   // element, as the group kernel's work for a partly covered group is that of a whole one.
@@ -300,6 +302,7 @@ hipError_t launch_stage(const StageParams& p, const void* k_new, const void* v_n
 
 hipError_t launch_gather(const StoreParams& p, void* k_out, void* v_out, int D, int dtype, int j0,
                          int count, hipStream_t stream) {
+  if (dtype == TEMPO_E4M3) return launch_gather_e4m3(p, k_out, v_out, D, j0, count, stream);
   const int threads = 256;
   const int64_t total = (int64_t)p.batch * count * p.Hkv * D;
   if (total == 0) return hipSuccess;

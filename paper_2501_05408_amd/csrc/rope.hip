@@ -8,6 +8,7 @@
 // [positions][D/2] in fp32.  The arithmetic is fp32; bf16 results are rounded to
 // nearest even once.  The attention kernels contain the same rotation for the
 // fully fused decode step.
+#include "attn_units.h"
 #include "tempo_internal.h"
 
 namespace tempo {
@@ -93,6 +94,12 @@ hipError_t launch_rope_rotate(const float* rope_cos, const float* rope_sin, cons
 
 hipError_t launch_rope_append(const StoreParams& p, const float* rope_cos, const float* rope_sin,
                               const void* k_raw, const void* v_new, int D, int dtype, hipStream_t stream) {
+  if (dtype == TEMPO_E4M3) {
+    StoreParams turned = p;
+    turned.rope_cos = rope_cos;
+    turned.rope_sin = rope_sin;
+    return launch_append_e4m3(turned, k_raw, v_new, D, stream);
+  }
   const int total = p.batch * p.Hkv * (D / 2);
   const dim3 grid((total + 255) / 256), block(256);
   if (dtype == TEMPO_BF16)

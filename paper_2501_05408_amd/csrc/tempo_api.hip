@@ -6,6 +6,7 @@
 
 #include <mutex>
 
+#include "attn_units.h"
 #include "tempo_internal.h"
 
 namespace {
@@ -22,11 +23,11 @@ int ilog2_exact(int32_t v) {  // log2 of a power of two, else -1
 // Layout fields only (no pointers): dtype, head_dim, block_size, heads, counts.
 int check_layout(const tempo_kv* kv) {
   if (!kv) return TEMPO_ERR_NULL;
-  if (kv->dtype != TEMPO_BF16 && kv->dtype != TEMPO_F32) return TEMPO_ERR_DTYPE;
+  if (kv->dtype != TEMPO_BF16 && kv->dtype != TEMPO_F32 && kv->dtype != TEMPO_E4M3) return TEMPO_ERR_DTYPE;
   if (kv->head_dim != 64 && kv->head_dim != 128) return TEMPO_ERR_SHAPE;
   const int zl = ilog2_exact(kv->block_size);
   if (zl < 0) return TEMPO_ERR_SHAPE;
-  if (kv->dtype == TEMPO_BF16 && kv->block_size < 32) return TEMPO_ERR_SHAPE;
+  if (kv->dtype != TEMPO_F32 && kv->block_size < 32) return TEMPO_ERR_SHAPE;
   if (kv->dtype == TEMPO_F32 && kv->block_size < 4) return TEMPO_ERR_SHAPE;
   if (kv->num_kv_heads < 1 || kv->num_kv_heads > 65535) return TEMPO_ERR_SHAPE;
   if (kv->num_blocks < 1 || kv->max_blocks_per_seq < 1) return TEMPO_ERR_SHAPE;
@@ -196,7 +197,7 @@ void make_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int
                             ? (int64_t)batch * Hq
                             : (int64_t)batch * kv->num_kv_heads * (kv->dtype == TEMPO_F32 ? (columns + 15) / 16 : 1);
   const int64_t len = (window > 0 && window < (int64_t)t_max + 1) ? window : (int64_t)t_max + 1;
-  const int bytes_per_key = 2 * kv->head_dim * (kv->dtype == TEMPO_BF16 ? 2 : 4);  // K and V of one head
+  const int bytes_per_key = 2 * kv->head_dim * (kv->dtype == TEMPO_E4M3 ? 1 : kv->dtype == TEMPO_BF16 ? 2 : 4);  // K and V of one head
   const int k_max = ragged ? 10 : 30;
   int best_k = -1;
   double best_cost = -1.0;
@@ -389,6 +390,7 @@ int check_attn(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, int32_t
     // more than 16 columns go to the kernels for wide blocks, whose launch shapes are fixed
     if (columns <= kNarrowColumns && partial_bf16_lds_bytes(plan->waves, columns, kv->head_dim) > kMaxLds) return TEMPO_ERR_SHAPE;
   }
+  if (kv->dtype == TEMPO_E4M3 && units_lds_bytes(plan->waves, queries * (Hq / kv->num_kv_heads), kv->head_dim) > kMaxLds) return TEMPO_ERR_SHAPE;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
   if (workspace_bytes < plan_bytes(kv, (int64_t)batch * queries * Hq, plan->num_splits)) return TEMPO_ERR_WORKSPACE;
   return TEMPO_OK;
@@ -423,6 +425,16 @@ int do_partial(const tempo_kv* kv, const void* q, const void* k_new, const void*
   const int32_t gs = grid_splits(plan, t, t_per_seq, window, queries, pad_t);
   if (kv->dtype == TEMPO_BF16 && queries * p.G > kNarrowColumns)  // a wide block: kernels of their own, key range split as planned
     return launch_status(launch_block_bf16(p, batch, kv->head_dim, gs, stream), "attn_block_partial");
+  if (kv->dtype == TEMPO_E4M3) {
+    if (k_new) {  // its kernel reads the store only
+      StoreParams sp = store_params(kv, batch, t, t_per_seq);
+      sp.rope_cos = p.rope_cos;
+      sp.rope_sin = p.rope_sin;
+      const int rc = launch_status(launch_append_e4m3(sp, k_new, v_new, kv->head_dim, stream), "kv_append");
+      if (rc != TEMPO_OK) return rc;
+    }
+    return launch_status(launch_partial_e4m3(p, batch, kv->head_dim, gs, plan->waves, stream), "attn_decode_partial");
+  }
   const hipError_t e = kv->dtype == TEMPO_BF16
                            ? launch_partial_bf16(p, batch, kv->head_dim, gs, plan->waves, stream)
                        : f32_on_vector_alu(kv, batch, Hq, last_step(t, queries), union_window(window, queries), queries)
@@ -437,7 +449,7 @@ int do_combine(const tempo_kv* kv, void* out, int32_t batch, int32_t Hq, int32_t
   AttnParams p = attn_params(kv, nullptr, out, Hq, t, t_per_seq, window, 1.0f, plan, workspace, batch, queries,
                              pad_t);
   if (io_steps > 0) p.io_steps = io_steps;
-  const hipError_t e = launch_combine(p, batch, kv->head_dim, kv->dtype, stream);
+  const hipError_t e = launch_combine(p, batch, kv->head_dim, kv->dtype == TEMPO_F32 ? TEMPO_F32 : TEMPO_BF16, stream);
   return launch_status(e, "attn_decode_combine");
 }
 
@@ -486,8 +498,12 @@ void make_stream_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, 
 void make_block_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, int32_t window,
                      bool ragged, int32_t queries, tempo_plan* plan, int64_t max_splits = kMaxSplits) {
   make_plan(kv, batch, Hq, last_step(t, queries), union_window(window, queries), ragged, queries, max_splits, plan);
-  if (kv->dtype != TEMPO_BF16) return;
   const int columns = queries * (Hq / kv->num_kv_heads);
+  if (kv->dtype == TEMPO_E4M3) {
+    while (plan->waves > 1 && units_lds_bytes(plan->waves, columns, kv->head_dim) > kMaxLds) plan->waves /= 2;
+    return;
+  }
+  if (kv->dtype != TEMPO_BF16) return;
   if (columns > kNarrowColumns && block_streams(kv->head_dim, columns, (int64_t)batch * kv->num_kv_heads, block_keys(t, queries, window))) {
     make_stream_plan(kv, batch, Hq, t, window, ragged, queries, max_splits, plan);
     return;
@@ -614,11 +630,23 @@ int64_t tempo_kv_element_offset(const tempo_kv* kv, int32_t which, int32_t block
   const int D = kv->head_dim;
   const int64_t base = ((int64_t)block * kv->num_kv_heads + head) * kv->block_size * D;
   if (kv->dtype == TEMPO_F32) return base + tile_off_f32(D, slot, d);
+  if (kv->dtype == TEMPO_E4M3) return base + (which == 0 ? tile_off_k_e4m3(D, slot, d) : tile_off_v_e4m3(D, slot, d));
   return base + (which == 0 ? tile_off_k_bf16(D, slot, d) : tile_off_v_bf16(D, slot, d));
+}
+
+int64_t tempo_kv_scale_offset(const tempo_kv* kv, int32_t which, int32_t block, int32_t head, int32_t slot) {
+  if (check_layout(kv) != TEMPO_OK || kv->dtype != TEMPO_E4M3) return -1;
+  if (which < 0 || which > 1 || block < 0 || block >= kv->num_blocks || head < 0 ||
+      head >= kv->num_kv_heads || slot < 0 || slot >= kv->block_size)
+    return -1;
+  const int64_t slots = (int64_t)kv->num_blocks * kv->num_kv_heads * kv->block_size;
+  const int64_t first = ((int64_t)block * kv->num_kv_heads + head) * kv->block_size;
+  return slots * kv->head_dim + first + (which == 0 ? scale_off_k(slot) : scale_off_v(slot));
 }
 
 size_t tempo_kv_pool_bytes(const tempo_kv* kv) {
   if (check_layout(kv) != TEMPO_OK) return 0;
+  if (kv->dtype == TEMPO_E4M3) return (size_t)kv->num_blocks * kv->num_kv_heads * kv->block_size * (kv->head_dim + 1);
   const size_t e = kv->dtype == TEMPO_BF16 ? 2 : 4;
   return (size_t)kv->num_blocks * kv->num_kv_heads * kv->block_size * kv->head_dim * e;
 }
@@ -726,7 +754,7 @@ int tempo_rope_kv_append_block(const tempo_kv* kv, const tempo_rope* rope, const
   int rc = check_store(kv);
   if (rc != TEMPO_OK) return rc;
   if (!k_raw || !v_new) return TEMPO_ERR_NULL;
-  if (kv->dtype != TEMPO_BF16) return TEMPO_ERR_DTYPE;  // the block write rotates in the bf16 kernels only
+  if (kv->dtype == TEMPO_F32) return TEMPO_ERR_DTYPE;  // the block write does not rotate in the fp32 kernel
   if (batch < 1 || batch > 65535) return TEMPO_ERR_SHAPE;
   if (count < 1 || count > 65536) return TEMPO_ERR_SHAPE;
   if (t < 0 || t > INT32_MAX - count) return TEMPO_ERR_RANGE;
@@ -878,7 +906,7 @@ int tempo_attn_decode_padded_causal(const tempo_kv* kv, const void* q, void* out
                                     int32_t num_q_heads, int32_t t, const int32_t* t_per_seq,
                                     int32_t t_pad, float scale, void* workspace, size_t workspace_bytes,
                                     void* stream) {
-  if (kv && kv->dtype == TEMPO_F32) return TEMPO_ERR_DTYPE;  // the baseline exists for the bf16 kernel only
+  if (kv && (kv->dtype == TEMPO_F32 || kv->dtype == TEMPO_E4M3)) return TEMPO_ERR_DTYPE;  // the baseline exists for the bf16 kernel only
   // ... and in the single-step kernel only: the kernels that serve larger query
   // groups walk the step's own range and know no padding bound
   if (kv && kv->num_kv_heads > 0 && num_q_heads / kv->num_kv_heads > kNarrowColumns) return TEMPO_ERR_SHAPE;
@@ -1332,6 +1360,7 @@ static int prefill(const tempo_kv* kv, const void* q, const void* k_new, const v
   int rc = check_store(kv);
   if (rc != TEMPO_OK) return rc;
   if (!q || !k_new || !v_new || !out) return TEMPO_ERR_NULL;
+  if (kv->dtype == TEMPO_E4M3) return TEMPO_ERR_DTYPE;
   if ((rc = check_heads(kv, batch, Hq)) != TEMPO_OK) return rc;
   if (count < 1 || count > (1 << 24)) return TEMPO_ERR_SHAPE;
   if (t < 0 || window < 0 || t > INT32_MAX - 64 - count) return TEMPO_ERR_RANGE;
@@ -1474,6 +1503,7 @@ int tempo_rope_prefill_window(const tempo_kv* kv, const tempo_rope* rope, const 
 
 int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t count) {
   if (check_layout(kv) != TEMPO_OK || check_heads(kv, batch, num_q_heads) != TEMPO_OK || count < 1) return 0;
+  if (kv->dtype == TEMPO_E4M3) return 0;
   const int32_t G = num_q_heads / kv->num_kv_heads, block = kMaxColumns / G;
   if (kv->ring_blocks == 0 && prompt_in_one_launch(kv, batch, num_q_heads, count)) {
     if (kv->dtype != TEMPO_BF16) return 3;
@@ -1484,6 +1514,7 @@ int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_head
 
 size_t tempo_prefill_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t) {
   if (check_layout(kv) != TEMPO_OK || check_heads(kv, batch, num_q_heads) != TEMPO_OK) return 0;
+  if (kv->dtype == TEMPO_E4M3) return 0;
   const int32_t block = kMaxColumns / (num_q_heads / kv->num_kv_heads);
   return tempo_attn_block_workspace_bytes(kv, batch, num_q_heads, block, max_t);
 }
@@ -1567,6 +1598,169 @@ int tempo_attn_decode_combine(const tempo_kv* kv, void* out, int32_t batch, int3
   if ((rc = check_attn(kv, batch, num_q_heads, t, window, t_per_seq != nullptr, plan, workspace, workspace_bytes)) != TEMPO_OK) return rc;
   return do_combine(kv, out, batch, num_q_heads, t, t_per_seq, window, plan,
                     const_cast<void*>(workspace), static_cast<hipStream_t>(stream));
+}
+
+// ---- attention over selected blocks ------------------------------------------------
+
+// Bounds, scores and lists are of bf16 and 8-bit linear stores.
+static int check_sparse_store(const tempo_kv* kv, int32_t batch) {
+  const int rc = check_layout(kv);
+  if (rc != TEMPO_OK) return rc;
+  if (kv->dtype == TEMPO_F32) return TEMPO_ERR_DTYPE;
+  if (kv->ring_blocks != 0) return TEMPO_ERR_SHAPE;
+  if (batch < 1 || batch > 65535) return TEMPO_ERR_SHAPE;
+  return TEMPO_OK;
+}
+
+// A list of `count` blocks: its places, block_size to an entry, are counted in 32 bits.
+static int check_list(const tempo_kv* kv, int32_t count) {
+  return count >= 1 && (int64_t)count * kv->block_size <= (1 << 30) ? TEMPO_OK : TEMPO_ERR_SHAPE;
+}
+
+static int check_choice(const tempo_kv* kv, int32_t count, int32_t first, int32_t last) {
+  const int rc = check_list(kv, count);
+  if (rc != TEMPO_OK) return rc;
+  return first >= 0 && last >= 1 && (int64_t)first + last <= count ? TEMPO_OK : TEMPO_ERR_RANGE;
+}
+
+size_t tempo_block_bounds_bytes(const tempo_kv* kv) {
+  if (check_sparse_store(kv, 1) != TEMPO_OK) return 0;
+  return (size_t)kv->num_blocks * kv->num_kv_heads * 2 * kv->head_dim * 2;
+}
+
+int tempo_block_bounds(const tempo_kv* kv, void* bounds, int32_t batch, int32_t t, const int32_t* t_per_seq,
+                       int32_t count, const int32_t* count_per_seq, void* stream) {
+  int rc = check_sparse_store(kv, batch);
+  if (rc != TEMPO_OK) return rc;
+  if (!bounds || (rc = check_store(kv)) != TEMPO_OK) return TEMPO_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(bounds) & 15u) != 0) return TEMPO_ERR_SHAPE;
+  if (count < 1 || count > (1 << 24)) return TEMPO_ERR_SHAPE;
+  if (t < 0 || t > INT32_MAX - 64 - count) return TEMPO_ERR_RANGE;
+  if ((rc = check_step(kv, t + count - 1)) != TEMPO_OK) return rc;
+  // a step that completes no block
+  if (!t_per_seq && (t + count) / kv->block_size == t / kv->block_size) return TEMPO_OK;
+  StoreParams p = store_params(kv, batch, t, t_per_seq, count);
+  p.count_per_seq = count_per_seq;
+  return launch_status(launch_block_bounds(p, bounds, kv->head_dim, kv->dtype, static_cast<hipStream_t>(stream)), "block_bounds");
+}
+
+// Scores, 8 bytes for every block of every (sequence, kv head).
+size_t tempo_select_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t) {
+  if (check_sparse_store(kv, batch) != TEMPO_OK || check_heads(kv, batch, num_q_heads) != TEMPO_OK) return 0;
+  if (max_t < 0 || max_t > INT32_MAX - 64) return 0;
+  return align_up((size_t)batch * kv->num_kv_heads * (max_t / kv->block_size + 1) * sizeof(uint64_t), 256);
+}
+
+int tempo_select_blocks(const tempo_kv* kv, const void* bounds, const void* q, int32_t* selected, int32_t count,
+                        int32_t first, int32_t last, int32_t batch, int32_t num_q_heads, int32_t t,
+                        const int32_t* t_per_seq, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_sparse_store(kv, batch);
+  if (rc != TEMPO_OK) return rc;
+  if (!bounds || !q || !selected || (rc = check_store(kv)) != TEMPO_OK) return TEMPO_ERR_NULL;
+  if ((rc = check_heads(kv, batch, num_q_heads)) != TEMPO_OK) return rc;
+  if ((reinterpret_cast<uintptr_t>(bounds) & 15u) != 0) return TEMPO_ERR_SHAPE;
+  if ((rc = check_choice(kv, count, first, last)) != TEMPO_OK) return rc;
+  if (t < 0 || t > INT32_MAX - 64) return TEMPO_ERR_RANGE;
+  if ((rc = check_step(kv, t)) != TEMPO_OK) return rc;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
+  if (workspace_bytes < tempo_select_workspace_bytes(kv, batch, num_q_heads, t)) return TEMPO_ERR_WORKSPACE;
+  ChooseParams p;
+  p.bounds = bounds;
+  p.q = q;
+  p.block_table = kv->block_table;
+  p.t_per_seq = t_per_seq;
+  p.scores = static_cast<uint64_t*>(workspace);
+  p.selected = selected;
+  p.t = t;
+  p.z_log2 = ilog2_exact(kv->block_size);
+  p.max_blocks_per_seq = kv->max_blocks_per_seq;
+  p.num_blocks = kv->num_blocks;
+  p.Hkv = kv->num_kv_heads;
+  p.Hq = num_q_heads;
+  p.G = num_q_heads / kv->num_kv_heads;
+  p.tiles = t / kv->block_size + 1;
+  p.pick = count;
+  p.first = first;
+  p.last = last;
+  return launch_status(launch_select_blocks(p, batch, kv->head_dim, static_cast<hipStream_t>(stream)), "select_blocks");
+}
+
+// The list's places, block_size for each entry, are cut into splits as the keys of a step of so many would be.
+static void selected_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t count, tempo_plan* plan) {
+  make_plan(kv, batch, Hq, count * kv->block_size - 1, 0, false, 1, kMaxSplits, plan);
+  while (plan->waves > 1 && units_lds_bytes(plan->waves, Hq / kv->num_kv_heads, kv->head_dim) > kMaxLds) plan->waves /= 2;
+}
+
+size_t tempo_attn_selected_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t count) {
+  if (check_sparse_store(kv, batch) != TEMPO_OK || check_heads(kv, batch, num_q_heads) != TEMPO_OK) return 0;
+  if (check_list(kv, count) != TEMPO_OK) return 0;
+  tempo_plan plan;
+  selected_plan(kv, batch, num_q_heads, count, &plan);
+  return plan_bytes(kv, (int64_t)batch * num_q_heads, plan.num_splits);
+}
+
+int tempo_attn_selected(const tempo_kv* kv, const void* q, void* out, const int32_t* selected, int32_t count,
+                        int32_t batch, int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_sparse_store(kv, batch);
+  if (rc != TEMPO_OK) return rc;
+  if (!q || !out || !selected || (rc = check_store(kv)) != TEMPO_OK) return TEMPO_ERR_NULL;
+  if ((rc = check_heads(kv, batch, num_q_heads)) != TEMPO_OK) return rc;
+  if ((rc = check_list(kv, count)) != TEMPO_OK) return rc;
+  if (t < 0 || t > INT32_MAX - 64) return TEMPO_ERR_RANGE;
+  if ((rc = check_step(kv, t)) != TEMPO_OK) return rc;
+  if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
+  tempo_plan plan;
+  selected_plan(kv, batch, num_q_heads, count, &plan);
+  if (workspace_bytes < plan_bytes(kv, (int64_t)batch * num_q_heads, plan.num_splits)) return TEMPO_ERR_WORKSPACE;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  SelectParams p;
+  static_cast<AttnParams&>(p) = attn_params(kv, q, out, num_q_heads, t, t_per_seq, 0, scale, &plan, workspace, batch, 1);
+  p.direct = plan.num_splits == 1;
+  p.selected = selected;
+  p.pick = count;
+  rc = launch_status(launch_partial_selected(p, batch, kv->head_dim, kv->dtype, plan.num_splits, plan.waves, s), "attn_selected");
+  if (rc != TEMPO_OK || p.direct) return rc;
+  AttnParams join = p;  // every list has the same places
+  join.t = count * kv->block_size - 1;
+  join.t_per_seq = nullptr;
+  return launch_status(launch_combine_selected(join, batch, kv->head_dim, s), "attn_selected_combine");
+}
+
+size_t tempo_step_selected_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t,
+                                           int32_t count) {
+  const size_t scores = tempo_select_workspace_bytes(kv, batch, num_q_heads, max_t);
+  const size_t partials = tempo_attn_selected_workspace_bytes(kv, batch, num_q_heads, count);
+  return scores && partials ? scores + partials : 0;
+}
+
+int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, const void* k_new, const void* v_new,
+                               void* out, int32_t* selected, int32_t count, int32_t first, int32_t last, int32_t batch,
+                               int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, float scale, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  // everything the four calls below refuse, before the first of them launches anything
+  int rc = check_sparse_store(kv, batch);
+  if (rc != TEMPO_OK) return rc;
+  if (!bounds || !q || !k_new || !v_new || !out || !selected || (rc = check_store(kv)) != TEMPO_OK) return TEMPO_ERR_NULL;
+  if ((rc = check_heads(kv, batch, num_q_heads)) != TEMPO_OK) return rc;
+  if ((int64_t)batch * kv->num_kv_heads * kv->head_dim > INT32_MAX) return TEMPO_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(bounds) & 15u) != 0) return TEMPO_ERR_SHAPE;
+  if ((rc = check_choice(kv, count, first, last)) != TEMPO_OK) return rc;
+  if (t < 0 || t > INT32_MAX - 128) return TEMPO_ERR_RANGE;
+  if ((rc = check_step(kv, t)) != TEMPO_OK) return rc;
+  if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
+  const size_t scores = tempo_select_workspace_bytes(kv, batch, num_q_heads, t);
+  const size_t partials = tempo_attn_selected_workspace_bytes(kv, batch, num_q_heads, count);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
+  if (workspace_bytes < scores + partials) return TEMPO_ERR_WORKSPACE;
+  if ((rc = tempo_kv_append(kv, k_new, v_new, batch, t, t_per_seq, stream)) != TEMPO_OK) return rc;
+  if ((rc = tempo_block_bounds(kv, bounds, batch, t, t_per_seq, 1, nullptr, stream)) != TEMPO_OK) return rc;
+  if ((rc = tempo_select_blocks(kv, bounds, q, selected, count, first, last, batch, num_q_heads, t, t_per_seq, workspace,
+                                scores, stream)) != TEMPO_OK)
+    return rc;
+  return tempo_attn_selected(kv, q, out, selected, count, batch, num_q_heads, t, t_per_seq, scale,
+                             static_cast<char*>(workspace) + scores, partials, stream);
 }
 
 int tempo_discounted_sum(const float* r, float* g, int32_t batch, int32_t T, int32_t n, float gamma, void* stream) {

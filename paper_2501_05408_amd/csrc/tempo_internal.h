@@ -40,6 +40,31 @@ __host__ __device__ inline int64_t tile_off_v_bf16(int D, int slot, int d) {
   return (int64_t)grp * 32 * D + (int64_t)((dt * 64) + c * 16 + n) * 8 + e;
 }
 
+// 8-bit codes, keys.  Groups of 32 slots; a group is 2 row-tiles (slots 0..15, 16..31) x D/64 units of 1 KiB, 64 lanes x 16
+// bytes: lane (row + 16c) holds dims 64w + 8c .. +7 and 64w + 32 + 8c .. +7 of slot `row` of the tile, which, turned
+// into bf16, are the A operands of two 16x16x32 MFMAs, contraction steps 2w and 2w + 1 of the bf16 store.
+__host__ __device__ inline int64_t tile_off_k_e4m3(int D, int slot, int d) {
+  const int grp = slot >> 5, u = slot & 31, tile = u >> 4, row = u & 15;
+  const int w = d >> 6, h = (d >> 5) & 1, c = (d & 31) >> 3, e = d & 7;
+  return (int64_t)grp * 32 * D + (int64_t)(((tile * (D >> 6) + w) * 64) + c * 16 + row) * 16 + h * 8 + e;
+}
+
+// 8-bit codes, values.  A group is D/32 units: lane (n + 16c) holds dims 32w + n and 32w + 16 + n of the 8 slots
+// {4c..4c+3, 16+4c..16+4c+3}: the B operands of column tiles 2w and 2w + 1 of the bf16 store.
+__host__ __device__ inline int64_t tile_off_v_e4m3(int D, int slot, int d) {
+  const int grp = slot >> 5, u = slot & 31, half = u >> 4, uu = u & 15;
+  const int c = uu >> 2, e = (uu & 3) + 4 * half;
+  const int w = d >> 5, h = (d >> 4) & 1, n = d & 15;
+  return (int64_t)grp * 32 * D + (int64_t)((w * 64) + c * 16 + n) * 16 + h * 8 + e;
+}
+
+// Scale bytes of an 8-bit store: behind the codes of all blocks, block_size bytes for each (block, kv head).  In a group, keys: slots row
+// and 16 + row side by side, what lane (row + 16c) of the codes needs; values: the 8 slots of lane (n + 16c) side by side.
+__host__ __device__ inline int scale_off_k(int slot) { return (slot & ~31) + 2 * (slot & 15) + ((slot >> 4) & 1); }
+__host__ __device__ inline int scale_off_v(int slot) {
+  return (slot & ~31) + 8 * ((slot & 15) >> 2) + 4 * ((slot >> 4) & 1) + (slot & 3);
+}
+
 __host__ __device__ inline int clamp_block(int phys, int num_blocks) {
   return phys < 0 ? 0 : (phys >= num_blocks ? num_blocks - 1 : phys);
 }

@@ -11,7 +11,8 @@ import torch
 
 from . import tempo as T
 
-_TORCH_DTYPE = {T.TEMPO_BF16: torch.bfloat16, T.TEMPO_F32: torch.float32}
+# of queries, rows and answers (an 8-bit store's own pools are bytes)
+_TORCH_DTYPE = {T.TEMPO_BF16: torch.bfloat16, T.TEMPO_F32: torch.float32, T.TEMPO_E4M3: torch.bfloat16}
 
 
 class BlockStore:
@@ -21,6 +22,8 @@ class BlockStore:
     block_table: int32 tensor [batch][max_blocks_per_seq] (tile n -> physical
     block); by default sequence b owns blocks b*max_blocks_per_seq + n.
     fill: "nan" poisons the pool so that any read outside the visible range shows.
+    dtype T.TEMPO_E4M3: rows are kept in 8 bits with a scale each; pools are flat uint8 tensors of
+    T.tempo_kv_pool_bytes(kv) bytes, everything else is bf16.
     """
 
     def __init__(self, batch, num_q_heads, num_kv_heads, head_dim, block_size, max_t, dtype,
@@ -34,14 +37,18 @@ class BlockStore:
         self.max_blocks_per_seq = ring_blocks if ring_blocks else max_t // block_size + 1
         self.max_t = max_t if ring_blocks else self.max_blocks_per_seq * block_size - 1
         self.num_blocks = num_blocks if num_blocks is not None else batch * self.max_blocks_per_seq
-        tdt = _TORCH_DTYPE[dtype]
+        tdt = _TORCH_DTYPE[dtype] if dtype != T.TEMPO_E4M3 else torch.uint8
         shape = (self.num_blocks, num_kv_heads, block_size * head_dim)
+        if dtype == T.TEMPO_E4M3:
+            shape = (self.num_blocks * num_kv_heads * block_size * (head_dim + 1),)
         if pools is not None:
             self.k_pool, self.v_pool = pools
             assert tuple(self.k_pool.shape) == shape and tuple(self.v_pool.shape) == shape
         elif fill == "nan":
-            self.k_pool = torch.full(shape, float("nan"), dtype=tdt, device=self.device)
-            self.v_pool = torch.full(shape, float("nan"), dtype=tdt, device=self.device)
+            # (every byte 0xFF of an 8-bit pool: codes of NaN under scales that are not finite)
+            poison = float("nan") if tdt != torch.uint8 else 255
+            self.k_pool = torch.full(shape, poison, dtype=tdt, device=self.device)
+            self.v_pool = torch.full(shape, poison, dtype=tdt, device=self.device)
         else:
             self.k_pool = torch.zeros(shape, dtype=tdt, device=self.device)
             self.v_pool = torch.zeros(shape, dtype=tdt, device=self.device)
@@ -139,7 +146,8 @@ class BlockStore:
         self.rope = T.make_rope(self._rope_tables[0], self._rope_tables[1], self.D)
 
     def rope_rotate(self, x, y, t, t_per_seq=None):
-        T.tempo_rope_rotate(self.rope, x, y, self.dtype, x.shape[0], x.shape[1], t, t_per_seq)
+        dtype = T.TEMPO_F32 if self.dtype == T.TEMPO_F32 else T.TEMPO_BF16  # (rows of an 8-bit store are bf16)
+        T.tempo_rope_rotate(self.rope, x, y, dtype, x.shape[0], x.shape[1], t, t_per_seq)
         return y
 
     def rope_append(self, k_raw, v_new, t, t_per_seq=None):
@@ -205,6 +213,48 @@ class BlockStore:
         else:
             T.tempo_prefill_causal(self.kv, q, k_new, v_new, out, self.batch, self.Hq, t, count, count_per_seq, s,
                                    self._prefill_ws, nbytes)
+        return out
+
+    # -- sparse attention over selected blocks -------------------------------------------
+    def new_bounds(self):
+        """Memory for the bounds of the store's blocks (bf16 [num_blocks][Hkv][2][D])."""
+        return torch.empty((self.num_blocks, self.Hkv, 2, self.D), dtype=torch.bfloat16, device=self.device)
+
+    def update_bounds(self, bounds, t, count=1, t_per_seq=None, count_per_seq=None):
+        """The bounds of the blocks that steps t .. t+count-1, already written, complete."""
+        T.tempo_block_bounds(self.kv, bounds, self.batch, t, t_per_seq, count, count_per_seq)
+
+    def _selected_ws(self, nbytes):
+        if nbytes == 0:
+            raise T.TempoError(T.TEMPO_ERR_SHAPE, "workspace of the attention over selected blocks")
+        if getattr(self, "_sel_ws", None) is None or self._sel_ws.numel() < nbytes:
+            self._sel_ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        return self._sel_ws, self._sel_ws.numel()
+
+    def select_blocks(self, bounds, q, t, count, first=1, last=1, t_per_seq=None, selected=None):
+        """The `count` blocks that step t of every (sequence, kv head) attends over, int32 [batch][Hkv][count]."""
+        if selected is None:
+            selected = torch.empty((self.batch, self.Hkv, count), dtype=torch.int32, device=self.device)
+        ws, nbytes = self._selected_ws(T.tempo_select_workspace_bytes(self.kv, self.batch, self.Hq, t))
+        T.tempo_select_blocks(self.kv, bounds, q, selected, count, first, last, self.batch, self.Hq, t, t_per_seq, ws, nbytes)
+        return selected
+
+    def attend_selected(self, q, out, selected, t, t_per_seq=None, scale=None):
+        """Attention of step t over the blocks of `selected`."""
+        count = selected.shape[2]
+        ws, nbytes = self._selected_ws(T.tempo_attn_selected_workspace_bytes(self.kv, self.batch, self.Hq, count))
+        T.tempo_attn_selected(self.kv, q, out, selected, count, self.batch, self.Hq, t, t_per_seq,
+                              self.scale if scale is None else scale, ws, nbytes)
+        return out
+
+    def step_selected(self, bounds, q, k_new, v_new, out, t, count, first=1, last=1, t_per_seq=None, scale=None,
+                      selected=None):
+        """Append step t, keep the bounds, choose `count` blocks and attend over them."""
+        if selected is None:
+            selected = torch.empty((self.batch, self.Hkv, count), dtype=torch.int32, device=self.device)
+        ws, nbytes = self._selected_ws(T.tempo_step_selected_workspace_bytes(self.kv, self.batch, self.Hq, t, count))
+        T.tempo_decode_step_selected(self.kv, bounds, q, k_new, v_new, out, selected, count, first, last, self.batch,
+                                     self.Hq, t, t_per_seq, self.scale if scale is None else scale, ws, nbytes)
         return out
 
     def attend_with_plan(self, q, out, t, plan, window=0, t_per_seq=None, scale=None):

@@ -18,6 +18,7 @@ from . import build as _build
 
 TEMPO_BF16 = 0
 TEMPO_F32 = 1
+TEMPO_E4M3 = 2
 
 TEMPO_OK = 0
 TEMPO_ERR_NULL = -1
@@ -86,6 +87,7 @@ SIGNATURES = {
     "tempo_kv_release": (ctypes.c_int, [_i32, _i32, _i32, _i32p, _i32p]),
     "tempo_ring_blocks": (ctypes.c_int, [_i32, _i32, _i32, _i32p]),
     "tempo_kv_element_offset": (ctypes.c_int64, [_kvp, _i32, _i32, _i32, _i32, _i32]),
+    "tempo_kv_scale_offset": (ctypes.c_int64, [_kvp, _i32, _i32, _i32, _i32]),
     "tempo_kv_pool_bytes": (ctypes.c_size_t, [_kvp]),
     "tempo_attn_plan": (ctypes.c_int, [_kvp, _i32, _i32, _i32, _i32, _i32, _planp]),
     "tempo_attn_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32]),
@@ -143,6 +145,17 @@ SIGNATURES = {
     "tempo_attn_decode_combine": (ctypes.c_int, [_kvp, _vp, _i32, _i32, _i32, _vp, _i32, _planp, _vp,
                                                  ctypes.c_size_t, _vp]),
     "tempo_attn_plan_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _planp]),
+    "tempo_block_bounds_bytes": (ctypes.c_size_t, [_kvp]),
+    "tempo_block_bounds": (ctypes.c_int, [_kvp, _vp, _i32, _i32, _vp, _i32, _vp, _vp]),
+    "tempo_select_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32]),
+    "tempo_select_blocks": (ctypes.c_int, [_kvp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp,
+                                           ctypes.c_size_t, _vp]),
+    "tempo_attn_selected_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32]),
+    "tempo_attn_selected": (ctypes.c_int, [_kvp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, ctypes.c_float, _vp,
+                                           ctypes.c_size_t, _vp]),
+    "tempo_step_selected_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32, _i32]),
+    "tempo_decode_step_selected": (ctypes.c_int, [_kvp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
+                                                  _vp, ctypes.c_float, _vp, ctypes.c_size_t, _vp]),
     "tempo_discounted_sum": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, ctypes.c_float, _vp]),
     "tempo_stream_read": (ctypes.c_int, [_vp, ctypes.c_size_t, _vp, _i32, _vp]),
     "tempo_stream_copy": (ctypes.c_int, [_vp, _vp, ctypes.c_size_t, _i32, _vp]),
@@ -266,6 +279,10 @@ def tempo_ring_blocks(window: int, Z: int, queries: int = 1) -> int:
 
 def tempo_kv_element_offset(kv: tempo_kv, which: int, block: int, head: int, slot: int, d: int) -> int:
     return load().tempo_kv_element_offset(ctypes.byref(kv), which, block, head, slot, d)
+
+
+def tempo_kv_scale_offset(kv: tempo_kv, which: int, block: int, head: int, slot: int) -> int:
+    return load().tempo_kv_scale_offset(ctypes.byref(kv), which, block, head, slot)
 
 
 def tempo_kv_pool_bytes(kv: tempo_kv) -> int:
@@ -509,6 +526,49 @@ def tempo_attn_decode_combine(kv, out, batch, num_q_heads, t, t_per_seq, window,
                                             _ptr(t_per_seq), window, ctypes.byref(plan), _ptr(workspace),
                                             workspace_bytes, _stream(stream)),
            "tempo_attn_decode_combine")
+
+
+def tempo_block_bounds_bytes(kv: tempo_kv) -> int:
+    return load().tempo_block_bounds_bytes(ctypes.byref(kv))
+
+
+def tempo_block_bounds(kv, bounds, batch, t, t_per_seq, count, count_per_seq=None, stream=None):
+    _check(load().tempo_block_bounds(ctypes.byref(kv), _ptr(bounds), batch, t, _ptr(t_per_seq), count,
+                                     _ptr(count_per_seq), _stream(stream)), "tempo_block_bounds")
+
+
+def tempo_select_workspace_bytes(kv: tempo_kv, batch: int, num_q_heads: int, max_t: int) -> int:
+    return load().tempo_select_workspace_bytes(ctypes.byref(kv), batch, num_q_heads, max_t)
+
+
+def tempo_select_blocks(kv, bounds, q, selected, count, first, last, batch, num_q_heads, t, t_per_seq, workspace,
+                        workspace_bytes, stream=None):
+    _check(load().tempo_select_blocks(ctypes.byref(kv), _ptr(bounds), _ptr(q), _ptr(selected), count, first, last, batch,
+                                      num_q_heads, t, _ptr(t_per_seq), _ptr(workspace), workspace_bytes,
+                                      _stream(stream)), "tempo_select_blocks")
+
+
+def tempo_attn_selected_workspace_bytes(kv: tempo_kv, batch: int, num_q_heads: int, count: int) -> int:
+    return load().tempo_attn_selected_workspace_bytes(ctypes.byref(kv), batch, num_q_heads, count)
+
+
+def tempo_attn_selected(kv, q, out, selected, count, batch, num_q_heads, t, t_per_seq, scale, workspace,
+                        workspace_bytes, stream=None):
+    _check(load().tempo_attn_selected(ctypes.byref(kv), _ptr(q), _ptr(out), _ptr(selected), count, batch, num_q_heads, t,
+                                      _ptr(t_per_seq), scale, _ptr(workspace), workspace_bytes, _stream(stream)),
+           "tempo_attn_selected")
+
+
+def tempo_step_selected_workspace_bytes(kv: tempo_kv, batch: int, num_q_heads: int, max_t: int, count: int) -> int:
+    return load().tempo_step_selected_workspace_bytes(ctypes.byref(kv), batch, num_q_heads, max_t, count)
+
+
+def tempo_decode_step_selected(kv, bounds, q, k_new, v_new, out, selected, count, first, last, batch, num_q_heads, t,
+                               t_per_seq, scale, workspace, workspace_bytes, stream=None):
+    _check(load().tempo_decode_step_selected(ctypes.byref(kv), _ptr(bounds), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out),
+                                             _ptr(selected), count, first, last, batch, num_q_heads, t, _ptr(t_per_seq),
+                                             scale, _ptr(workspace), workspace_bytes, _stream(stream)),
+           "tempo_decode_step_selected")
 
 
 def tempo_discounted_sum(r, g, batch, T, n, gamma, stream=None):
