@@ -89,20 +89,225 @@ __device__ inline uint32_t values_of(uint32_t codes, bool high, float scale) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// Read-back, element by element: out[b][j - j0][head][d].
+// ---- by 32-slot groups ------------------------------------------------------------------
+// One wavefront per (sequence, head, group).  A lane works on blocks of 4 consecutive slots x 8 consecutive dims, D/8
+// lanes side by side on the same slots: 16-byte pieces of 4 rows in the caller's arrays, and in the store 8 codes of each
+// key row and, of the values, 4 codes (the 4 slots) of each dim, between which a block is turned in registers.  The group's
+// image passes through LDS, so that the store is read and written in whole units of 1 KiB, the rows in runs of D elements.
+// Bound by memory: 8 x 2047 rows in 8 heads of 128 are written in 24.6 us (101 MB, 4.1 TB/s; a large copy moves 4.9) and
+// read back in 16.3; row by row and element by element it was 52.6 and 73.2.
+
+// 4 words of 4 bytes, a[i] = byte i of every column: columns to rows.
+__device__ inline void turn4(uint32_t* a) {
+  const uint32_t t0 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400), t1 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602);
+  const uint32_t t2 = __builtin_amdgcn_perm(a[3], a[2], 0x05010400), t3 = __builtin_amdgcn_perm(a[3], a[2], 0x07030602);
+  a[0] = __builtin_amdgcn_perm(t2, t0, 0x05040100);
+  a[1] = __builtin_amdgcn_perm(t2, t0, 0x07060302);
+  a[2] = __builtin_amdgcn_perm(t3, t1, 0x05040100);
+  a[3] = __builtin_amdgcn_perm(t3, t1, 0x07060302);
+}
+
+// Maximum of both 16-bit halves over the D/8 lanes that hold a row.
 template <int D>
-__global__ __launch_bounds__(256) void kv_gather_e4m3(StoreParams p, uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out,
-                                                      int j0, int count) {
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (idx >= (int64_t)p.batch * count * p.Hkv * D) return;
-  const int d = (int)(idx % D), head = (int)(idx / D % p.Hkv);
-  const int j = j0 + (int)(idx / ((int64_t)D * p.Hkv) % count), b = (int)(idx / ((int64_t)D * p.Hkv * count));
-  const int slot = j & ((1 << p.z_log2) - 1);
-  const int64_t first = tile_slot(p, b, head, j), scales = all_slots(p) * D + first;
-  const uint8_t* const kp = static_cast<const uint8_t*>(p.k_pool);
-  const uint8_t* const vp = static_cast<const uint8_t*>(p.v_pool);
-  if (k_out) k_out[idx] = (uint16_t)values_of(kp[first * D + tile_off_k_e4m3(D, slot, d)], false, scale_of(kp[scales + scale_off_k(slot)]));
-  if (v_out) v_out[idx] = (uint16_t)values_of(vp[first * D + tile_off_v_e4m3(D, slot, d)], false, scale_of(vp[scales + scale_off_v(slot)]));
+__device__ inline uint32_t row_max(uint32_t v) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  auto step = [&](uint32_t o) { v = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v), __builtin_bit_cast(u16x2, o))); };
+  step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lanes 1, 0, 3, 2 of four
+  step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // 2, 3, 0, 1
+  step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));  // eight lanes reversed
+  if (D == 128) step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));  // sixteen
+  return v;
+}
+
+// Offsets of a block inside a group's image: of 8 codes of key slot 4 sg + i, dims 8 part ..; of the 4 codes of dim
+// 8 part + k, slots 4 sg .. +3.
+template <int D>
+__device__ inline int key_piece(int sg, int part, int i) {
+  const int tile = sg >> 2, row = 4 * (sg & 3) + i, w = part >> 3, h = (part >> 2) & 1, c = part & 3;
+  return ((tile * (D >> 6) + w) * 64 + c * 16 + row) * 16 + h * 8;
+}
+template <int D>
+__device__ inline int value_piece(int sg, int part, int k) {
+  const int d = 8 * part + k, c = sg & 3, half = sg >> 2;
+  return ((d >> 5) * 64 + c * 16 + (d & 15)) * 16 + ((d >> 4) & 1) * 8 + half * 4;
+}
+// The image in LDS: 16 bytes more for every 256, so that the pieces that lanes touch together lie in different banks.
+__host__ __device__ constexpr int in_lds(int at) { return at + (at >> 8) * 16; }
+
+template <int D>
+__global__ __launch_bounds__(64) void kv_append_groups_e4m3(StoreParams p, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new) {
+  constexpr int PARTS = D / 8, BLOCKS = 8 * PARTS / 64;  // blocks a lane works on
+  __shared__ __align__(16) uint8_t image[in_lds(32 * D)];
+  const int lane = threadIdx.x;
+  const int g = blockIdx.x, head = blockIdx.y, b = blockIdx.z;
+  const int rows_b = rows_of(p, b) < p.count ? rows_of(p, b) : p.count;
+  const int t0 = ((p.t >> 5) + g) << 5;  // first step of this group
+  const int first_row = t0 - p.t;        // source row of slot 0 (negative: before the call)
+  const int lo = first_row < 0 ? -first_row : 0;
+  const int hi = rows_b - first_row < 32 ? rows_b - first_row : 32;  // slots lo .. hi-1 are written
+  if (hi <= lo) return;                  // uniform over the workgroup
+  const bool whole = lo == 0 && hi == 32;
+  const int64_t slot0 = tile_slot(p, b, head, t0) + (t0 & ((1 << p.z_log2) - 1)), scales = all_slots(p) * D + slot0;
+  const int64_t row0 = ((int64_t)b * p.src_steps + first_row) * p.Hkv + head;  // (rows are Hkv apart)
+
+  // The caller's pieces; rows outside the call are read as its nearest row and not written.
+  u32x4 k[BLOCKS][4], v[BLOCKS][4];
+#pragma unroll
+  for (int n = 0; n < BLOCKS; ++n) {
+    const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int slot = 4 * sg + i;
+      const int64_t at = (row0 + (int64_t)(slot < lo ? lo : (slot < hi ? slot : hi - 1)) * p.Hkv) * D + 8 * part;
+      k[n][i] = *reinterpret_cast<const u32x4*>(k_new + at);
+      v[n][i] = *reinterpret_cast<const u32x4*>(v_new + at);
+    }
+  }
+  if (p.rope_cos) {  // a piece and its partner D/2 dims away are turned together, each lane for its own
+#pragma unroll
+    for (int n = 0; n < BLOCKS; ++n) {
+      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+      const int other = part < PARTS / 2 ? part + PARTS / 2 : part - PARTS / 2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int slot = 4 * sg + i, from = slot < lo ? lo : (slot < hi ? slot : hi - 1);
+        u32x4 o = *reinterpret_cast<const u32x4*>(k_new + (row0 + (int64_t)from * p.Hkv) * D + 8 * other);
+        if (part < PARTS / 2) rotate_pieces(p.rope_cos, p.rope_sin, t0 + from, D / 2, 8 * part, k[n][i], o);
+        else rotate_pieces(p.rope_cos, p.rope_sin, t0 + from, D / 2, 8 * other, o, k[n][i]);
+      }
+    }
+  }
+
+  uint8_t* const k_pool = static_cast<uint8_t*>(p.k_pool);
+  uint8_t* const v_pool = static_cast<uint8_t*>(p.v_pool);
+  uint32_t vc[BLOCKS][2][4];  // values: codes of slot i, dims 0..3 and 4..7 of the block; turned: of dim k, slots 0..3
+#pragma unroll
+  for (int n = 0; n < BLOCKS; ++n) {
+    const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t kt = 0, vt = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        kt = top_of(k[n][i][e], kt);
+        vt = top_of(v[n][i][e], vt);
+      }
+      const uint32_t top = row_max<D>(kt | (vt << 16));
+      const uint32_t Ek = (uint32_t)scale_byte(top & 0xFFFFu), Ev = (uint32_t)scale_byte(top >> 16);
+      const float ki = inverse_scale_of(Ek), vi = inverse_scale_of(Ev), km = largest_code(Ek), vm = largest_code(Ev);
+      const u32x4 a = k[n][i], z = v[n][i];
+      *reinterpret_cast<uint2*>(image + in_lds(key_piece<D>(sg, part, i))) =
+          uint2{codes_of(a.x, ki, km) | (codes_of(a.y, ki, km) << 16), codes_of(a.z, ki, km) | (codes_of(a.w, ki, km) << 16)};
+      vc[n][0][i] = codes_of(z.x, vi, vm) | (codes_of(z.y, vi, vm) << 16);
+      vc[n][1][i] = codes_of(z.z, vi, vm) | (codes_of(z.w, vi, vm) << 16);
+      const int slot = 4 * sg + i;
+      if (part == 0 && slot >= lo && slot < hi) {
+        k_pool[scales + scale_off_k(slot)] = (uint8_t)Ek;
+        v_pool[scales + scale_off_v(slot)] = (uint8_t)Ev;
+      }
+    }
+  }
+  __syncthreads();
+  // keys: a unit's 16 bytes belong to one slot
+#pragma unroll
+  for (int u = 0; u < D / 32; ++u) {
+    const int slot = 16 * (u / (D / 64)) + (lane & 15), at = u * 1024 + lane * 16;
+    if (slot >= lo && slot < hi) *reinterpret_cast<u32x4*>(k_pool + slot0 * D + at) = *reinterpret_cast<const u32x4*>(image + in_lds(at));
+  }
+  if (!whole) {  // this call's slots only, byte by byte: another launch may write the others at the same time
+#pragma unroll
+    for (int n = 0; n < BLOCKS; ++n) {
+      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (4 * sg + i < lo || 4 * sg + i >= hi) continue;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v_pool[slot0 * D + value_piece<D>(sg, part, e) + i] = (uint8_t)(vc[n][e >> 2][i] >> (8 * (e & 3)));
+      }
+    }
+    return;
+  }
+  __syncthreads();  // the image is written again
+#pragma unroll
+  for (int n = 0; n < BLOCKS; ++n) {
+    const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      turn4(vc[n][q]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(image + in_lds(value_piece<D>(sg, part, 4 * q + e))) = vc[n][q][e];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < D / 32; ++u) {
+    const int at = u * 1024 + lane * 16;
+    *reinterpret_cast<u32x4*>(v_pool + slot0 * D + at) = *reinterpret_cast<const u32x4*>(image + in_lds(at));
+  }
+}
+
+// Read-back of steps j0 .. j0+count-1: out[b][j - j0][head][d].
+template <int D>
+__global__ __launch_bounds__(64) void kv_gather_e4m3(StoreParams p, uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out, int j0, int count) {
+  constexpr int PARTS = D / 8, BLOCKS = 8 * PARTS / 64, UNITS = D / 32;
+  __shared__ __align__(16) uint8_t image[in_lds(32 * D)];
+  const int lane = threadIdx.x;
+  const int g = blockIdx.x, head = blockIdx.y, b = blockIdx.z;
+  const int t0 = ((j0 >> 5) + g) << 5, first_row = t0 - j0;
+  const int lo = first_row < 0 ? -first_row : 0, hi = count - first_row < 32 ? count - first_row : 32;
+  const int64_t slot0 = tile_slot(p, b, head, t0) + (t0 & ((1 << p.z_log2) - 1)), scales = all_slots(p) * D + slot0;
+  const int64_t row0 = ((int64_t)b * count + first_row) * p.Hkv + head;
+  const uint8_t* const k_pool = static_cast<const uint8_t*>(p.k_pool);
+  const uint8_t* const v_pool = static_cast<const uint8_t*>(p.v_pool);
+  u32x4 k[UNITS], v[UNITS];
+  if (k_out) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) k[u] = *reinterpret_cast<const u32x4*>(k_pool + slot0 * D + u * 1024 + lane * 16);
+  }
+  if (v_out) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) v[u] = *reinterpret_cast<const u32x4*>(v_pool + slot0 * D + u * 1024 + lane * 16);
+  }
+  auto piece_out = [&](uint16_t* out, int sg, int part, int i, uint32_t a, uint32_t z, float scale) {
+    const int slot = 4 * sg + i;
+    if (slot < lo || slot >= hi) return;
+    const u32x4 o = {values_of(a, false, scale), values_of(a, true, scale), values_of(z, false, scale), values_of(z, true, scale)};
+    *reinterpret_cast<u32x4*>(out + (row0 + (int64_t)slot * p.Hkv) * D + 8 * part) = o;
+  };
+  if (k_out) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) *reinterpret_cast<u32x4*>(image + in_lds(u * 1024 + lane * 16)) = k[u];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < BLOCKS; ++n) {
+      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint2 x = *reinterpret_cast<const uint2*>(image + in_lds(key_piece<D>(sg, part, i)));
+        piece_out(k_out, sg, part, i, x.x, x.y, scale_of(k_pool[scales + scale_off_k(4 * sg + i)]));
+      }
+    }
+    __syncthreads();
+  }
+  if (v_out) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) *reinterpret_cast<u32x4*>(image + in_lds(u * 1024 + lane * 16)) = v[u];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < BLOCKS; ++n) {
+      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+      uint32_t x[2][4];  // of dim k, slots 0..3; turned: of slot i, dims 0..3 and 4..7
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[q][e] = *reinterpret_cast<const uint32_t*>(image + in_lds(value_piece<D>(sg, part, 4 * q + e)));
+        turn4(x[q]);
+      }
+      const uint32_t s4 = *reinterpret_cast<const uint32_t*>(v_pool + scales + scale_off_v(4 * sg));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) piece_out(v_out, sg, part, i, x[0][i], x[1][i], scale_of((s4 >> (8 * i)) & 0xFFu));
+    }
+  }
 }
 
 }  // namespace
@@ -110,6 +315,16 @@ __global__ __launch_bounds__(256) void kv_gather_e4m3(StoreParams p, uint16_t* _
 hipError_t launch_append_e4m3(const StoreParams& p, const void* k_new, const void* v_new, int D, hipStream_t stream) {
   const uint16_t* k = static_cast<const uint16_t*>(k_new);
   const uint16_t* v = static_cast<const uint16_t*>(v_new);
+  // Uniform first step and at least one whole 32-slot group: by groups, unless the last one lies in the first one's slots
+  // (a ring whose every slot is written, from the middle of a group on), where two launches would be needed.
+  const int first_whole = (p.t + 31) >> 5, past_whole = (p.t + p.count) >> 5;
+  const int groups = ((p.t + p.count - 1) >> 5) - (p.t >> 5) + 1;
+  const int64_t ring_slots = p.tile_mask == INT32_MAX ? INT64_MAX : ((int64_t)p.tile_mask + 1) << p.z_log2;
+  if (!p.t_per_seq && past_whole > first_whole && (int64_t)groups * 32 <= ring_slots) {
+    const dim3 grid(groups, p.Hkv, p.batch);
+    if (D == 128) return launch(kv_append_groups_e4m3<128>, grid, dim3(64), 0, stream, p, k, v);
+    return launch(kv_append_groups_e4m3<64>, grid, dim3(64), 0, stream, p, k, v);
+  }
   const int64_t threads = (int64_t)p.batch * p.count * p.Hkv * (D / 4);
   const dim3 grid((unsigned)((threads + 255) / 256));
   if (D == 128) return launch(kv_append_e4m3<128>, grid, dim3(256), 0, stream, p, k, v);
@@ -117,13 +332,12 @@ hipError_t launch_append_e4m3(const StoreParams& p, const void* k_new, const voi
 }
 
 hipError_t launch_gather_e4m3(const StoreParams& p, void* k_out, void* v_out, int D, int j0, int count, hipStream_t stream) {
-  const int64_t total = (int64_t)p.batch * count * p.Hkv * D;
-  if (total == 0) return hipSuccess;
-  const dim3 grid((unsigned)((total + 255) / 256));
+  if (count == 0) return hipSuccess;
+  const dim3 grid((unsigned)((int)(((int64_t)j0 + count - 1) >> 5) - (j0 >> 5) + 1), (unsigned)p.Hkv, (unsigned)p.batch);
   uint16_t* k = static_cast<uint16_t*>(k_out);
   uint16_t* v = static_cast<uint16_t*>(v_out);
-  if (D == 128) return launch(kv_gather_e4m3<128>, grid, dim3(256), 0, stream, p, k, v, j0, count);
-  return launch(kv_gather_e4m3<64>, grid, dim3(256), 0, stream, p, k, v, j0, count);
+  if (D == 128) return launch(kv_gather_e4m3<128>, grid, dim3(64), 0, stream, p, k, v, j0, count);
+  return launch(kv_gather_e4m3<64>, grid, dim3(64), 0, stream, p, k, v, j0, count);
 }
 
 }  // namespace tempo
