@@ -11,9 +11,9 @@ struct SelectParams : AttnParams {
   int32_t pick;
 };
 
-// Dynamic LDS of a launch of attn_units.
+// Dynamic LDS of a launch of attn_units: the merge of its wavefronts, and the codes and scale bytes of a new row.
 inline size_t units_lds_bytes(int waves, int columns, int D) {
-  return (size_t)waves * (32 + (size_t)(columns < 16 ? columns : 16) * D) * sizeof(float);
+  return (size_t)waves * (32 + (size_t)(columns < 16 ? columns : 16) * D) * sizeof(float) + 2 * (size_t)D + 16;
 }
 
 // Score and choice of blocks.

@@ -21,6 +21,8 @@
 namespace tempo {
 namespace {
 
+constexpr int kNoKey = -1;  // in the place of a group's first key: none that the step sees
+
 // The register image of a 32-slot group: keys, values, and in an 8-bit store the lane's scale bytes.
 template <int D, bool k8>
 struct Image {
@@ -106,6 +108,97 @@ __device__ __forceinline__ bf16x8 scaled_weights(bf16x8 pa, uint2 scales) {
   return pa;
 }
 
+// ---- fused write of an 8-bit row (Section 6, "in-place writes") ------------------------------------
+// The wavefront that holds step t's group quantises the step's key and value itself: lanes 0 .. D/8-1 hold the key row, 8
+// dims each, the next D/8 the value row.  It writes them to the store, and puts them into the group's register image from a
+// copy in LDS, [key codes D][value codes D][key scale byte][value scale byte], when it comes to that group.  A launch less
+// than writing first (us a step, 24/8 heads of 128, fused / written first: 1 sequence, 300 keys 6.6 / 11.2; 32 sequences, 1000
+// keys 12.6 / 15.5; even at 1024 pairs of 4000 keys, 175.0 / 173.3).
+template <int D>
+__device__ __forceinline__ u32x4 fetch_new_rows(const AttnParams& p, int b, int hkv, int lane) {
+  const int lanes = D / 8, at = lane % (2 * lanes);  // (the lanes beyond hold copies)
+  const uint16_t* const src = static_cast<const uint16_t*>(at < lanes ? p.k_new : p.v_new) + ((int64_t)b * p.Hkv + hkv) * D + (at % lanes) * 8;
+  return *reinterpret_cast<const u32x4*>(src);
+}
+
+template <int D, bool kRope>
+__device__ __forceinline__ void write_new_rows(const AttnParams& p, u32x4 x, int t_b, int64_t slot, int64_t slots, bool store, int lane, uint8_t* stage) {
+  constexpr int LANES = D / 8;
+  if (kRope) {  // the partner dims, D/2 away, lie in lane ^ (LANES / 2)
+    u32x4 other;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) other[w] = (uint32_t)__shfl_xor((int)x[w], LANES / 2);
+    const int d = 8 * (lane % LANES);
+    u32x4 lo = d < D / 2 ? x : other, hi = d < D / 2 ? other : x;
+    rotate_pieces(p.rope_cos, p.rope_sin, t_b, D / 2, d % (D / 2), lo, hi);
+    if (lane < LANES) x = d < D / 2 ? lo : hi;
+  }
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = top_of(x[i], top);
+#pragma unroll
+  for (int m = LANES / 2; m > 0; m >>= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)top, m);
+    top = o > top ? o : top;
+  }
+  const uint32_t E = (uint32_t)scale_byte(top);
+  const float inverse = inverse_scale_of(E), most = largest_code(E);
+  const uint32_t lo = codes_of(x.x, inverse, most) | (codes_of(x.y, inverse, most) << 16);
+  const uint32_t hi = codes_of(x.z, inverse, most) | (codes_of(x.w, inverse, most) << 16);
+  if (lane >= 2 * LANES) return;
+  const bool value = lane >= LANES;
+  const int part = lane % LANES, u = t_b & 31;
+  *reinterpret_cast<uint2*>(stage + lane * 8) = uint2{lo, hi};
+  if (part == 0) stage[2 * D + value] = (uint8_t)E;
+  if (!store) return;
+  // slot: of the group's first step, in the numbering of all slots
+  uint8_t* const pool = static_cast<uint8_t*>(value ? p.v_pool : p.k_pool);
+  if (!value) {
+    *reinterpret_cast<uint2*>(pool + slot * D + tile_off_k_e4m3(D, u, 8 * part)) = uint2{lo, hi};
+  } else {
+    uint8_t* const to = pool + slot * D + tile_off_v_e4m3(D, u, 8 * part);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      to[16 * i] = (uint8_t)(lo >> (8 * i));
+      to[16 * (4 + i)] = (uint8_t)(hi >> (8 * i));
+    }
+  }
+  if (part == 0) pool[slots * D + slot + (value ? scale_off_v(u) : scale_off_k(u))] = (uint8_t)E;
+}
+
+template <int D>
+__device__ __forceinline__ void patch_keys(int t_b, int lane, const uint8_t* stage, Image<D, true>& g) {
+  const int u = t_b & 31, row = u & 15, tile = u >> 4, c = lane >> 4;
+  if ((lane & 15) != row) return;
+#pragma unroll
+  for (int w = 0; w < D / 64; ++w) {
+    const uint2 a = *reinterpret_cast<const uint2*>(stage + 64 * w + 8 * c), b = *reinterpret_cast<const uint2*>(stage + 64 * w + 32 + 8 * c);
+    const u32x4 val = {a.x, a.y, b.x, b.y};
+    g.k[w] = tile == 0 ? val : g.k[w];
+    g.k[D / 64 + w] = tile == 1 ? val : g.k[D / 64 + w];
+  }
+  const uint32_t E = stage[2 * D];
+  g.k_scales = tile == 0 ? (g.k_scales & 0xFF00u) | E : (g.k_scales & 0xFFu) | (E << 8);
+}
+
+template <int D>
+__device__ __forceinline__ void patch_values(int t_b, int lane, const uint8_t* stage, Image<D, true>& g) {
+  const int u = t_b & 31, row = u & 15, tile = u >> 4, n = lane & 15, shift = 8 * (row & 3);
+  if ((lane >> 4) != (row >> 2)) return;
+  const uint32_t others = ~(0xFFu << shift);
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w) {
+    const uint32_t a = (uint32_t)stage[D + 32 * w + n] << shift, b = (uint32_t)stage[D + 32 * w + 16 + n] << shift;
+    g.v[w].x = tile == 0 ? (g.v[w].x & others) | a : g.v[w].x;
+    g.v[w].y = tile == 1 ? (g.v[w].y & others) | a : g.v[w].y;
+    g.v[w].z = tile == 0 ? (g.v[w].z & others) | b : g.v[w].z;
+    g.v[w].w = tile == 1 ? (g.v[w].w & others) | b : g.v[w].w;
+  }
+  const uint32_t E = (uint32_t)stage[2 * D + 1] << shift;
+  g.v_scales.x = tile == 0 ? (g.v_scales.x & others) | E : g.v_scales.x;
+  g.v_scales.y = tile == 1 ? (g.v_scales.y & others) | E : g.v_scales.y;
+}
+
 // Merge of the workgroup's wavefronts, as in attn_partial_bf16.hip; column j is column first_col + j of the call.
 template <int D, int NW, bool kSelect>
 __device__ __forceinline__ void merge_units(const AttnParams& p, const float* smem, int first_col, int ncols, int b, int hkv, int split) {
@@ -176,29 +269,30 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
     end = rg.hi < ce ? rg.hi : ce;
   }
   const int g_last = end >> 5;
+  const int from = kSelect ? 0 : start, upto = kSelect ? t_b : end;  // keys
   const int64_t slots = ((int64_t)p.num_blocks * p.Hkv) << p.z_log2;  // of the store
   const_i32_ptr const table = (const_i32_ptr)p.block_table + (int64_t)b * p.max_blocks_per_seq;
   const_i32_ptr const list = kSelect ? (const_i32_ptr)p.selected + ((int64_t)b * p.Hkv + hkv) * p.pick : nullptr;
 
-  // First key of the group at position group `at`; negative: none that step t_b sees.
+  // First key of the group at position group `at`; kNoKey: none that step t_b sees.
   auto key_of = [&](int at) __attribute__((always_inline)) {
     if constexpr (!kSelect) return at << 5;
     const int pos = at << 5, n = list[pos >> p.z_log2];
-    if (n < 0 || n > (t_b >> p.z_log2)) return -1;
-    const int key = (n << p.z_log2) + (pos & ((1 << p.z_log2) - 1));
-    return key <= t_b ? key : -1;
+    if (n < 0 || n > (t_b >> p.z_log2)) return kNoKey;
+    const int first = (n << p.z_log2) + (pos & ((1 << p.z_log2) - 1));
+    return first <= t_b ? first : kNoKey;
   };
   // From position group `at` on, in this wavefront's turn, the first one with keys.
-  auto next_of = [&](int at, int& key) __attribute__((always_inline)) {
+  auto next_of = [&](int at, int& first) __attribute__((always_inline)) {
     for (; at <= g_last; at += nwaves) {
-      key = key_of(at);
-      if (!kSelect || key >= 0) break;
+      first = key_of(at);
+      if (!kSelect || first != kNoKey) break;
     }
     return at;
   };
-  auto slot_of = [&](int key) __attribute__((always_inline)) {
-    const int phys = clamp_block(table[(key >> p.z_log2) & p.tile_mask], p.num_blocks);
-    return (((int64_t)phys * p.Hkv + hkv) << p.z_log2) + (key & ((1 << p.z_log2) - 1));
+  auto slot_of = [&](int first) __attribute__((always_inline)) {
+    const int phys = clamp_block(table[(first >> p.z_log2) & p.tile_mask], p.num_blocks);
+    return (((int64_t)phys * p.Hkv + hkv) << p.z_log2) + (first & ((1 << p.z_log2) - 1));
   };
 
   Image<D, k8> g;
@@ -213,7 +307,6 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
   // Columns and their ranges, as in attn_partial_bf16.hip.
   const int all_cols = p.queries * p.G - first_col, ncols = all_cols < 16 ? all_cols : 16;
   const int t_end = t_b + p.queries - 1;
-  const int from = kSelect ? 0 : start, upto = kSelect ? t_b : end;  // keys
   const int lo_last = (p.window > 0 && t_end - p.window + 1 > 0) ? t_end - p.window + 1 : 0;
   const int all_lo = lo_last > from ? lo_last : from;
   const int all_hi = t_b < upto ? t_b : upto;
@@ -238,33 +331,45 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
   }
   if (kRope) rotate_query<D>(p, t_b + cq, lane, qreg);
 
+  // A fused write lands in group t_b >> 5, which only the newest split holds.
+  int key_new = -1;  // first key of that group, in the wavefront that will reach it
+  uint8_t* const stage = reinterpret_cast<uint8_t*>(smem + nwaves * (32 + ncols * D));
+  if constexpr (k8 && !kSelect) {
+    const int grp_new = t_b >> 5;
+    if (p.k_new && blockIdx.z == 0 && grp_new >= grp && (grp_new - grp) % nwaves == 0) {
+      key_new = grp_new << 5;
+      const u32x4 rows = fetch_new_rows<D>(p, b, hkv, lane);
+      write_new_rows<D, kRope>(p, rows, t_b, slot_of(key_new), slots, first_col == 0, lane, stage);
+    }
+  }
+
   WaveState<D> st;
   st.m = -INFINITY;
   st.l = 0.f;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) st.acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  while (grp <= g_last) {
-    int key_nxt = 0;
-    const int nxt = next_of(grp + nwaves, key_nxt);
-    const bool more = nxt <= g_last;
+  // The group in the registers; `more`: and request the one whose first key is key_nxt.
+  auto group = [&](int key_nxt, bool more) __attribute__((always_inline)) {
     const int64_t slot_nxt = more ? slot_of(key_nxt) : 0;
-
+    if constexpr (k8 && !kSelect) {
+      if (key == key_new) patch_keys<D>(t_b, lane, stage, g);
+    }
     float x[8];
     image_logits<D, k8>(p, qreg, g, x);
     if (more) load_image_keys<D, k8>(p, slot_nxt, slots, lane, g);
-
-    const bool cut = key < all_lo || key + 31 > all_hi;  // wave-uniform
-    uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};             // bf16 values: masks of the lane's 8 slots
-    uint2 keep8 = {~0u, ~0u};
-    if (cut) {
+    // Slots that no step of the call sees may be unwritten: codes and scales of 0, bf16 values of 0, under the weight of 0.
+    uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};               // bf16 values: masks of the lane's 8 slots
+    uint2 keep8 = {~0u, ~0u};                              // codes
+    if (key < all_lo || key > all_hi - 31) {               // wave-uniform: a group that some column's range cuts
       mask_logits(key >> 5, lo_col, hi_col, lane, x);
       if constexpr (k8) keep8 = seen_bytes(key, from, seen_hi, lane);
       else value_masks(key >> 5, from, seen_hi, lane, keep);
     }
     bf16x8 pa = softmax_update<D>(x, lane, st);
-
-    // Slots that no step of the call sees may be unwritten: codes and scales of 0 under the weight of 0.
+    if constexpr (k8 && !kSelect) {
+      if (key == key_new) patch_values<D>(t_b, lane, stage, g);
+    }
     if constexpr (k8) {
       pa = scaled_weights(pa, uint2{g.v_scales.x & keep8.x, g.v_scales.y & keep8.y});
 #pragma unroll
@@ -282,8 +387,19 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
       }
     }
     if (more) load_image_values<D, k8>(p, slot_nxt, slots, lane, g);
-    grp = nxt;
-    key = key_nxt;
+  };
+  // The last group has a body of its own: behind a condition, requests make every wait one for all of them
+  // (attn_partial_bf16.hip).
+  if (grp <= g_last) {
+    for (;;) {
+      int key_nxt = 0;
+      const int nxt = next_of(grp + nwaves, key_nxt);
+      if (nxt > g_last) break;
+      group(key_nxt, true);
+      grp = nxt;
+      key = key_nxt;
+    }
+    group(0, false);
   }
 
   const float l_tot = column_sum(st.l);

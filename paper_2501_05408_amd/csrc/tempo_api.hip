@@ -198,7 +198,11 @@ void make_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int
                             : (int64_t)batch * kv->num_kv_heads * (kv->dtype == TEMPO_F32 ? (columns + 15) / 16 : 1);
   const int64_t len = (window > 0 && window < (int64_t)t_max + 1) ? window : (int64_t)t_max + 1;
   const int bytes_per_key = 2 * kv->head_dim * (kv->dtype == TEMPO_E4M3 ? 1 : kv->dtype == TEMPO_BF16 ? 2 : 4);  // K and V of one head
-  const int k_max = ragged ? 10 : 30;
+  // (8 bits: the same bytes are twice the keys; and a window of so many is not cut at all, us a call for 48 sequences of
+  // 32/8 heads of 64 at steps up to 8191, window 1000: 2 splits of 1024 15.3, one 11.1; 64 of 24/8 heads of 128, causal, at
+  // steps up to 2000: 2 splits of 1024 30.6, one of 2048 27.6)
+  const bool k8 = kv->dtype == TEMPO_E4M3;
+  const int k_max = !ragged || (k8 && window > 0 && window <= 2048) ? 30 : k8 ? 11 : 10;
   int best_k = -1;
   double best_cost = -1.0;
   double costs[26];
@@ -426,13 +430,6 @@ int do_partial(const tempo_kv* kv, const void* q, const void* k_new, const void*
   if (kv->dtype == TEMPO_BF16 && queries * p.G > kNarrowColumns)  // a wide block: kernels of their own, key range split as planned
     return launch_status(launch_block_bf16(p, batch, kv->head_dim, gs, stream), "attn_block_partial");
   if (kv->dtype == TEMPO_E4M3) {
-    if (k_new) {  // its kernel reads the store only
-      StoreParams sp = store_params(kv, batch, t, t_per_seq);
-      sp.rope_cos = p.rope_cos;
-      sp.rope_sin = p.rope_sin;
-      const int rc = launch_status(launch_append_e4m3(sp, k_new, v_new, kv->head_dim, stream), "kv_append");
-      if (rc != TEMPO_OK) return rc;
-    }
     return launch_status(launch_partial_e4m3(p, batch, kv->head_dim, gs, plan->waves, stream), "attn_decode_partial");
   }
   const hipError_t e = kv->dtype == TEMPO_BF16
