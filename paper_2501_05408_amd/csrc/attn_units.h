@@ -18,7 +18,7 @@ inline size_t units_lds_bytes(int waves, int columns, int D) {
 
 // Score and choice of blocks.
 struct ChooseParams {
-  const void* bounds;         // [num_blocks][Hkv][2][D] bf16
+  void* bounds;               // [num_blocks][Hkv][2][D] bf16
   const void* q;              // [B][Hq][D] bf16
   const int32_t* block_table;
   const int32_t* t_per_seq;   // may be null
@@ -41,7 +41,8 @@ TEMPO_LAUNCHER launch_partial_e4m3(const AttnParams& p, int batch, int D, int gr
 TEMPO_LAUNCHER launch_partial_selected(const SelectParams& p, int batch, int D, int dtype, int grid_splits, int waves, hipStream_t stream);
 TEMPO_LAUNCHER launch_combine_selected(const AttnParams& p, int batch, int D, hipStream_t stream);
 TEMPO_LAUNCHER launch_block_bounds(const StoreParams& p, void* bounds, int D, int dtype, hipStream_t stream);
-TEMPO_LAUNCHER launch_select_blocks(const ChooseParams& p, int batch, int D, hipStream_t stream);
+TEMPO_LAUNCHER launch_select_blocks(const ChooseParams& p, const StoreParams* store, const void* k_new, const void* v_new, int batch, int D,
+                                    int dtype, hipStream_t stream);
 #undef TEMPO_LAUNCHER
 
 }  // namespace tempo

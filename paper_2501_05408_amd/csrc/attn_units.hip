@@ -121,6 +121,7 @@ __device__ __forceinline__ u32x4 fetch_new_rows(const AttnParams& p, int b, int 
   return *reinterpret_cast<const u32x4*>(src);
 }
 
+// slot: the number of the group's first slot among the store's `slots`.
 template <int D, bool kRope>
 __device__ __forceinline__ void write_new_rows(const AttnParams& p, u32x4 x, int t_b, int64_t slot, int64_t slots, bool store, int lane, uint8_t* stage) {
   constexpr int LANES = D / 8;
@@ -133,37 +134,13 @@ __device__ __forceinline__ void write_new_rows(const AttnParams& p, u32x4 x, int
     rotate_pieces(p.rope_cos, p.rope_sin, t_b, D / 2, d % (D / 2), lo, hi);
     if (lane < LANES) x = d < D / 2 ? lo : hi;
   }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = top_of(x[i], top);
-#pragma unroll
-  for (int m = LANES / 2; m > 0; m >>= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)top, m);
-    top = o > top ? o : top;
-  }
-  const uint32_t E = (uint32_t)scale_byte(top);
-  const float inverse = inverse_scale_of(E), most = largest_code(E);
-  const uint32_t lo = codes_of(x.x, inverse, most) | (codes_of(x.y, inverse, most) << 16);
-  const uint32_t hi = codes_of(x.z, inverse, most) | (codes_of(x.w, inverse, most) << 16);
+  const RowPiece r = quantise_piece<D>(x);
   if (lane >= 2 * LANES) return;
   const bool value = lane >= LANES;
-  const int part = lane % LANES, u = t_b & 31;
-  *reinterpret_cast<uint2*>(stage + lane * 8) = uint2{lo, hi};
-  if (part == 0) stage[2 * D + value] = (uint8_t)E;
-  if (!store) return;
-  // slot: of the group's first step, in the numbering of all slots
-  uint8_t* const pool = static_cast<uint8_t*>(value ? p.v_pool : p.k_pool);
-  if (!value) {
-    *reinterpret_cast<uint2*>(pool + slot * D + tile_off_k_e4m3(D, u, 8 * part)) = uint2{lo, hi};
-  } else {
-    uint8_t* const to = pool + slot * D + tile_off_v_e4m3(D, u, 8 * part);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      to[16 * i] = (uint8_t)(lo >> (8 * i));
-      to[16 * (4 + i)] = (uint8_t)(hi >> (8 * i));
-    }
-  }
-  if (part == 0) pool[slots * D + slot + (value ? scale_off_v(u) : scale_off_k(u))] = (uint8_t)E;
+  const int part = lane % LANES;
+  *reinterpret_cast<uint2*>(stage + lane * 8) = uint2{r.lo, r.hi};
+  if (part == 0) stage[2 * D + value] = (uint8_t)r.scale;
+  if (store) store_piece<D>(static_cast<uint8_t*>(value ? p.v_pool : p.k_pool), slots, slot, t_b & 31, value, part, r);
 }
 
 template <int D>

@@ -28,7 +28,7 @@ __device__ inline int64_t tile_slot(const StoreParams& p, int b, int head, int t
 __device__ inline int64_t all_slots(const StoreParams& p) { return ((int64_t)p.num_blocks * p.Hkv) << p.z_log2; }
 
 // Row by row: D/8 lanes take a row of 8 values each, keys and values of a (sequence, step, head) side by side, so a
-// wavefront writes 64 / (D/4) pairs of rows.  Codes of a key row are 8-byte pieces, of a value row single bytes.
+// wavefront writes 64 / (D/4) pairs of rows.
 template <int D>
 __global__ __launch_bounds__(256) void kv_append_e4m3(StoreParams p, const uint16_t* __restrict__ k_new,
                                                       const uint16_t* __restrict__ v_new) {
@@ -50,35 +50,10 @@ __global__ __launch_bounds__(256) void kv_append_e4m3(StoreParams p, const uint1
     if (d < D / 2) rotate_pieces(p.rope_cos, p.rope_sin, t, D / 2, d, x, other);
     else rotate_pieces(p.rope_cos, p.rope_sin, t, D / 2, other_d, other, x);
   }
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) top = top_of(x[i], top);
-#pragma unroll
-  for (int m = LANES / 2; m > 0; m >>= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)top, m);
-    top = o > top ? o : top;
-  }
+  const RowPiece r = quantise_piece<D>(x);
   if (!live || c >= rows_of(p, b)) return;
-  const uint32_t E = (uint32_t)scale_byte(top);
-  const float inverse = inverse_scale_of(E), most = largest_code(E);
-  const uint32_t lo = codes_of(x.x, inverse, most) | (codes_of(x.y, inverse, most) << 16);
-  const uint32_t hi = codes_of(x.z, inverse, most) | (codes_of(x.w, inverse, most) << 16);
-  const int slot = t & ((1 << p.z_log2) - 1);
-  const int64_t first = tile_slot(p, b, head, t), scales = all_slots(p) * D + first;
-  if (!value) {
-    uint8_t* const pool = static_cast<uint8_t*>(p.k_pool);
-    *reinterpret_cast<uint2*>(pool + first * D + tile_off_k_e4m3(D, slot, d)) = uint2{lo, hi};
-    if (part == 0) pool[scales + scale_off_k(slot)] = (uint8_t)E;
-  } else {
-    uint8_t* const pool = static_cast<uint8_t*>(p.v_pool);
-    uint8_t* const to = pool + first * D + tile_off_v_e4m3(D, slot, d);  // dims d .. d+7 lie 16 bytes apart
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      to[16 * i] = (uint8_t)(lo >> (8 * i));
-      to[16 * (4 + i)] = (uint8_t)(hi >> (8 * i));
-    }
-    if (part == 0) pool[scales + scale_off_v(slot)] = (uint8_t)E;
-  }
+  uint8_t* const pool = static_cast<uint8_t*>(value ? p.v_pool : p.k_pool);
+  store_piece<D>(pool, all_slots(p), tile_slot(p, b, head, t), t & ((1 << p.z_log2) - 1), value, part, r);
 }
 
 // Two codes of a word (its low or high half) as bf16 values.

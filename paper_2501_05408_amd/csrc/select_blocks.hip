@@ -27,52 +27,49 @@ __device__ inline int step_of(const int32_t* t_per_seq, int t, int b) {
 __device__ inline float min_nan(float m, float x) { return x < m || x != x ? x : m; }
 __device__ inline float max_nan(float m, float x) { return x > m || x != x ? x : m; }
 
-// One workgroup per (block of a sequence, kv head); wavefront w reads the 1 KiB units of its part of the dims: in a bf16
-// store 8 dims a lane (unit s = w of each row-tile), in an 8-bit store 16.  Lane (row + 16c) goes through the rows
-// row, 16 + row, ... of the block, then the 16 lanes of equal c are reduced.
+// Bounds of the block of one kv head whose first slot has number `first` among the store's; wavefronts w < D/64 (8-bit store)
+// or D/32 (bf16) read the 1 KiB units of their part of the dims, 16 or 8 of them a lane.  Lane (row + 16c) goes through the
+// rows row, 16 + row, ... of the block, then the 16 lanes of equal c are reduced.
 template <int D, bool k8>
-__global__ __launch_bounds__(k8 ? D : 2 * D) void block_bounds(StoreParams p, uint16_t* __restrict__ bounds) {
+__device__ __forceinline__ void bounds_of_block(const StoreParams& p, int64_t first, int w, int lane, uint16_t* __restrict__ to) {
   constexpr int PER_TILE = k8 ? D / 64 : D / 32;  // units of a row-tile
   constexpr int N = k8 ? 16 : 8;                  // dims a lane holds
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int head = blockIdx.y, b = blockIdx.z;
-  const int t_b = step_of(p.t_per_seq, p.t, b);
-  int rows = p.count;
-  if (p.count_per_seq) rows = p.count_per_seq[b] < rows ? p.count_per_seq[b] : rows;
-  const int n = (t_b >> p.z_log2) + (int)blockIdx.x;           // block of the sequence
-  const int64_t last = (((int64_t)n + 1) << p.z_log2) - 1;     // its last step
-  if (last < t_b || last > (int64_t)t_b + rows - 1) return;    // not completed by the call's steps; uniform
-  const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + (n & p.tile_mask)], p.num_blocks);
-  const int64_t pair = (int64_t)phys * p.Hkv + head, first = pair << p.z_log2;
   const char* const at = static_cast<const char*>(p.k_pool) + first * (k8 ? D : 2 * D) + w * 1024 + lane * 16;
-  const uint8_t* const scales = static_cast<const uint8_t*>(p.k_pool) + ((((int64_t)p.num_blocks * p.Hkv) << p.z_log2) * D + first);
+  const uint8_t* const scales = static_cast<const uint8_t*>(p.k_pool) + ((((int64_t)p.num_blocks * p.Hkv) << p.z_log2) * D + first) + 2 * (lane & 15);
   float lo[N], hi[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     lo[i] = INFINITY;
     hi[i] = -INFINITY;
   }
-  const int tiles = 1 << (p.z_log2 - 4);
-#pragma unroll 4
-  for (int t = 0; t < tiles; ++t) {
-    const u32x4 u = *reinterpret_cast<const u32x4*>(at + (int64_t)t * PER_TILE * 1024);
-    float x[N];
-    if constexpr (k8) {
-      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-      const float scale = scale_of(scales[scale_off_k(16 * t + (lane & 15))]);
+  const int groups = 1 << (p.z_log2 - 5);
+#pragma unroll 2
+  for (int t = 0; t < groups; ++t) {
+    u32x4 u[2];
+    uint32_t both = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, false);
-        const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[i], scale, true);
-        x[4 * i] = (float)a[0]; x[4 * i + 1] = (float)a[1]; x[4 * i + 2] = (float)c[0]; x[4 * i + 3] = (float)c[1];
+    for (int r = 0; r < 2; ++r) u[r] = *reinterpret_cast<const u32x4*>(at + (int64_t)(2 * t + r) * PER_TILE * 1024);
+    if constexpr (k8) both = *reinterpret_cast<const uint16_t*>(scales + 32 * t);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float x[N];
+      if constexpr (k8) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const float scale = scale_of(r == 0 ? both & 0xFFu : both >> 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[r][i], scale, false);
+          const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[r][i], scale, true);
+          x[4 * i] = (float)a[0]; x[4 * i + 1] = (float)a[1]; x[4 * i + 2] = (float)c[0]; x[4 * i + 3] = (float)c[1];
+        }
+      } else {
+        unpack8(u[r], x);
       }
-    } else {
-      unpack8(u, x);
-    }
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      lo[i] = min_nan(lo[i], x[i]);
-      hi[i] = max_nan(hi[i], x[i]);
+      for (int i = 0; i < N; ++i) {
+        lo[i] = min_nan(lo[i], x[i]);
+        hi[i] = max_nan(hi[i], x[i]);
+      }
     }
   }
 #pragma unroll
@@ -85,13 +82,59 @@ __global__ __launch_bounds__(k8 ? D : 2 * D) void block_bounds(StoreParams p, ui
   }
   if ((lane & 15) != 0) return;
   const int c = lane >> 4;
-  uint16_t* const to = bounds + pair * 2 * D;
 #pragma unroll
   for (int h = 0; h < N / 8; ++h) {
     const int d = k8 ? 64 * w + 32 * h + 8 * c : 32 * w + 8 * c;
     *reinterpret_cast<u32x4*>(to + d) = pack8(lo + 8 * h);
     *reinterpret_cast<u32x4*>(to + D + d) = pack8(hi + 8 * h);
   }
+}
+
+// One workgroup per (block of a sequence, kv head).
+template <int D, bool k8>
+__global__ __launch_bounds__(k8 ? D : 2 * D) void block_bounds(StoreParams p, uint16_t* __restrict__ bounds) {
+  const int head = blockIdx.y, b = blockIdx.z;
+  const int t_b = step_of(p.t_per_seq, p.t, b);
+  int rows = p.count;
+  if (p.count_per_seq) rows = p.count_per_seq[b] < rows ? p.count_per_seq[b] : rows;
+  const int n = (t_b >> p.z_log2) + (int)blockIdx.x;         // block of the sequence
+  const int64_t last = (((int64_t)n + 1) << p.z_log2) - 1;   // its last step
+  if (last < t_b || last > (int64_t)t_b + rows - 1) return;  // not completed by the call's steps; uniform
+  const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
+  const int64_t pair = (int64_t)phys * p.Hkv + head;
+  bounds_of_block<D, k8>(p, pair << p.z_log2, threadIdx.x >> 6, threadIdx.x & 63, bounds + pair * 2 * D);
+}
+
+// A step's row of one (sequence, kv head) into the store, by one wavefront, and the bounds of its block if the step is the
+// block's last.  All wavefronts of the workgroup call this.
+template <int D, bool k8>
+__device__ __forceinline__ void write_and_bound(const StoreParams& p, const void* k_new, const void* v_new, uint16_t* bounds, int b, int head) {
+  constexpr int LANES = D / 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int t = step_of(p.t_per_seq, p.t, b), n = t >> p.z_log2, slot = t & ((1 << p.z_log2) - 1);
+  const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
+  const int64_t pair = (int64_t)phys * p.Hkv + head, first = pair << p.z_log2, slots = ((int64_t)p.num_blocks * p.Hkv) << p.z_log2;
+  if (wave == 0) {
+    const int at = lane % (2 * LANES), part = at % LANES;  // keys, then values; the lanes beyond hold copies
+    const bool value = at >= LANES;
+    const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(value ? v_new : k_new) + ((int64_t)b * p.Hkv + head) * D + 8 * part);
+    if constexpr (k8) {
+      const RowPiece r = quantise_piece<D>(x);
+      if (lane < 2 * LANES) store_piece<D>(static_cast<uint8_t*>(value ? p.v_pool : p.k_pool), slots, first, slot, value, part, r);
+    } else if (lane < LANES) {
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.k_pool) + first * D + tile_off_k_bf16(D, slot, 8 * part)) = x;
+    } else if (lane < 2 * LANES) {
+      uint16_t* const to = static_cast<uint16_t*>(p.v_pool) + first * D + tile_off_v_bf16(D, slot, 8 * part);  // (dims lie 8 elements apart)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        to[16 * i] = (uint16_t)x[i];
+        to[16 * i + 8] = (uint16_t)(x[i] >> 16);
+      }
+    }
+  }
+  if (slot != (1 << p.z_log2) - 1) return;  // uniform
+  __syncthreads();                          // the row is read back with the block's others
+  if (wave < (k8 ? D / 64 : D / 32)) bounds_of_block<D, k8>(p, first, wave, lane, bounds + pair * 2 * D);
 }
 
 // Bits of a score in an order that whole numbers share; NaN above all.
@@ -102,13 +145,23 @@ __device__ inline uint64_t key_of(double s) {
 }
 
 // A wavefront scores 16 blocks: lane (row + 16c) holds dims 32s + 8c .. +7 of block `row`.
-template <int D>
-__global__ __launch_bounds__(256) void score_blocks(ChooseParams p) {
+// kStore: of a whole step, whose row is written, and its block's bounds if it completes it, by the first workgroup of
+// every (sequence, kv head): no score reads either, as the newest block is chosen anyway (0: neither; 1: bf16 store; 2: 8-bit).
+template <int D, int kStore>
+__global__ __launch_bounds__(256) void score_blocks(ChooseParams p, StoreParams store, const void* __restrict__ k_new, const void* __restrict__ v_new) {
   constexpr int KS = D / 32;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, c = lane >> 4;
   const int hkv = blockIdx.y, b = blockIdx.z;
+  int part = blockIdx.x;
+  if constexpr (kStore != 0) {
+    if (part == 0) {
+      write_and_bound<D, kStore == 2>(store, k_new, v_new, static_cast<uint16_t*>(p.bounds), b, hkv);
+      return;
+    }
+    --part;
+  }
   const int newest = step_of(p.t_per_seq, p.t, b) >> p.z_log2;
-  const int n0 = ((int)blockIdx.x * 4 + wave) * 16;
+  const int n0 = (part * 4 + wave) * 16;
   if (newest < p.pick || n0 > newest - p.last) return;  // all blocks are taken; or only blocks that are taken anyway
   const int n = n0 + row <= newest - p.last ? n0 + row : n0;
   const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
@@ -120,22 +173,36 @@ __global__ __launch_bounds__(256) void score_blocks(ChooseParams p) {
     hi[s] = *reinterpret_cast<const u32x4*>(at + D + 32 * s);
   }
   const uint16_t* const q = static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D + 8 * c;
+  u32x4 u[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) u[s] = *reinterpret_cast<const u32x4*>(q + 32 * s);
+  float l[8 * KS], h[8 * KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    unpack8(lo[s], l + 8 * s);
+    unpack8(hi[s], h + 8 * s);
+  }
   uint64_t best = 0;
   for (int g = 0; g < p.G; ++g) {
-    double sum = 0.0;
+    u32x4 now[KS];
+    const int ahead = g + 1 < p.G ? g + 1 : g;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const u32x4 u = *reinterpret_cast<const u32x4*>(q + g * D + 32 * s);
-      float x[8], l[8], h[8];
-      unpack8(u, x);
-      unpack8(lo[s], l);
-      unpack8(hi[s], h);
+      now[s] = u[s];
+      u[s] = *reinterpret_cast<const u32x4*>(q + (int64_t)ahead * D + 32 * s);
+    }
+    double sums[2] = {0.0, 0.0};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      float x[8];
+      unpack8(now[s], x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float a = x[e] * l[e], z = x[e] * h[e];  // exact
-        sum += (double)max_nan(a, z);
+        const float m = x[e] < 0.f ? l[8 * s + e] : h[8 * s + e];  // the larger product's
+        sums[e & 1] = fma((double)x[e], (double)m, sums[e & 1]);   // (NaN where a bound is)
       }
     }
+    double sum = sums[0] + sums[1];
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     const uint64_t key = key_of(sum);
@@ -144,14 +211,48 @@ __global__ __launch_bounds__(256) void score_blocks(ChooseParams p) {
   if (c == 0 && n0 + row <= newest - p.last) p.scores[((int64_t)b * p.Hkv + hkv) * p.tiles + n0 + row] = best;
 }
 
-// One workgroup per (sequence, kv head).  The m-th largest key of the candidates by its bytes from the top down: a
-// histogram of the next byte over the keys that share the bytes found so far.  Then the blocks in ascending order.
-constexpr int kChoose = 256;
+// ---- choice ---------------------------------------------------------------------------------
+// One workgroup per (sequence, kv head).  The border, the m-th largest key of the candidates: keys are counted in 512 equal
+// parts of their range, then of the part that the border lies in, until at most 64 keys are left, which are ranked one by
+// one, or the part holds a single value.  Then the chosen blocks in ascending order.  (Counting by the keys' bytes from the
+// top down, 256 parts at a time, takes three or four rounds, as scores of one sign share their first byte.)
+constexpr int kChoose = 512, kWaves = kChoose / 64, kParts = 512, kRanked = 64;
+constexpr int kCached = 4096;  // keys held in LDS; more are read again from memory
+
+__device__ inline uint64_t shfl_xor_u64(uint64_t v, int m) {
+  const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, m), hi = (uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), m);
+  return (uint64_t)hi << 32 | lo;
+}
+
+// Sum of `v` over the threads before this one; `total`: over all.  (at: kWaves integers; two barriers apart from other uses.)
+__device__ inline int sum_before(int v, int* at, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int sum = v;
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int o = __shfl_up(sum, m);
+    sum += lane >= m ? o : 0;
+  }
+  if (lane == 63) at[wave] = sum;
+  __syncthreads();
+  int before = sum - v;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    before += w < wave ? at[w] : 0;
+    total += at[w];
+  }
+  return before;
+}
 
 __global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
-  __shared__ int bins[256];
-  __shared__ int at_wave[2][kChoose / 64];
-  __shared__ int found[3];  // next byte; keys above it; keys that have it
+  __shared__ uint64_t cache[kCached];
+  __shared__ int bins[kParts];
+  __shared__ uint64_t ends[2][kWaves];
+  __shared__ uint64_t ranked_key[kRanked];
+  __shared__ int ranked_at[kRanked];
+  __shared__ int sums[2][kWaves], found[3], left, border_at;
+  __shared__ uint64_t border;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.y;
   const int newest = step_of(p.t_per_seq, p.t, b) >> p.z_log2;
@@ -164,31 +265,64 @@ __global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
   }
   const int lo = p.first, hi = newest - p.last;  // candidates
   int wanted = p.pick - p.first - p.last;        // of them; fewer than there are
-  uint64_t prefix = 0, mask = 0;
+  const bool cached = hi - lo < kCached;
+  auto key_at = [&](int n) { return cached ? cache[n - lo] : scores[n]; };
+  // Chosen are the candidates with keys above cut, and of those with keys equal to it the ones up to cut_at.
+  uint64_t cut = ~(uint64_t)0;
+  int cut_at = -1;
   if (wanted > 0) {
-    for (int shift = 56; shift >= 0; shift -= 8) {
+    uint64_t least = ~(uint64_t)0, most = 0;
+    for (int n = lo + tid; n <= hi; n += kChoose) {
+      const uint64_t key = scores[n];
+      if (cached) cache[n - lo] = key;
+      least = key < least ? key : least;
+      most = key > most ? key : most;
+    }
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) {
+      const uint64_t a = shfl_xor_u64(least, m), z = shfl_xor_u64(most, m);
+      least = a < least ? a : least;
+      most = z > most ? z : most;
+    }
+    if (lane == 0) {
+      ends[0][wave] = least;
+      ends[1][wave] = most;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      least = ends[0][w] < least ? ends[0][w] : least;
+      most = ends[1][w] > most ? ends[1][w] : most;
+    }
+    int count = hi - lo + 1;  // candidates in least .. most
+    while (count > kRanked && least != most && count != wanted) {
+      const int bits = 64 - __clzll((long long)(most - least));
+      const int shift = bits > 9 ? bits - 9 : 0;
       bins[tid] = 0;
       __syncthreads();
       for (int n = lo + tid; n <= hi; n += kChoose) {
-        const uint64_t key = scores[n];
-        if ((key & mask) == prefix) atomicAdd(&bins[(key >> shift) & 255u], 1);
+        const uint64_t key = key_at(n);
+        if (key >= least && key <= most) atomicAdd(&bins[(key - least) >> shift], 1);
       }
       __syncthreads();
-      if (wave == 0) {  // lane i: bins 4i .. 4i+3; how many keys lie in higher bins than those
-        int own[4], sum = 0;
-        for (int k = 0; k < 4; ++k) {
-          own[k] = bins[4 * lane + k];
+      if (wave == 0) {  // lane i: parts 8i .. 8i+7, and how many keys lie above those
+        int own[8], sum = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          own[k] = bins[8 * lane + k];
           sum += own[k];
         }
         int above = sum;
+#pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
           const int o = __shfl_down(above, m);
           above += lane + m < 64 ? o : 0;
         }
         above -= sum;
-        for (int k = 3; k >= 0; --k) {
+#pragma unroll
+        for (int k = 7; k >= 0; --k) {
           if (above < wanted && above + own[k] >= wanted) {
-            found[0] = 4 * lane + k;
+            found[0] = 8 * lane + k;
             found[1] = above;
             found[2] = own[k];
           }
@@ -196,41 +330,67 @@ __global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
         }
       }
       __syncthreads();
-      prefix |= (uint64_t)found[0] << shift;
-      mask |= (uint64_t)255 << shift;
+      least += (uint64_t)found[0] << shift;
+      const uint64_t width = ((uint64_t)1 << shift) - 1;
+      most = most - least > width ? least + width : most;
       wanted -= found[1];
-      const bool all = found[2] == wanted;  // every key that begins so is taken
-      __syncthreads();                      // bins and found are written again
-      if (all) break;
+      count = found[2];
+      __syncthreads();  // found and bins are written again
+    }
+    if (count == wanted) {  // all that are left
+      cut = least;
+      cut_at = INT32_MAX;
+    } else if (least == most) {  // one value: the first `wanted` blocks that have it
+      cut = least;
+      const int each = (hi - lo + kChoose) / kChoose, n0 = lo + tid * each;
+      int mine = 0, all;
+      for (int n = n0; n < n0 + each && n <= hi; ++n) mine += key_at(n) == least;
+      int before = sum_before(mine, sums[0], all);
+      for (int n = n0; n < n0 + each && n <= hi; ++n) {
+        if (key_at(n) == least && ++before == wanted) border_at = n;
+      }
+      __syncthreads();
+      cut_at = border_at;
+    } else {  // few: the one that wanted - 1 of them come before
+      if (tid == 0) left = 0;
+      __syncthreads();
+      for (int n = lo + tid; n <= hi; n += kChoose) {
+        const uint64_t key = key_at(n);
+        if (key >= least && key <= most) {
+          const int i = atomicAdd(&left, 1);  // (in any order: ranks do not depend on it)
+          ranked_key[i] = key;
+          ranked_at[i] = n;
+        }
+      }
+      __syncthreads();
+      if (tid < count) {
+        const uint64_t key = ranked_key[tid];
+        const int n = ranked_at[tid];
+        int rank = 0;
+        for (int i = 0; i < count; ++i) rank += ranked_key[i] > key || (ranked_key[i] == key && ranked_at[i] < n);
+        if (rank == wanted - 1) {
+          border = key;
+          border_at = n;
+        }
+      }
+      __syncthreads();
+      cut = border;
+      cut_at = border_at;
     }
   }
-  // Keys whose top bytes exceed `prefix` are taken, of those that share them the first `wanted`.
-  int taken = 0, equal = 0;
-  for (int n0 = 0; n0 <= newest; n0 += kChoose) {
-    const int n = n0 + tid;
-    const bool candidate = n >= lo && n <= hi && p.pick > p.first + p.last;
-    const uint64_t key = candidate ? scores[n] & mask : 0;
-    const bool tie = candidate && key == prefix;
-    const uint64_t ties = __ballot(tie);
-    if (lane == 0) at_wave[0][wave] = __popcll(ties);
-    __syncthreads();
-    int before = equal;
-    for (int w = 0; w < wave; ++w) before += at_wave[0][w];
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    before += __popcll(ties & below);
-    const bool take = n <= newest && (n < lo || n > hi || (candidate && key > prefix) || (tie && before < wanted));
-    const uint64_t takes = __ballot(take);
-    if (lane == 0) at_wave[1][wave] = __popcll(takes);
-    __syncthreads();
-    int place = taken;
-    for (int w = 0; w < wave; ++w) place += at_wave[1][w];
-    place += __popcll(takes & below);
-    if (take && place < p.pick) out[place] = n;
-    for (int w = 0; w < kChoose / 64; ++w) {
-      equal += at_wave[0][w];
-      taken += at_wave[1][w];
-    }
-    __syncthreads();
+  // In ascending order: every thread the blocks of one run.
+  const int each = (newest + kChoose) / kChoose, n0 = tid * each;
+  auto chosen = [&](int n) {
+    if (n > newest) return false;
+    if (n < lo || n > hi) return true;
+    const uint64_t key = key_at(n);
+    return key > cut || (key == cut && n <= cut_at);
+  };
+  int mine = 0, all;
+  for (int n = n0; n < n0 + each; ++n) mine += chosen(n);
+  int place = sum_before(mine, sums[1], all);
+  for (int n = n0; n < n0 + each; ++n) {
+    if (chosen(n) && place < p.pick) out[place++] = n;
   }
 }
 
@@ -250,13 +410,24 @@ hipError_t launch_block_bounds(const StoreParams& p, void* bounds, int D, int dt
   return launch((block_bounds<64, false>), grid, dim3(128), 0, stream, p, to);
 }
 
-hipError_t launch_select_blocks(const ChooseParams& p, int batch, int D, hipStream_t stream) {
+// k_new, v_new: null, or the rows of the step, which are written (and bounded) by the same launch.
+template <int D, int kStore>
+static hipError_t launch_score(const ChooseParams& p, const StoreParams& store, const void* k_new, const void* v_new, int batch, hipStream_t stream) {
   // (no sequence has more blocks than are taken: nothing to score)
-  if (p.tiles > p.pick && p.pick > p.first + p.last) {
-    const dim3 grid((unsigned)((p.tiles + 63) / 64), (unsigned)p.Hkv, (unsigned)batch);
-    const hipError_t e = D == 128 ? launch(score_blocks<128>, grid, dim3(256), 0, stream, p) : launch(score_blocks<64>, grid, dim3(256), 0, stream, p);
-    if (e != hipSuccess) return e;
-  }
+  const int parts = p.tiles > p.pick && p.pick > p.first + p.last ? (p.tiles + 63) / 64 : 0;
+  const int workgroups = parts + (kStore != 0 ? 1 : 0);
+  if (workgroups == 0) return hipSuccess;
+  return launch((score_blocks<D, kStore>), dim3((unsigned)workgroups, (unsigned)p.Hkv, (unsigned)batch), dim3(256), 0, stream, p, store, k_new, v_new);
+}
+
+hipError_t launch_select_blocks(const ChooseParams& p, const StoreParams* store, const void* k_new, const void* v_new, int batch, int D, int dtype,
+                                hipStream_t stream) {
+  const StoreParams none = {};
+  hipError_t e;
+  if (!store) e = D == 128 ? launch_score<128, 0>(p, none, nullptr, nullptr, batch, stream) : launch_score<64, 0>(p, none, nullptr, nullptr, batch, stream);
+  else if (dtype == TEMPO_E4M3) e = D == 128 ? launch_score<128, 2>(p, *store, k_new, v_new, batch, stream) : launch_score<64, 2>(p, *store, k_new, v_new, batch, stream);
+  else e = D == 128 ? launch_score<128, 1>(p, *store, k_new, v_new, batch, stream) : launch_score<64, 1>(p, *store, k_new, v_new, batch, stream);
+  if (e != hipSuccess) return e;
   return launch(choose_blocks, dim3((unsigned)p.Hkv, (unsigned)batch), dim3(kChoose), 0, stream, p);
 }
 

@@ -12,7 +12,7 @@
 // their relative step, and would add a rounding to every value read.
 #pragma once
 
-#include "tempo_internal.h"
+#include "attn_bf16_common.h"
 
 namespace tempo {
 
@@ -43,6 +43,45 @@ __device__ inline uint32_t top_of(uint32_t pair, uint32_t top) {
   const uint32_t a = lo < 0x7F80u ? lo : 0u, b = hi < 0x7F80u ? hi : 0u;
   const uint32_t m = a > b ? a : b;
   return m > top ? m : top;
+}
+
+// 8 consecutive values of a row that D/8 lanes hold side by side: their codes (two words) and the row's scale byte.
+struct RowPiece {
+  uint32_t lo, hi, scale;
+};
+template <int D>
+__device__ inline RowPiece quantise_piece(u32x4 x) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top = top_of(x[i], top);
+#pragma unroll
+  for (int m = D / 16; m > 0; m >>= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)top, m);
+    top = o > top ? o : top;
+  }
+  RowPiece r;
+  r.scale = (uint32_t)scale_byte(top);
+  const float inverse = inverse_scale_of(r.scale), most = largest_code(r.scale);
+  r.lo = codes_of(x.x, inverse, most) | (codes_of(x.y, inverse, most) << 16);
+  r.hi = codes_of(x.z, inverse, most) | (codes_of(x.w, inverse, most) << 16);
+  return r;
+}
+
+// Piece `part` of a row into a pool: `slot` of the tile (or of any run of whole groups of it) whose first slot has number
+// `first` among the store's `slots`.  Codes of a key row are 8-byte pieces, of a value row single bytes.
+template <int D>
+__device__ inline void store_piece(uint8_t* pool, int64_t slots, int64_t first, int slot, bool value, int part, const RowPiece& r) {
+  if (!value) {
+    *reinterpret_cast<uint2*>(pool + first * D + tile_off_k_e4m3(D, slot, 8 * part)) = uint2{r.lo, r.hi};
+  } else {
+    uint8_t* const to = pool + first * D + tile_off_v_e4m3(D, slot, 8 * part);  // dims 8 part .. +7 lie 16 bytes apart
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      to[16 * i] = (uint8_t)(r.lo >> (8 * i));
+      to[16 * (4 + i)] = (uint8_t)(r.hi >> (8 * i));
+    }
+  }
+  if (part == 0) pool[slots * D + first + (value ? scale_off_v(slot) : scale_off_k(slot))] = (uint8_t)r.scale;
 }
 
 }  // namespace tempo

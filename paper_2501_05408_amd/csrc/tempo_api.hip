@@ -1648,6 +1648,32 @@ size_t tempo_select_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t n
   return align_up((size_t)batch * kv->num_kv_heads * (max_t / kv->block_size + 1) * sizeof(uint64_t), 256);
 }
 
+// Scores and choice; k_new, v_new set: a whole step's, whose row is written and whose block is bounded by the first launch.
+static int select_blocks(const tempo_kv* kv, void* bounds, const void* q, int32_t* selected, int32_t count, int32_t first,
+                         int32_t last, int32_t batch, int32_t Hq, int32_t t, const int32_t* t_per_seq, const void* k_new,
+                         const void* v_new, void* workspace, hipStream_t stream) {
+  ChooseParams p;
+  p.bounds = bounds;
+  p.q = q;
+  p.block_table = kv->block_table;
+  p.t_per_seq = t_per_seq;
+  p.scores = static_cast<uint64_t*>(workspace);
+  p.selected = selected;
+  p.t = t;
+  p.z_log2 = ilog2_exact(kv->block_size);
+  p.max_blocks_per_seq = kv->max_blocks_per_seq;
+  p.num_blocks = kv->num_blocks;
+  p.Hkv = kv->num_kv_heads;
+  p.Hq = Hq;
+  p.G = Hq / kv->num_kv_heads;
+  p.tiles = t / kv->block_size + 1;
+  p.pick = count;
+  p.first = first;
+  p.last = last;
+  const StoreParams store = store_params(kv, batch, t, t_per_seq);
+  return launch_status(launch_select_blocks(p, k_new ? &store : nullptr, k_new, v_new, batch, kv->head_dim, kv->dtype, stream), "select_blocks");
+}
+
 int tempo_select_blocks(const tempo_kv* kv, const void* bounds, const void* q, int32_t* selected, int32_t count,
                         int32_t first, int32_t last, int32_t batch, int32_t num_q_heads, int32_t t,
                         const int32_t* t_per_seq, void* workspace, size_t workspace_bytes, void* stream) {
@@ -1661,25 +1687,8 @@ int tempo_select_blocks(const tempo_kv* kv, const void* bounds, const void* q, i
   if ((rc = check_step(kv, t)) != TEMPO_OK) return rc;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
   if (workspace_bytes < tempo_select_workspace_bytes(kv, batch, num_q_heads, t)) return TEMPO_ERR_WORKSPACE;
-  ChooseParams p;
-  p.bounds = bounds;
-  p.q = q;
-  p.block_table = kv->block_table;
-  p.t_per_seq = t_per_seq;
-  p.scores = static_cast<uint64_t*>(workspace);
-  p.selected = selected;
-  p.t = t;
-  p.z_log2 = ilog2_exact(kv->block_size);
-  p.max_blocks_per_seq = kv->max_blocks_per_seq;
-  p.num_blocks = kv->num_blocks;
-  p.Hkv = kv->num_kv_heads;
-  p.Hq = num_q_heads;
-  p.G = num_q_heads / kv->num_kv_heads;
-  p.tiles = t / kv->block_size + 1;
-  p.pick = count;
-  p.first = first;
-  p.last = last;
-  return launch_status(launch_select_blocks(p, batch, kv->head_dim, static_cast<hipStream_t>(stream)), "select_blocks");
+  return select_blocks(kv, const_cast<void*>(bounds), q, selected, count, first, last, batch, num_q_heads, t, t_per_seq, nullptr,
+                       nullptr, workspace, static_cast<hipStream_t>(stream));
 }
 
 // The list's places, block_size for each entry, are cut into splits as the keys of a step of so many would be.
@@ -1736,7 +1745,7 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
                                void* out, int32_t* selected, int32_t count, int32_t first, int32_t last, int32_t batch,
                                int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, float scale, void* workspace,
                                size_t workspace_bytes, void* stream) {
-  // everything the four calls below refuse, before the first of them launches anything
+  // everything that is refused, before the first launch
   int rc = check_sparse_store(kv, batch);
   if (rc != TEMPO_OK) return rc;
   if (!bounds || !q || !k_new || !v_new || !out || !selected || (rc = check_store(kv)) != TEMPO_OK) return TEMPO_ERR_NULL;
@@ -1751,10 +1760,8 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
   const size_t partials = tempo_attn_selected_workspace_bytes(kv, batch, num_q_heads, count);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
   if (workspace_bytes < scores + partials) return TEMPO_ERR_WORKSPACE;
-  if ((rc = tempo_kv_append(kv, k_new, v_new, batch, t, t_per_seq, stream)) != TEMPO_OK) return rc;
-  if ((rc = tempo_block_bounds(kv, bounds, batch, t, t_per_seq, 1, nullptr, stream)) != TEMPO_OK) return rc;
-  if ((rc = tempo_select_blocks(kv, bounds, q, selected, count, first, last, batch, num_q_heads, t, t_per_seq, workspace,
-                                scores, stream)) != TEMPO_OK)
+  if ((rc = select_blocks(kv, bounds, q, selected, count, first, last, batch, num_q_heads, t, t_per_seq, k_new, v_new, workspace,
+                          static_cast<hipStream_t>(stream))) != TEMPO_OK)
     return rc;
   return tempo_attn_selected(kv, q, out, selected, count, batch, num_q_heads, t, t_per_seq, scale,
                              static_cast<char*>(workspace) + scores, partials, stream);
