@@ -23,24 +23,46 @@ __device__ inline int step_of(const int32_t* t_per_seq, int t, int b) {
   return t_b < 0 ? 0 : t_b;
 }
 
-// Smaller / larger of two values; NaN if one is.
-__device__ inline float min_nan(float m, float x) { return x < m || x != x ? x : m; }
-__device__ inline float max_nan(float m, float x) { return x > m || x != x ? x : m; }
+// ---- bounds -----------------------------------------------------------------------------------
+// Values are compared as whole numbers, two to a word: a bf16 value's bits, with all but the sign turned over where it is
+// negative, are in the order of the values, NaN above infinity or below minus infinity by its sign.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+
+__device__ inline i16x2 ordered(uint32_t pair) {
+  const i16x2 v = __builtin_bit_cast(i16x2, pair);
+  return v ^ ((v >> 15) & i16x2{0x7FFF, 0x7FFF});
+}
+__device__ inline uint32_t values_in_order(i16x2 v) { return __builtin_bit_cast(uint32_t, v ^ ((v >> 15) & i16x2{0x7FFF, 0x7FFF})); }
+
+// Over the 16 lanes of a row of lanes.
+template <typename F>
+__device__ inline i16x2 reduce_row(i16x2 v, F f) {
+  v = f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0xB1, 0xF, 0xF, true)));
+  v = f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x4E, 0xF, 0xF, true)));
+  v = f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x141, 0xF, 0xF, true)));
+  return f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x140, 0xF, 0xF, true)));
+}
 
 // Bounds of the block of one kv head whose first slot has number `first` among the store's; wavefronts w < D/64 (8-bit store)
 // or D/32 (bf16) read the 1 KiB units of their part of the dims, 16 or 8 of them a lane.  Lane (row + 16c) goes through the
-// rows row, 16 + row, ... of the block, then the 16 lanes of equal c are reduced.
+// rows row, 16 + row, ... of the block, then the 16 lanes of equal c are reduced.  fresh: the block's last row is not in the
+// store yet; the lane's part of it is in `last` (8 bits: codes, with scale byte last_scale).
+// Bound by memory, as long as the comparisons are whole words' (8 x 4096 keys of 4 heads of 128 in blocks of 64, 34 MB:
+// 7.4 us; one value at a time in fp32 10.2).
 template <int D, bool k8>
-__device__ __forceinline__ void bounds_of_block(const StoreParams& p, int64_t first, int w, int lane, uint16_t* __restrict__ to) {
+__device__ __forceinline__ void bounds_of_block(const StoreParams& p, int64_t first, int w, int lane, uint16_t* __restrict__ to, bool fresh, u32x4 last,
+                                                uint32_t last_scale) {
   constexpr int PER_TILE = k8 ? D / 64 : D / 32;  // units of a row-tile
-  constexpr int N = k8 ? 16 : 8;                  // dims a lane holds
+  constexpr int N = k8 ? 8 : 4;                   // words of two values
   const char* const at = static_cast<const char*>(p.k_pool) + first * (k8 ? D : 2 * D) + w * 1024 + lane * 16;
   const uint8_t* const scales = static_cast<const uint8_t*>(p.k_pool) + ((((int64_t)p.num_blocks * p.Hkv) << p.z_log2) * D + first) + 2 * (lane & 15);
-  float lo[N], hi[N];
+  const auto less = [](i16x2 a, i16x2 z) { return __builtin_elementwise_min(a, z); };
+  const auto more = [](i16x2 a, i16x2 z) { return __builtin_elementwise_max(a, z); };
+  i16x2 lo[N], hi[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    lo[i] = INFINITY;
-    hi[i] = -INFINITY;
+    lo[i] = i16x2{0x7FFF, 0x7FFF};
+    hi[i] = i16x2{-0x8000, -0x8000};
   }
   const int groups = 1 << (p.z_log2 - 5);
 #pragma unroll 2
@@ -50,43 +72,48 @@ __device__ __forceinline__ void bounds_of_block(const StoreParams& p, int64_t fi
 #pragma unroll
     for (int r = 0; r < 2; ++r) u[r] = *reinterpret_cast<const u32x4*>(at + (int64_t)(2 * t + r) * PER_TILE * 1024);
     if constexpr (k8) both = *reinterpret_cast<const uint16_t*>(scales + 32 * t);
+    if (fresh && t == groups - 1 && (lane & 15) == 15) {
+      u[1] = last;
+      both = (both & 0xFFu) | (last_scale << 8);
+    }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-      float x[N];
+      i16x2 x[N];
       if constexpr (k8) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
         const float scale = scale_of(r == 0 ? both & 0xFFu : both >> 8);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[r][i], scale, false);
-          const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[r][i], scale, true);
-          x[4 * i] = (float)a[0]; x[4 * i + 1] = (float)a[1]; x[4 * i + 2] = (float)c[0]; x[4 * i + 3] = (float)c[1];
+          x[2 * i] = ordered(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[r][i], scale, false)));
+          x[2 * i + 1] = ordered(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[r][i], scale, true)));
         }
       } else {
-        unpack8(u[r], x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = ordered(u[r][i]);
       }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        lo[i] = min_nan(lo[i], x[i]);
-        hi[i] = max_nan(hi[i], x[i]);
+        lo[i] = less(lo[i], x[i]);
+        hi[i] = more(hi[i], x[i]);
       }
     }
   }
 #pragma unroll
-  for (int m = 8; m > 0; m >>= 1) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      lo[i] = min_nan(lo[i], __shfl_xor(lo[i], m));
-      hi[i] = max_nan(hi[i], __shfl_xor(hi[i], m));
-    }
+  for (int i = 0; i < N; ++i) {
+    lo[i] = reduce_row(lo[i], less);
+    hi[i] = reduce_row(hi[i], more);
+    const i16x2 nan = (hi[i] > (short)0x7F80) | (lo[i] < (short)~0x7F80);  // -1 where there is one, of either sign
+    lo[i] = (lo[i] & ~nan) | (nan & (short)0x7FC0);
+    hi[i] = (hi[i] & ~nan) | (nan & (short)0x7FC0);
   }
   if ((lane & 15) != 0) return;
   const int c = lane >> 4;
 #pragma unroll
-  for (int h = 0; h < N / 8; ++h) {
+  for (int h = 0; h < N / 4; ++h) {
     const int d = k8 ? 64 * w + 32 * h + 8 * c : 32 * w + 8 * c;
-    *reinterpret_cast<u32x4*>(to + d) = pack8(lo + 8 * h);
-    *reinterpret_cast<u32x4*>(to + D + d) = pack8(hi + 8 * h);
+    const u32x4 l = {values_in_order(lo[4 * h]), values_in_order(lo[4 * h + 1]), values_in_order(lo[4 * h + 2]), values_in_order(lo[4 * h + 3])};
+    const u32x4 m = {values_in_order(hi[4 * h]), values_in_order(hi[4 * h + 1]), values_in_order(hi[4 * h + 2]), values_in_order(hi[4 * h + 3])};
+    *reinterpret_cast<u32x4*>(to + d) = l;
+    *reinterpret_cast<u32x4*>(to + D + d) = m;
   }
 }
 
@@ -102,28 +129,33 @@ __global__ __launch_bounds__(k8 ? D : 2 * D) void block_bounds(StoreParams p, ui
   if (last < t_b || last > (int64_t)t_b + rows - 1) return;  // not completed by the call's steps; uniform
   const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
   const int64_t pair = (int64_t)phys * p.Hkv + head;
-  bounds_of_block<D, k8>(p, pair << p.z_log2, threadIdx.x >> 6, threadIdx.x & 63, bounds + pair * 2 * D);
+  bounds_of_block<D, k8>(p, pair << p.z_log2, threadIdx.x >> 6, threadIdx.x & 63, bounds + pair * 2 * D, false, u32x4{0u, 0u, 0u, 0u}, 0u);
 }
 
-// A step's row of one (sequence, kv head) into the store, by one wavefront, and the bounds of its block if the step is the
-// block's last.  All wavefronts of the workgroup call this.
+// A step's row of one (sequence, kv head) into the store, and the bounds of its block if the step is the block's last.  All
+// wavefronts of the workgroup call this; each has the whole key row, so that none waits for the write.
 template <int D, bool k8>
 __device__ __forceinline__ void write_and_bound(const StoreParams& p, const void* k_new, const void* v_new, uint16_t* bounds, int b, int head) {
   constexpr int LANES = D / 8;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 4;
   const int t = step_of(p.t_per_seq, p.t, b), n = t >> p.z_log2, slot = t & ((1 << p.z_log2) - 1);
   const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
   const int64_t pair = (int64_t)phys * p.Hkv + head, first = pair << p.z_log2, slots = ((int64_t)p.num_blocks * p.Hkv) << p.z_log2;
-  if (wave == 0) {
-    const int at = lane % (2 * LANES), part = at % LANES;  // keys, then values; the lanes beyond hold copies
-    const bool value = at >= LANES;
-    const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(value ? v_new : k_new) + ((int64_t)b * p.Hkv + head) * D + 8 * part);
-    if constexpr (k8) {
-      const RowPiece r = quantise_piece<D>(x);
-      if (lane < 2 * LANES) store_piece<D>(static_cast<uint8_t*>(value ? p.v_pool : p.k_pool), slots, first, slot, value, part, r);
-    } else if (lane < LANES) {
+  const int at = lane % (2 * LANES), part = at % LANES;  // lanes: key row, value row, copies of both
+  const bool value = at >= LANES;
+  const u32x4 x = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(value ? v_new : k_new) + ((int64_t)b * p.Hkv + head) * D + 8 * part);
+  u32x4 last;  // what lane (15 + 16c) of unit `wave` of the row's tile will hold of it
+  uint32_t last_scale = 0;
+  if constexpr (k8) {
+    const RowPiece r = quantise_piece<D>(x);
+    if (wave == 0 && lane < 2 * LANES) store_piece<D>(static_cast<uint8_t*>(value ? p.v_pool : p.k_pool), slots, first, slot, value, part, r);
+    const int from = (8 * wave + c) % LANES, other = (8 * wave + 4 + c) % LANES;
+    last = u32x4{(uint32_t)__shfl((int)r.lo, from), (uint32_t)__shfl((int)r.hi, from), (uint32_t)__shfl((int)r.lo, other), (uint32_t)__shfl((int)r.hi, other)};
+    last_scale = (uint32_t)__shfl((int)r.scale, 0);
+  } else {
+    if (wave == 0 && lane < LANES) {
       *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.k_pool) + first * D + tile_off_k_bf16(D, slot, 8 * part)) = x;
-    } else if (lane < 2 * LANES) {
+    } else if (wave == 0 && lane < 2 * LANES) {
       uint16_t* const to = static_cast<uint16_t*>(p.v_pool) + first * D + tile_off_v_bf16(D, slot, 8 * part);  // (dims lie 8 elements apart)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -131,10 +163,11 @@ __device__ __forceinline__ void write_and_bound(const StoreParams& p, const void
         to[16 * i + 8] = (uint16_t)(x[i] >> 16);
       }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) last[i] = (uint32_t)__shfl((int)x[i], (4 * wave + c) % LANES);
   }
   if (slot != (1 << p.z_log2) - 1) return;  // uniform
-  __syncthreads();                          // the row is read back with the block's others
-  if (wave < (k8 ? D / 64 : D / 32)) bounds_of_block<D, k8>(p, first, wave, lane, bounds + pair * 2 * D);
+  if (wave < (k8 ? D / 64 : D / 32)) bounds_of_block<D, k8>(p, first, wave, lane, bounds + pair * 2 * D, true, last, last_scale);
 }
 
 // Bits of a score in an order that whole numbers share; NaN above all.
