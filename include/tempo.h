@@ -484,10 +484,13 @@ int tempo_rope_attn_block_window(const tempo_kv* kv, const tempo_rope* rope, con
  *   count_per_seq device, int32 [batch], or NULL: sequence b has only count_per_seq[b]
  *                 (0 .. count) prompt steps; its later rows of q / k_new / v_new are not
  *                 read into the store, its later rows of out and its later slots in
- *                 the store are left as they are.  bf16 linear stores only
+ *                 the store are left as they are.  bf16 and e4m3 linear stores only
  *                 (TEMPO_ERR_SHAPE otherwise).
  *   workspace     device, 256-byte aligned, >= tempo_prefill_workspace_bytes(kv, batch,
  *                 num_q_heads, t + count - 1) bytes
+ * On an 8-bit store steps attend over the rows as the store holds them, quantised: the rows are written
+ * first; one block of 128 columns is answered over the codes, more over a bf16 copy of the keys/values
+ * they see, for which tempo_prefill_workspace_bytes has room (without it: TEMPO_ERR_WORKSPACE).
  * All arguments are validated for every block before the first launch.
  */
 int tempo_prefill_causal(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new,
@@ -503,7 +506,7 @@ int tempo_prefill_window(const tempo_kv* kv, const void* q, const void* k_new, c
 /* tempo_prefill_* with the rotary producer fused in: q_raw and k_raw arrive
  * unrotated; keys are turned to their step's position on the way into the store
  * (the same bits tempo_rope_kv_append stores), queries when the attention kernel loads
- * them.  bf16 linear stores only (TEMPO_ERR_SHAPE otherwise); rope->positions must
+ * them.  bf16 and e4m3 linear stores only (TEMPO_ERR_SHAPE otherwise); rope->positions must
  * exceed t + count - 1.  Other arguments as
  * tempo_prefill_causal / _window. */
 int tempo_rope_prefill_causal(const tempo_kv* kv, const tempo_rope* rope, const void* q_raw,
@@ -522,7 +525,7 @@ int tempo_rope_prefill_window(const tempo_kv* kv, const tempo_rope* rope, const 
  * only; 0 on unsupported arguments): 2 when the prompt's query blocks fill the part
  * (bf16, linear store: one block-store write, then one launch in which every workgroup
  * walks the whole key range of its (step, head) columns through LDS and writes `out`
- * directly), 3 on fp32 linear stores, else 3 per block of
+ * directly), 3 on fp32 linear stores, 4 on e4m3 ones (3 for one block), else 3 (e4m3: 4) per block of
  * 128 / (num_q_heads / num_kv_heads) steps. */
 int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t count);
 

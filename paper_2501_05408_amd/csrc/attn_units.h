@@ -16,6 +16,16 @@ inline size_t units_lds_bytes(int waves, int columns, int D) {
   return (size_t)waves * (32 + (size_t)(columns < 16 ? columns : 16) * D) * sizeof(float) + 2 * (size_t)D + 16;
 }
 
+// The bf16 store that an 8-bit store's groups are turned into for a prompt.
+struct UnpackParams {
+  void* k;                    // [batch * tiles][Hkv][Z * D] bf16
+  void* v;
+  int32_t* table;             // [batch][tiles]
+  int32_t tiles;
+  int32_t tile_mask;          // tile n lies in place n & tile_mask
+  int32_t first_group;        // of the sequence
+};
+
 // Score and choice of blocks.
 struct ChooseParams {
   void* bounds;               // [num_blocks][Hkv][2][D] bf16
@@ -37,6 +47,7 @@ struct ChooseParams {
 #define TEMPO_LAUNCHER __attribute__((weak)) hipError_t
 TEMPO_LAUNCHER launch_append_e4m3(const StoreParams& p, const void* k_new, const void* v_new, int D, hipStream_t stream);
 TEMPO_LAUNCHER launch_gather_e4m3(const StoreParams& p, void* k_out, void* v_out, int D, int j0, int count, hipStream_t stream);
+TEMPO_LAUNCHER launch_unpack_e4m3(const StoreParams& p, const UnpackParams& u, int groups, int D, hipStream_t stream);
 TEMPO_LAUNCHER launch_partial_e4m3(const AttnParams& p, int batch, int D, int grid_splits, int waves, hipStream_t stream);
 TEMPO_LAUNCHER launch_partial_selected(const SelectParams& p, int batch, int D, int dtype, int grid_splits, int waves, hipStream_t stream);
 TEMPO_LAUNCHER launch_combine_selected(const AttnParams& p, int batch, int D, hipStream_t stream);

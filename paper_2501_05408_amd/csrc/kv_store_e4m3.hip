@@ -1,6 +1,7 @@
 // The 8-bit block store: rows are quantised as they are written, and read back as the bf16 values that
 // their codes stand for (layout and scale: store_e4m3.h).  Where a row goes is as in kv_store.hip.
 #include "attn_bf16_common.h"
+#include "attn_units.h"
 #include "store_e4m3.h"
 
 namespace tempo {
@@ -285,7 +286,68 @@ __global__ __launch_bounds__(64) void kv_gather_e4m3(StoreParams p, uint16_t* __
   }
 }
 
+// ---- a prompt's keys and values as a bf16 store -----------------------------------------------
+// The prompt kernels are bound by the matrix cores and read each key many times, so an 8-bit store's groups are turned into
+// bf16 once, into a store laid out in the caller's workspace (u.table, u.k, u.v), which they then read.  A wavefront per
+// (sequence, head, group); a unit of codes is two units of bf16, lane by lane.
+template <int D>
+__global__ __launch_bounds__(64) void kv_unpack_e4m3(StoreParams p, UnpackParams u) {
+  const int lane = threadIdx.x;
+  const int grp = u.first_group + (int)blockIdx.x, head = blockIdx.y, b = blockIdx.z;
+  if (blockIdx.x == 0 && head == 0) {
+    for (int n = lane; n < u.tiles; n += 64) u.table[(int64_t)b * u.tiles + n] = b * u.tiles + n;
+  }
+  const int t0 = grp << 5, in = t0 & ((1 << p.z_log2) - 1);
+  const int64_t from = tile_slot(p, b, head, t0) + in, scales = all_slots(p) * D + from;
+  const int64_t to = ((((int64_t)b * u.tiles + ((t0 >> p.z_log2) & u.tile_mask)) * p.Hkv + head) << p.z_log2) + in;
+  const uint8_t* const k_pool = static_cast<const uint8_t*>(p.k_pool);
+  const uint8_t* const v_pool = static_cast<const uint8_t*>(p.v_pool);
+  const u32x4* const kp = reinterpret_cast<const u32x4*>(k_pool + from * D) + lane;
+  const u32x4* const vp = reinterpret_cast<const u32x4*>(v_pool + from * D) + lane;
+  u32x4* const ko = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(u.k) + to * D) + lane;
+  u32x4* const vo = reinterpret_cast<u32x4*>(static_cast<uint16_t*>(u.v) + to * D) + lane;
+  constexpr int UNITS = D / 32;
+  u32x4 k[UNITS], v[UNITS];
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    k[i] = __builtin_nontemporal_load(kp + i * 64);
+    v[i] = __builtin_nontemporal_load(vp + i * 64);
+  }
+  const uint32_t ks = *reinterpret_cast<const uint16_t*>(k_pool + scales + 2 * (lane & 15));
+  const uint2 vs = *reinterpret_cast<const uint2*>(v_pool + scales + 8 * (lane >> 4));
+  float sv[8];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    sv[r] = scale_of((vs.x >> (8 * r)) & 0xFFu);
+    sv[4 + r] = scale_of((vs.y >> (8 * r)) & 0xFFu);
+  }
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    const float s = scale_of(i < UNITS / 2 ? ks & 0xFFu : ks >> 8);
+    ko[(2 * i) * 64] = u32x4{values_of(k[i].x, false, s), values_of(k[i].x, true, s), values_of(k[i].y, false, s), values_of(k[i].y, true, s)};
+    ko[(2 * i + 1) * 64] = u32x4{values_of(k[i].z, false, s), values_of(k[i].z, true, s), values_of(k[i].w, false, s), values_of(k[i].w, true, s)};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {  // 8 slots of one dim: exact products, exact in bf16
+      float x[8];
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t word = v[i][2 * h + r];
+        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(word, false), z = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
+        x[4 * r] = a[0] * sv[4 * r]; x[4 * r + 1] = a[1] * sv[4 * r + 1];
+        x[4 * r + 2] = z[0] * sv[4 * r + 2]; x[4 * r + 3] = z[1] * sv[4 * r + 3];
+      }
+      vo[(2 * i + h) * 64] = pack8(x);
+    }
+  }
+}
+
 }  // namespace
+
+hipError_t launch_unpack_e4m3(const StoreParams& p, const UnpackParams& u, int groups, int D, hipStream_t stream) {
+  const dim3 grid((unsigned)groups, (unsigned)p.Hkv, (unsigned)p.batch);
+  if (D == 128) return launch(kv_unpack_e4m3<128>, grid, dim3(64), 0, stream, p, u);
+  return launch(kv_unpack_e4m3<64>, grid, dim3(64), 0, stream, p, u);
+}
 
 hipError_t launch_append_e4m3(const StoreParams& p, const void* k_new, const void* v_new, int D, hipStream_t stream) {
   const uint16_t* k = static_cast<const uint16_t*>(k_new);

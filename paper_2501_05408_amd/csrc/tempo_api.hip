@@ -1093,7 +1093,7 @@ PromptPlan plan_prompt(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t,
 // Does one launch answer all steps of a prompt (of a ring store's chunk)?  It does unless the call
 // is too large for the index range of its launches.
 bool prompt_in_one_launch(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t count) {
-  const int32_t heads = kv->dtype == TEMPO_BF16 ? kv->num_kv_heads : Hq;
+  const int32_t heads = kv->dtype == TEMPO_F32 ? Hq : kv->num_kv_heads;
   return (int64_t)batch * count * heads * kv->head_dim <= INT32_MAX;
 }
 
@@ -1149,7 +1149,7 @@ bool rows_apart(const tempo_kv* kv, const void* k_new, const void* v_new, const 
                 int32_t count) {
   const uintptr_t k = reinterpret_cast<uintptr_t>(k_new), v = reinterpret_cast<uintptr_t>(v_new);
   const uintptr_t o = reinterpret_cast<uintptr_t>(out);
-  const uintptr_t step_bytes = (uintptr_t)batch * count * kv->head_dim * (kv->dtype == TEMPO_BF16 ? 2 : 4);
+  const uintptr_t step_bytes = (uintptr_t)batch * count * kv->head_dim * (kv->dtype == TEMPO_F32 ? 4 : 2);
   const uintptr_t out_bytes = step_bytes * Hq, row_bytes = step_bytes * kv->num_kv_heads;
   return (o + out_bytes <= k || k + row_bytes <= o) && (o + out_bytes <= v || v + row_bytes <= o);
 }
@@ -1157,7 +1157,7 @@ bool rows_apart(const tempo_kv* kv, const void* k_new, const void* v_new, const 
 // Do answers of steps before the call's step c lie over rows (its k_new or v_new) of steps from c on?
 bool answers_over_later_rows(const tempo_kv* kv, const void* rows, const void* out, int32_t batch, int32_t Hq,
                              int32_t count, int32_t c) {
-  const int64_t step_bytes = (int64_t)kv->head_dim * (kv->dtype == TEMPO_BF16 ? 2 : 4);
+  const int64_t step_bytes = (int64_t)kv->head_dim * (kv->dtype == TEMPO_F32 ? 4 : 2);
   const int64_t row = step_bytes * kv->num_kv_heads, answer = step_bytes * Hq;
   const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(rows));
   for (int32_t b = 0; b < batch; ++b) {
@@ -1349,6 +1349,114 @@ int prefill_by_blocks(const tempo_kv* kv, const void* q, const void* k_new, cons
   return TEMPO_OK;
 }
 
+// An 8-bit store's keys and values as a bf16 store of `tiles` blocks for each sequence: table, keys, values.
+static size_t unpacked_pool_bytes(const tempo_kv* kv, int32_t batch, int32_t tiles) {
+  return align_up((size_t)batch * tiles * kv->num_kv_heads * kv->block_size * kv->head_dim * 2, 256);
+}
+static size_t unpacked_bytes(const tempo_kv* kv, int32_t batch, int32_t tiles) {
+  return align_up((size_t)batch * tiles * sizeof(int32_t), 256) + 2 * unpacked_pool_bytes(kv, batch, tiles);
+}
+
+// How many blocks a sequence's bf16 store needs for steps t .. t+C-1: all from its beginning, or, if fewer are seen, a ring of
+// so many (a power of two).
+static int32_t unpacked_tiles(const tempo_kv* kv, int32_t t, int32_t C, int32_t window, bool* ring) {
+  const int32_t Z = kv->block_size, last = t + C - 1, lo = window > 0 && t - window + 1 > 0 ? t - window + 1 : 0;
+  const int32_t all = last / Z + 1, seen = last / Z - lo / Z + 1;
+  int32_t R = 1;
+  while (R < seen) R *= 2;
+  *ring = kv->ring_blocks != 0 || R < all;
+  return *ring ? R : all;
+}
+
+// Steps from t on that an 8-bit store's prompt takes at a time: what a ring can hold, and one launch can index.
+static int32_t e4m3_chunk(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, int32_t left, int32_t window) {
+  const int64_t most = INT32_MAX / ((int64_t)batch * kv->num_kv_heads * kv->head_dim);
+  const int32_t C = ring_chunk(kv, t, left, window, kMaxColumns / (Hq / kv->num_kv_heads));
+  return C < most ? C : (int32_t)most;
+}
+// Are C steps answered over the codes?
+static bool e4m3_by_codes(const tempo_kv* kv, int32_t Hq, int32_t C, const int32_t* count_per_seq) {
+  return !count_per_seq && (int64_t)C * (Hq / kv->num_kv_heads) <= kMaxColumns;
+}
+// Bytes of the largest bf16 copy that a prompt needs.
+static size_t e4m3_copy_bytes(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window) {
+  size_t bytes = 0;
+  for (int32_t c0 = 0, C; c0 < count; c0 += C) {
+    C = e4m3_chunk(kv, batch, Hq, t + c0, count - c0, window);
+    bool ring;
+    const size_t own = e4m3_by_codes(kv, Hq, C, count_per_seq) ? 0 : unpacked_bytes(kv, batch, unpacked_tiles(kv, t + c0, C, window, &ring));
+    bytes = own > bytes ? own : bytes;
+  }
+  return bytes;
+}
+
+// A prompt on an 8-bit store: the rows are written, and attended over as they were written.  One block of columns is answered
+// over the codes; more by the bf16 prompt kernels over a bf16 copy of what the prompt sees, in the last copy_bytes bytes of
+// the workspace.  On a ring store in chunks that it can hold.
+static int prefill_e4m3(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch, int32_t Hq,
+                 int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window, float scale, void* workspace,
+                 size_t workspace_bytes, size_t copy_bytes, hipStream_t s, const tempo_rope* rope) {
+  const size_t partials = (workspace_bytes - copy_bytes) & ~(size_t)255;
+  const auto write = [&](int32_t c0, int32_t C) {
+    const size_t at = (size_t)c0 * kv->num_kv_heads * kv->head_dim * 2;
+    StoreParams sp = store_params(kv, batch, t + c0, nullptr, C);
+    sp.src_steps = count;
+    sp.count_per_seq = count_per_seq;
+    if (rope) {
+      sp.rope_cos = rope->cos;
+      sp.rope_sin = rope->sin;
+    }
+    return launch_status(launch_append(sp, static_cast<const char*>(k_new) + at, static_cast<const char*>(v_new) + at, kv->head_dim, kv->dtype, s),
+                         "kv_append_block");
+  };
+  int rc;
+  // a linear store takes all rows first (answers may lie over rows)
+  for (int32_t c0 = 0, C; c0 < count && !kv->ring_blocks; c0 += C) {
+    C = e4m3_chunk(kv, batch, Hq, t + c0, count - c0, window);
+    if ((rc = write(c0, C)) != TEMPO_OK) return rc;
+  }
+  for (int32_t c0 = 0, C; c0 < count; c0 += C) {
+    C = e4m3_chunk(kv, batch, Hq, t + c0, count - c0, window);
+    if (kv->ring_blocks && (rc = write(c0, C)) != TEMPO_OK) return rc;
+    const size_t q_at = (size_t)c0 * Hq * kv->head_dim * 2;
+    const char* const qc = static_cast<const char*>(q) + q_at;
+    char* const oc = static_cast<char*>(out) + q_at;
+    if (e4m3_by_codes(kv, Hq, C, count_per_seq)) {
+      tempo_plan plan;
+      make_block_plan(kv, batch, Hq, t + c0, window, false, C, &plan);
+      rc = do_partial(kv, qc, nullptr, nullptr, oc, batch, Hq, t + c0, nullptr, window, scale, &plan, workspace, s, C, rope, 0, count);
+      if (rc == TEMPO_OK && plan.num_splits > 1)
+        rc = do_combine(kv, oc, batch, Hq, t + c0, nullptr, window, &plan, workspace, s, C, 0, count);
+      if (rc != TEMPO_OK) return rc;
+      continue;
+    }
+    bool ring;
+    UnpackParams u;
+    u.tiles = unpacked_tiles(kv, t + c0, C, window, &ring);
+    u.tile_mask = ring ? u.tiles - 1 : INT32_MAX;
+    char* const at = static_cast<char*>(workspace) + partials;
+    u.table = reinterpret_cast<int32_t*>(at);
+    u.k = at + align_up((size_t)batch * u.tiles * sizeof(int32_t), 256);
+    u.v = static_cast<char*>(u.k) + unpacked_pool_bytes(kv, batch, u.tiles);
+    const int32_t lo = window > 0 && t + c0 - window + 1 > 0 ? t + c0 - window + 1 : 0;
+    u.first_group = lo >> 5;
+    const int groups = ((t + c0 + C - 1) >> 5) - (lo >> 5) + 1;
+    rc = launch_status(launch_unpack_e4m3(store_params(kv, batch, 0, nullptr), u, groups, kv->head_dim, s), "kv_unpack");
+    if (rc != TEMPO_OK) return rc;
+    tempo_kv copy = *kv;
+    copy.k_pool = u.k;
+    copy.v_pool = u.v;
+    copy.block_table = u.table;
+    copy.num_blocks = batch * u.tiles;
+    copy.max_blocks_per_seq = u.tiles;
+    copy.dtype = TEMPO_BF16;
+    copy.ring_blocks = ring ? u.tiles : 0;
+    rc = attend_prompt(&copy, qc, oc, batch, Hq, t + c0, C, count, count_per_seq, window, scale, workspace, partials, s, rope);
+    if (rc != TEMPO_OK) return rc;
+  }
+  return TEMPO_OK;
+}
+
 // Prompt processing: `count` steps per sequence, written and answered in one launch each, or
 // in blocks of as many steps as the column tiles hold.
 static int prefill(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch,
@@ -1357,7 +1465,6 @@ static int prefill(const tempo_kv* kv, const void* q, const void* k_new, const v
   int rc = check_store(kv);
   if (rc != TEMPO_OK) return rc;
   if (!q || !k_new || !v_new || !out) return TEMPO_ERR_NULL;
-  if (kv->dtype == TEMPO_E4M3) return TEMPO_ERR_DTYPE;
   if ((rc = check_heads(kv, batch, Hq)) != TEMPO_OK) return rc;
   if (count < 1 || count > (1 << 24)) return TEMPO_ERR_SHAPE;
   if (t < 0 || window < 0 || t > INT32_MAX - 64 - count) return TEMPO_ERR_RANGE;
@@ -1366,7 +1473,7 @@ static int prefill(const tempo_kv* kv, const void* q, const void* k_new, const v
   const int G = Hq / kv->num_kv_heads;
   const int32_t block = kMaxColumns / G;  // steps per block: all four column tiles
   if ((int64_t)batch * block * Hq * kv->head_dim > INT32_MAX) return TEMPO_ERR_SHAPE;
-  const size_t esz = kv->dtype == TEMPO_BF16 ? 2 : 4;
+  const size_t esz = kv->dtype == TEMPO_F32 ? 4 : 2;  // of rows and answers
   const bool ragged = false;  // every sequence starts at step t
   hipStream_t s = static_cast<hipStream_t>(stream);
   // validate every block before the first launch, so that an error leaves the store untouched
@@ -1381,10 +1488,14 @@ static int prefill(const tempo_kv* kv, const void* q, const void* k_new, const v
     const size_t partials = plan_bytes(kv, (int64_t)batch * C * Hq, plan.num_splits);
     need = partials > need ? partials : need;
   }
+  const bool k8 = kv->dtype == TEMPO_E4M3;
+  const size_t copy_bytes = k8 ? e4m3_copy_bytes(kv, batch, Hq, t, count, count_per_seq, window) : 0;
+  need = k8 ? align_up(need, 256) + align_up(copy_bytes, 256) : need;
+  if (k8 && workspace_bytes < need) return TEMPO_ERR_WORKSPACE;
 
   const bool one_launch = prompt_in_one_launch(kv, batch, Hq, count);
   // per-sequence prompt lengths exist in the prompt kernel only; the rotary producer is refused where that could not take the prompt
-  if ((count_per_seq || rope) && (kv->dtype != TEMPO_BF16 || kv->ring_blocks != 0 || !one_launch))
+  if ((count_per_seq || rope) && (kv->dtype == TEMPO_F32 || kv->ring_blocks != 0 || !one_launch))
     return TEMPO_ERR_SHAPE;
   if (rope && (rc = check_rope(rope, kv->head_dim, t + count - 1)) != TEMPO_OK) return rc;
   // A ring store keeps little more than its window, so it can't be written ahead of the answers.  Where the prompt
@@ -1394,7 +1505,9 @@ static int prefill(const tempo_kv* kv, const void* q, const void* k_new, const v
   if (kv->ring_blocks && !rows_apart(kv, k_new, v_new, out, batch, Hq, count)) {
     bool chunks = false, over = false;
     for (int32_t c = 0;;) {
-      c += one_launch ? ring_chunk(kv, t + c, count - c, window, block) : (count - c < block ? count - c : block);
+      c += k8           ? e4m3_chunk(kv, batch, Hq, t + c, count - c, window)
+           : one_launch ? ring_chunk(kv, t + c, count - c, window, block)
+                        : (count - c < block ? count - c : block);
       if (c >= count) break;
       chunks = true;
       over = over || answers_over_later_rows(kv, k_new, out, batch, Hq, count, c) ||
@@ -1417,6 +1530,8 @@ static int prefill(const tempo_kv* kv, const void* q, const void* k_new, const v
       }
     }
   }
+  if (k8)
+    return prefill_e4m3(kv, q, k_new, v_new, out, batch, Hq, t, count, count_per_seq, window, scale, workspace, workspace_bytes, copy_bytes, s, rope);
   const bool one_f32_block = kv->dtype == TEMPO_F32 && count <= block;  // (goes by blocks, which know the way by rows too)
   if (!rope && !one_f32_block && prompt_from_rows(kv, k_new, v_new, out, batch, Hq, t, count, window)) {
     const int64_t slots = kv->ring_blocks ? (int64_t)kv->ring_blocks * kv->block_size : count;
@@ -1500,20 +1615,22 @@ int tempo_rope_prefill_window(const tempo_kv* kv, const tempo_rope* rope, const 
 
 int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t count) {
   if (check_layout(kv) != TEMPO_OK || check_heads(kv, batch, num_q_heads) != TEMPO_OK || count < 1) return 0;
-  if (kv->dtype == TEMPO_E4M3) return 0;
   const int32_t G = num_q_heads / kv->num_kv_heads, block = kMaxColumns / G;
   if (kv->ring_blocks == 0 && prompt_in_one_launch(kv, batch, num_q_heads, count)) {
+    if (kv->dtype == TEMPO_E4M3) return count <= block ? 3 : 4;  // write, turn into bf16, attend, combine
     if (kv->dtype != TEMPO_BF16) return 3;
     if (prompt_fills_part(kv, batch, G, count)) return 2;  // one launch, and no key range is split
   }
-  return 3 * ((count + block - 1) / block);
+  return (kv->dtype == TEMPO_E4M3 ? 4 : 3) * ((count + block - 1) / block);
 }
 
 size_t tempo_prefill_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t) {
   if (check_layout(kv) != TEMPO_OK || check_heads(kv, batch, num_q_heads) != TEMPO_OK) return 0;
-  if (kv->dtype == TEMPO_E4M3) return 0;
   const int32_t block = kMaxColumns / (num_q_heads / kv->num_kv_heads);
-  return tempo_attn_block_workspace_bytes(kv, batch, num_q_heads, block, max_t);
+  const size_t partials = tempo_attn_block_workspace_bytes(kv, batch, num_q_heads, block, max_t);
+  if (kv->dtype != TEMPO_E4M3 || partials == 0) return partials;
+  // (behind partials for more splits than a block's plan takes: whole prompts may use them)
+  return align_up(partials, 256) + unpacked_bytes(kv, batch, kv->ring_blocks ? kv->ring_blocks : max_t / kv->block_size + 1);
 }
 
 int tempo_attn_block_with_plan(const tempo_kv* kv, const void* q, void* out, int32_t batch,

@@ -279,6 +279,68 @@ def test_rotary_steps_and_blocks(D, window):
         assert_attention(block[:, c], np64(turned), K, V, first + c, window, st.scale, f"rotary block, step {c}")
 
 
+# ---- prompts ----------------------------------------------------------------------------------------
+
+PROMPTS = [  # Hq, Hkv, D, Z, B, t, count, window, ring, rope, counts
+    (6, 2, 128, 64, 2, 0, 1, 0, 0, False, False), (6, 2, 128, 64, 2, 0, 42, 0, 0, False, False), (6, 2, 128, 64, 2, 0, 43, 0, 0, False, False),
+    (8, 2, 64, 32, 2, 37, 100, 0, 0, False, False), (24, 8, 128, 256, 2, 0, 300, 0, 0, False, False), (6, 2, 128, 64, 3, 0, 200, 0, 0, False, True),
+    (6, 2, 128, 64, 3, 70, 20, 0, 0, False, True), (6, 2, 64, 64, 2, 50, 150, 0, 0, True, False), (6, 2, 128, 64, 2, 3, 20, 0, 0, True, False),
+    (4, 2, 128, 32, 2, 500, 90, 33, 0, False, False), (4, 2, 128, 32, 2, 500, 90, 200, 0, True, True), (80, 1, 64, 64, 1, 20, 5, 0, 0, False, False),
+    (6, 2, 128, 64, 2, 300, 250, 100, 4, False, False), (8, 8, 64, 32, 1, 77, 600, 40, 8, False, False), (6, 2, 128, 64, 1, 0, 30, 64, 2, False, False),
+    (100, 1, 128, 64, 2, 0, 40, 0, 0, False, False),
+]
+
+
+@pytest.mark.parametrize("over_rows", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,D,Z,B,t,count,window,ring,rope,counts", PROMPTS)
+def test_prompts(Hq, Hkv, D, Z, B, t, count, window, ring, rope, counts, over_rows):
+    """Every step of a prompt against the oracle over what the store holds after it; with over_rows, the answers lie over
+    the prompt's own rows."""
+    n = t + count
+    q, K, V = normal(51, 1, (B, count, Hq, D)), normal(51, 2, (B, n, Hkv, D)), normal(51, 3, (B, n, Hkv, D))
+    st = make_store(51, B, Hq, Hkv, D, Z, n - 1, ring)
+    slots = ring * Z if ring else n
+    for t0 in range(max(0, t - slots) // 32 * 32 if ring else 0, t, slots):
+        m = min(slots, t - t0)
+        st.append_block(bf16(K[:, t0:t0 + m]), bf16(V[:, t0:t0 + m]), t0, m)
+    own = np.array([count, 0, count // 3])[:B] if counts else np.full(B, count)
+    rows = torch.empty(2 * B * count * Hkv * D + B * count * Hq * D, dtype=torch.bfloat16, device=DEV)
+    k_new, v_new = (rows[i * B * count * Hkv * D:(i + 1) * B * count * Hkv * D].view(B, count, Hkv, D) for i in (0, 1))
+    k_new.copy_(bf16(K[:, t:])), v_new.copy_(bf16(V[:, t:]))
+    out = (rows[:B * count * Hq * D] if over_rows else torch.empty(B * count * Hq * D, dtype=torch.bfloat16, device=DEV)).view(B, count, Hq, D)
+    if rope:
+        cos, sin = (torch.from_numpy(x.astype(np.float32)).to(DEV) for x in oracle.rope_table(n, D, 500000.0))
+        st.set_rope(cos, sin)
+        for c in range(count):
+            q[:, c], K[:, t + c] = (np64(st.rope_rotate(bf16(x), bf16(x), t + c)) for x in (q[:, c], K[:, t + c]))
+    raw_q = normal(51, 1, (B, count, Hq, D))
+    before = out.clone()
+    need = T.tempo_prefill_workspace_bytes(st.kv, B, Hq, n - 1 if not ring else slots + 128)
+    if ring:
+        need += 4 * rows.numel()
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    args = (B, Hq, t, count, torch.from_numpy(own.astype(np.int32)).to(DEV) if counts else None)
+    if window:
+        args += (window,)
+    call = {(0, 0): T.tempo_prefill_causal, (1, 0): T.tempo_prefill_window, (0, 1): T.tempo_rope_prefill_causal, (1, 1): T.tempo_rope_prefill_window}
+    lead = (st.kv, st.rope) if rope else (st.kv,)
+    call[(int(window > 0), int(rope))](*lead, bf16(raw_q), k_new, v_new, out, *args, st.scale, ws, need)
+    Kh, Vh = held(K), held(V)
+    for c in sorted({0, 1, 2, 31, 32, 63, 64, count // 2, count - 2, count - 1}):
+        live = [b for b in range(B) if 0 <= c < own[b]]
+        if live:
+            assert_attention(out[live, c], q[live, c], Kh[live], Vh[live], t + c, window, st.scale, f"step {c}")
+    for b in range(B):
+        if not over_rows:
+            assert torch.equal(out[b, own[b]:].view(torch.int16), before[b, own[b]:].view(torch.int16))
+        last = t + own[b]
+        first = max(0, last - slots) if ring else 0
+        if last > first:
+            kg, vg = st.gather(first, last - first)
+            np.testing.assert_array_equal(np64(kg)[b], Kh[b, first:last])
+            np.testing.assert_array_equal(np64(vg)[b], Vh[b, first:last])
+
+
 def test_nan_shows_where_it_is_seen_only():
     Hq, Hkv, D, Z, B, t, window = 6, 2, 128, 64, 2, 300, 100
     q, K, V = normal(17, 1, (B, Hq, D)), normal(17, 2, (B, t + 1, Hkv, D)), normal(17, 3, (B, t + 1, Hkv, D))
