@@ -32,7 +32,7 @@ struct ChooseParams {
   const void* q;              // [B][Hq][D] bf16
   const int32_t* block_table;
   const int32_t* t_per_seq;   // may be null
-  uint64_t* scores;           // [B][Hkv][tiles]: order-preserving bits of the scores
+  uint64_t* scores;           // [B][Hkv][tiles]: intervals of the scores, or their order-preserving bits
   int32_t* selected;          // [B][Hkv][pick]
   int32_t t;
   int32_t z_log2;

@@ -7,9 +7,11 @@
 //   choice   the first `first` blocks, the `last` newest ones (the newest may be incomplete: it has no bounds yet), and
 //            of the others those with the largest S_n, `pick` blocks in all; of equal scores the earlier block
 //
-// Scores are summed in 64 bits.  A product of two bf16 values is exact in fp32 and the sum of such products is exact, or
-// 1e-16 off, in fp64, so that the choice is that of the formula whatever the order of the sums; in fp32 blocks whose
-// scores lie within 1e-6 of the border would be chosen by rounding.
+// The choice is that of scores summed in 64 bits, in which products of two bf16 values are exact and their sums exact or 1e-16
+// off, so that it is the formula's whatever the order of the sums; by fp32 sums alone, blocks whose scores lie within 1e-6 of
+// the border would be chosen by rounding.
+#include <type_traits>
+
 #include "attn_bf16_common.h"
 #include "attn_units.h"
 #include "store_e4m3.h"
@@ -21,6 +23,42 @@ __device__ inline int step_of(const int32_t* t_per_seq, int t, int b) {
   int t_b = t_per_seq ? t_per_seq[b] : t;
   t_b = t_b > t ? t : t_b;
   return t_b < 0 ? 0 : t_b;
+}
+
+// A value of another lane of the row of 16, by lane moves instead of trips through the LDS permute unit; 0 where there is none.
+constexpr int kPairs = 0xB1, kFours = 0x4E, kEights = 0x141, kSixteens = 0x140;  // 1 0 3 2; 2 3 0 1; eight, sixteen lanes reversed
+constexpr int kRight = 0x100, kLeft = 0x110;                                    // + n: of the lane n further right / left
+template <int How>
+__device__ inline int lane_move(int v) { return __builtin_amdgcn_mov_dpp(v, How, 0xF, 0xF, true); }
+template <int How>
+__device__ inline float lane_move(float v) { return __builtin_bit_cast(float, lane_move<How>(__builtin_bit_cast(int, v))); }
+template <int How>
+__device__ inline double lane_move(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)lane_move<How>((int)(uint32_t)u), hi = (uint32_t)lane_move<How>((int)(uint32_t)(u >> 32));
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ inline float row_maximum(float v) {
+  v = fmaxf(v, lane_move<kPairs>(v));
+  v = fmaxf(v, lane_move<kFours>(v));
+  v = fmaxf(v, lane_move<kEights>(v));
+  return fmaxf(v, lane_move<kSixteens>(v));
+}
+__device__ inline float wave_max(float v) { return column_max(row_maximum(v)); }
+// Sums over the wavefront's lanes from this one on (kRight) or up to it (kLeft), and its total.
+template <int Side>
+__device__ inline int wave_sums(int v, int& total) {
+  v += lane_move<Side + 1>(v);
+  v += lane_move<Side + 2>(v);
+  v += lane_move<Side + 4>(v);
+  v += lane_move<Side + 8>(v);
+  constexpr int end = Side == kRight ? 0 : 15;  // of a row: its total
+  const int r0 = __builtin_amdgcn_readlane(v, end), r1 = __builtin_amdgcn_readlane(v, 16 + end);
+  const int r2 = __builtin_amdgcn_readlane(v, 32 + end), r3 = __builtin_amdgcn_readlane(v, 48 + end);
+  const int row = (threadIdx.x & 63) >> 4;
+  total = r0 + r1 + r2 + r3;
+  if (Side == kRight) return v + (row == 0 ? r1 + r2 + r3 : row == 1 ? r2 + r3 : row == 2 ? r3 : 0);
+  return v + (row == 0 ? 0 : row == 1 ? r0 : row == 2 ? r0 + r1 : r0 + r1 + r2);
 }
 
 // ---- bounds -----------------------------------------------------------------------------------
@@ -37,10 +75,11 @@ __device__ inline uint32_t values_in_order(i16x2 v) { return __builtin_bit_cast(
 // Over the 16 lanes of a row of lanes.
 template <typename F>
 __device__ inline i16x2 reduce_row(i16x2 v, F f) {
-  v = f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0xB1, 0xF, 0xF, true)));
-  v = f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x4E, 0xF, 0xF, true)));
-  v = f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x141, 0xF, 0xF, true)));
-  return f(v, __builtin_bit_cast(i16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x140, 0xF, 0xF, true)));
+  const auto moved = [&](auto how) { return __builtin_bit_cast(i16x2, lane_move<how.value>(__builtin_bit_cast(int, v))); };
+  v = f(v, moved(std::integral_constant<int, kPairs>()));
+  v = f(v, moved(std::integral_constant<int, kFours>()));
+  v = f(v, moved(std::integral_constant<int, kEights>()));
+  return f(v, moved(std::integral_constant<int, kSixteens>()));
 }
 
 // Bounds of the block of one kv head whose first slot has number `first` among the store's; wavefronts w < D/64 (8-bit store)
@@ -170,14 +209,22 @@ __device__ __forceinline__ void write_and_bound(const StoreParams& p, const void
   if (wave < (k8 ? D / 64 : D / 32)) bounds_of_block<D, k8>(p, first, wave, lane, bounds + pair * 2 * D, true, last, last_scale);
 }
 
-// Bits of a score in an order that whole numbers share; NaN above all.
-__device__ inline uint64_t key_of(double s) {
-  if (s != s) return ~(uint64_t)0;
-  const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);  // (-0 and 0 are equal)
-  return u >> 63 ? ~u : u | ((uint64_t)1 << 63);
-}
+// ---- scores -----------------------------------------------------------------------------------
+// Interval of a score: L <= S_n <= U.  sum_d max(q_d lo_d, q_d hi_d) is the product of [max(q, 0), min(q, 0)] and [hi, lo],
+// which the matrix cores take for 16 blocks and 16 heads at a time; how far its fp32 sums are off is bounded by kOff times
+// A = sum_d |q_d| max(|lo_d|, |hi_d|), another such product: 2 D = 256 exact products are added in some order, each addition
+// off by at most 2^-22 of the sums' magnitude, which A bounds (2^-24 is an fp32 rounding), so by 2^-14 A in all; a sixteenth
+// of it covers A's own error and the roundings of L and U.
+// Blocks whose interval leaves it open whether they are chosen are scored again, in 64 bits (exact_key), by the kernel that
+// chooses: one or two of hundreds.  All of them in 64 bits took 11.7 us for 16 sequences of 512 blocks and 24 heads of 128.
+constexpr float kOff = 1.0625f / 16384.f;
 
-// A wavefront scores 16 blocks: lane (row + 16c) holds dims 32s + 8c .. +7 of block `row`.
+struct Interval {
+  float lo, hi;
+};
+
+// A wavefront scores 16 blocks: lane (row + 16c) holds dims 32s + 8c .. +7 of block `row`, and of the query head that is
+// column `row` of a product.
 // kStore: of a whole step, whose row is written, and its block's bounds if it completes it, by the first workgroup of
 // every (sequence, kv head): no score reads either, as the newest block is chosen anyway (0: neither; 1: bf16 store; 2: 8-bit).
 template <int D, int kStore>
@@ -199,58 +246,87 @@ __global__ __launch_bounds__(256) void score_blocks(ChooseParams p, StoreParams 
   const int n = n0 + row <= newest - p.last ? n0 + row : n0;
   const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
   const uint16_t* const at = static_cast<const uint16_t*>(p.bounds) + ((int64_t)phys * p.Hkv + hkv) * 2 * D + 8 * c;
-  u32x4 lo[KS], hi[KS];
+  u32x4 lo[KS], hi[KS], far[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     lo[s] = *reinterpret_cast<const u32x4*>(at + 32 * s);
     hi[s] = *reinterpret_cast<const u32x4*>(at + D + 32 * s);
   }
   const uint16_t* const q = static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D + 8 * c;
-  u32x4 u[KS];
+  float low[4], high[4];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) u[s] = *reinterpret_cast<const u32x4*>(q + 32 * s);
-  float l[8 * KS], h[8 * KS];
+  for (int r = 0; r < 4; ++r) low[r] = high[r] = -INFINITY;
+  for (int g0 = 0; g0 < p.G; g0 += 16) {
+    const int g = g0 + row < p.G ? g0 + row : p.G - 1;
+    u32x4 x[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    unpack8(lo[s], l + 8 * s);
-    unpack8(hi[s], h + 8 * s);
-  }
-  uint64_t best = 0;
-  for (int g = 0; g < p.G; ++g) {
-    u32x4 now[KS];
-    const int ahead = g + 1 < p.G ? g + 1 : g;
+    for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const u32x4*>(q + (int64_t)g * D + 32 * s);
+    if (g0 == 0) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      now[s] = u[s];
-      u[s] = *reinterpret_cast<const u32x4*>(q + (int64_t)ahead * D + 32 * s);
-    }
-    double sums[2] = {0.0, 0.0};
+      for (int s = 0; s < KS; ++s) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      float x[8];
-      unpack8(now[s], x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float m = x[e] < 0.f ? l[8 * s + e] : h[8 * s + e];  // the larger product's
-        sums[e & 1] = fma((double)x[e], (double)m, sums[e & 1]);   // (NaN where a bound is)
+        for (int i = 0; i < 4; ++i)
+          far[s][i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2, lo[s][i] & 0x7FFF7FFFu),
+                                                                             __builtin_bit_cast(i16x2, hi[s][i] & 0x7FFF7FFFu)));
       }
     }
-    double sum = sums[0] + sums[1];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    const uint64_t key = key_of(sum);
-    best = key > best ? key : best;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f}, size = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      u32x4 plus, minus, both;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t pair = x[s][i];  // (a copy: a bit cast of a vector's element takes the vector's first one)
+        const uint32_t negative = __builtin_bit_cast(uint32_t, __builtin_bit_cast(i16x2, pair) >> 15);
+        plus[i] = pair & ~negative;
+        minus[i] = pair & negative;
+        both[i] = pair & 0x7FFF7FFFu;
+      }
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(hi[s]), as_bf16x8(plus), sum, 0, 0, 0);
+      size = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(far[s]), as_bf16x8(both), size, 0, 0, 0);
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(lo[s]), as_bf16x8(minus), sum, 0, 0, 0);
+    }
+    // lane (column + 16c): blocks n0 + 4c .. +3 for head g0 + column
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float off = size[r] * kOff, l = sum[r] - off, u = sum[r] + off;
+      const bool fine = u - l < INFINITY;  // false too where NaN or infinite: left to exact_key
+      low[r] = g0 + row < p.G && fine ? fmaxf(low[r], l) : low[r];
+      high[r] = g0 + row < p.G ? (fine ? fmaxf(high[r], u) : INFINITY) : high[r];
+    }
   }
-  if (c == 0 && n0 + row <= newest - p.last) p.scores[((int64_t)b * p.Hkv + hkv) * p.tiles + n0 + row] = best;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {  // over the heads
+    low[r] = row_maximum(low[r]);
+    high[r] = row_maximum(high[r]);
+  }
+  const int mine = n0 + 4 * c + row;  // lanes row < 4 write one block each
+  const float l = row == 0 ? low[0] : row == 1 ? low[1] : row == 2 ? low[2] : low[3];
+  const float u = row == 0 ? high[0] : row == 1 ? high[1] : row == 2 ? high[2] : high[3];
+  if (row < 4 && mine <= newest - p.last)
+    p.scores[((int64_t)b * p.Hkv + hkv) * p.tiles + mine] = (uint64_t)__builtin_bit_cast(uint32_t, u) << 32 | __builtin_bit_cast(uint32_t, l);
+}
+
+// Bits of a score in an order that whole numbers share; NaN above all, 0 below all.
+__device__ inline uint64_t key_of(double s) {
+  if (s != s) return ~(uint64_t)0;
+  const uint64_t u = __builtin_bit_cast(uint64_t, s + 0.0);  // (-0 and 0 are equal)
+  return u >> 63 ? ~u : u | ((uint64_t)1 << 63);
+}
+__device__ inline uint32_t key_of(float s) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, s + 0.0f);
+  return u >> 31 ? ~u : u | 0x80000000u;
 }
 
 // ---- choice ---------------------------------------------------------------------------------
-// One workgroup per (sequence, kv head).  The border, the m-th largest key of the candidates: keys are counted in 512 equal
-// parts of their range, then of the part that the border lies in, until at most 64 keys are left, which are ranked one by
-// one, or the part holds a single value.  Then the chosen blocks in ascending order.  (Counting by the keys' bytes from the
-// top down, 256 parts at a time, takes three or four rounds, as scores of one sign share their first byte.)
+// One workgroup per (sequence, kv head).  Of the candidates' intervals [L, U], `wanted` have an L of at least the wanted-th
+// largest one, so a score below that is not chosen, and at most `wanted` scores exceed the wanted-th largest U, so a score
+// above that is.  Both borders are taken a little outwards, at the edges of 512 equal parts of the intervals' range.  What
+// lies between them is scored in 64 bits: at most 64 blocks in LDS, where they are ranked one by one; more (equal scores, or
+// values far apart) in memory, where the border is searched for among the 64-bit keys, again by parts of their range.
 constexpr int kChoose = 512, kWaves = kChoose / 64, kParts = 512, kRanked = 64;
-constexpr int kCached = 4096;  // keys held in LDS; more are read again from memory
+constexpr int kHeads = 16;     // query heads held in LDS
+constexpr int kCached = 4096;  // intervals or keys held in LDS; more are read again from memory
 
 __device__ inline uint64_t shfl_xor_u64(uint64_t v, int m) {
   const uint32_t lo = (uint32_t)__shfl_xor((int)(uint32_t)v, m), hi = (uint32_t)__shfl_xor((int)(uint32_t)(v >> 32), m);
@@ -260,15 +336,10 @@ __device__ inline uint64_t shfl_xor_u64(uint64_t v, int m) {
 // Sum of `v` over the threads before this one; `total`: over all.  (at: kWaves integers; two barriers apart from other uses.)
 __device__ inline int sum_before(int v, int* at, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int sum = v;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(sum, m);
-    sum += lane >= m ? o : 0;
-  }
-  if (lane == 63) at[wave] = sum;
+  int all;
+  int before = wave_sums<kLeft>(v, all) - v;
+  if (lane == 0) at[wave] = all;
   __syncthreads();
-  int before = sum - v;
   total = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
@@ -278,152 +349,276 @@ __device__ inline int sum_before(int v, int* at, int& total) {
   return before;
 }
 
-__global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
-  __shared__ uint64_t cache[kCached];
-  __shared__ int bins[kParts];
-  __shared__ uint64_t ends[2][kWaves];
-  __shared__ uint64_t ranked_key[kRanked];
-  __shared__ int ranked_at[kRanked];
-  __shared__ int sums[2][kWaves], found[3], left, border_at;
-  __shared__ uint64_t border;
+// The part that the wanted-th largest of the values counted in bins[kParts] lies in, how many lie above it, and in it.  One
+// wavefront calls this; lane i has parts 8i .. 8i+7.
+__device__ inline void find_part(const int* bins, int wanted, int* found) {
+  const int lane = threadIdx.x & 63;
+  int own[8], sum = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    own[k] = bins[8 * lane + k];
+    sum += own[k];
+  }
+  int all;
+  int above = wave_sums<kRight>(sum, all) - sum;
+#pragma unroll
+  for (int k = 7; k >= 0; --k) {
+    if (above < wanted && above + own[k] >= wanted) {
+      found[0] = 8 * lane + k;
+      found[1] = above;
+      found[2] = own[k];
+    }
+    above += own[k];
+  }
+}
+
+// Score of block `phys` of the pool in 64 bits, by 16 lanes, in all of them.  ahead: the group's first kHeads query heads.
+template <int D>
+__device__ inline uint64_t exact_key(const ChooseParams& p, const uint16_t* ahead, int b, int hkv, int phys) {
+  const int d = 8 * (threadIdx.x & 15);
+  const bool live = d < D;
+  const uint16_t* const at = static_cast<const uint16_t*>(p.bounds) + ((int64_t)clamp_block(phys, p.num_blocks) * p.Hkv + hkv) * 2 * D + (live ? d : 0);
+  const uint16_t* const q = static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D + (live ? d : 0);
+  float l[8], h[8];
+  unpack8(*reinterpret_cast<const u32x4*>(at), l);
+  unpack8(*reinterpret_cast<const u32x4*>(at + D), h);
+  uint64_t best = 0;
+  for (int g = 0; g < p.G; ++g) {
+    float x[8];
+    unpack8(g < kHeads ? *reinterpret_cast<const u32x4*>(ahead + g * D + (live ? d : 0)) : *reinterpret_cast<const u32x4*>(q + (int64_t)g * D), x);
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float m = x[e] < 0.f ? l[e] : h[e];  // the larger product's (NaN where a bound is)
+      sum = fma((double)x[e], (double)m, sum);
+    }
+    sum = live ? sum : 0.0;
+    sum += lane_move<kPairs>(sum);
+    sum += lane_move<kFours>(sum);
+    sum += lane_move<kEights>(sum);
+    sum += lane_move<kSixteens>(sum);
+    const uint64_t key = key_of(sum);
+    best = key > best ? key : best;
+  }
+  return best;
+}
+
+struct ChooseShared {
+  uint64_t cache[kCached];
+  int phys[kCached];      // the candidates' blocks in the pool
+  __align__(16) uint16_t q[kHeads * 128];
+  int bins[2][kParts];
+  float range[2][kWaves];
+  uint64_t ends[2][kWaves];
+  uint64_t ranked_key[kRanked];
+  int ranked_at[kRanked];
+  int sums[2][kWaves], found[2][3], left, sure, border_at;
+  uint64_t border;
+};
+
+// The border among 64-bit keys (key_at(n), n = lo .. hi): chosen are keys above cut, and of those equal to it the blocks up to
+// cut_at.
+template <typename Key>
+__device__ void search_border(ChooseShared& sh, Key key_at, int lo, int hi, int wanted, uint64_t& cut, int& cut_at) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int b = blockIdx.y;
+  uint64_t least = ~(uint64_t)0, most = 0;
+  for (int n = lo + tid; n <= hi; n += kChoose) {
+    const uint64_t key = key_at(n);
+    least = key < least ? key : least;
+    most = key > most ? key : most;
+  }
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) {
+    const uint64_t a = shfl_xor_u64(least, m), z = shfl_xor_u64(most, m);
+    least = a < least ? a : least;
+    most = z > most ? z : most;
+  }
+  if (lane == 0) {
+    sh.ends[0][wave] = least;
+    sh.ends[1][wave] = most;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    least = sh.ends[0][w] < least ? sh.ends[0][w] : least;
+    most = sh.ends[1][w] > most ? sh.ends[1][w] : most;
+  }
+  int count = hi - lo + 1;  // candidates in least .. most
+  while (least != most && count != wanted) {
+    const int bits = 64 - __clzll((long long)(most - least));
+    const int shift = bits > 9 ? bits - 9 : 0;
+    sh.bins[0][tid] = 0;
+    __syncthreads();
+    for (int n = lo + tid; n <= hi; n += kChoose) {
+      const uint64_t key = key_at(n);
+      if (key >= least && key <= most) atomicAdd(&sh.bins[0][(key - least) >> shift], 1);
+    }
+    __syncthreads();
+    if (wave == 0) find_part(sh.bins[0], wanted, sh.found[0]);
+    __syncthreads();
+    least += (uint64_t)sh.found[0][0] << shift;
+    const uint64_t width = ((uint64_t)1 << shift) - 1;
+    most = most - least > width ? least + width : most;
+    wanted -= sh.found[0][1];
+    count = sh.found[0][2];
+    __syncthreads();  // found and bins are written again
+  }
+  cut = least;
+  cut_at = INT32_MAX;  // all that are left
+  if (count != wanted) {  // one value: the first `wanted` blocks that have it
+    const int each = (hi - lo + kChoose) / kChoose, n0 = lo + tid * each;
+    int mine = 0, all;
+    for (int n = n0; n < n0 + each && n <= hi; ++n) mine += key_at(n) == least;
+    int before = sum_before(mine, sh.sums[0], all);
+    for (int n = n0; n < n0 + each && n <= hi; ++n) {
+      if (key_at(n) == least && ++before == wanted) sh.border_at = n;
+    }
+    __syncthreads();
+    cut_at = sh.border_at;
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
+  __shared__ ChooseShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int hkv = blockIdx.x, b = blockIdx.y;
   const int newest = step_of(p.t_per_seq, p.t, b) >> p.z_log2;
-  const int64_t pair = (int64_t)b * p.Hkv + blockIdx.x;
-  const uint64_t* const scores = p.scores + pair * p.tiles;
+  const int64_t pair = (int64_t)b * p.Hkv + hkv;
+  uint64_t* const scores = p.scores + pair * p.tiles;
   int32_t* const out = p.selected + pair * p.pick;
+  const int32_t* const table = p.block_table + (int64_t)b * p.max_blocks_per_seq;
   if (newest < p.pick) {  // all of them
     for (int i = tid; i < p.pick; i += kChoose) out[i] = i <= newest ? i : -1;
     return;
   }
-  const int lo = p.first, hi = newest - p.last;  // candidates
-  int wanted = p.pick - p.first - p.last;        // of them; fewer than there are
+  for (int i = tid; i < (p.G < kHeads ? p.G : kHeads) * (D / 8); i += kChoose)
+    reinterpret_cast<u32x4*>(sh.q)[i] = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D)[i];
+  const int lo = p.first, hi = newest - p.last;     // candidates
+  const int wanted = p.pick - p.first - p.last;     // of them; fewer than there are
   const bool cached = hi - lo < kCached;
-  auto key_at = [&](int n) { return cached ? cache[n - lo] : scores[n]; };
-  // Chosen are the candidates with keys above cut, and of those with keys equal to it the ones up to cut_at.
+  auto word_at = [&](int n) { return cached ? sh.cache[n - lo] : scores[n]; };
+  auto phys_at = [&](int n) { return cached ? sh.phys[n - lo] : table[n]; };
+  auto interval = [&](uint64_t w) {
+    return Interval{__builtin_bit_cast(float, (uint32_t)w), __builtin_bit_cast(float, (uint32_t)(w >> 32))};
+  };
+  constexpr uint32_t kNone = ~0u - 1, kSure = ~0u;  // keys beyond all values': no border; of a block that has been found chosen
+  uint32_t sure_above = kNone, open_from = kSure;   // keys of U's outer border and L's
+  bool by_key = false;                         // words are 64-bit keys
   uint64_t cut = ~(uint64_t)0;
-  int cut_at = -1;
+  int cut_at = -1, open = 0, open_taken = 0;
+  auto sure = [&](uint64_t w) { return key_of(interval(w).lo) > sure_above; };
+  auto undecided = [&](uint64_t w) { return key_of(interval(w).hi) >= open_from && key_of(interval(w).lo) <= sure_above; };
   if (wanted > 0) {
-    uint64_t least = ~(uint64_t)0, most = 0;
+    float bottom = -INFINITY, top = -INFINITY;  // the largest finite -L and U
     for (int n = lo + tid; n <= hi; n += kChoose) {
-      const uint64_t key = scores[n];
-      if (cached) cache[n - lo] = key;
-      least = key < least ? key : least;
-      most = key > most ? key : most;
+      const uint64_t w = scores[n];
+      if (cached) {
+        sh.cache[n - lo] = w;
+        sh.phys[n - lo] = table[n];
+      }
+      const Interval v = interval(w);
+      bottom = v.lo > -INFINITY ? fmaxf(bottom, -v.lo) : bottom;
+      top = v.hi < INFINITY ? fmaxf(top, v.hi) : top;
     }
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) {
-      const uint64_t a = shfl_xor_u64(least, m), z = shfl_xor_u64(most, m);
-      least = a < least ? a : least;
-      most = z > most ? z : most;
-    }
+    bottom = wave_max(bottom);
+    top = wave_max(top);
     if (lane == 0) {
-      ends[0][wave] = least;
-      ends[1][wave] = most;
+      sh.range[0][wave] = bottom;
+      sh.range[1][wave] = top;
     }
+    sh.bins[0][tid] = sh.bins[1][tid] = 0;
+    if (tid == 0) sh.left = sh.sure = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      least = ends[0][w] < least ? ends[0][w] : least;
-      most = ends[1][w] > most ? ends[1][w] : most;
+      bottom = fmaxf(bottom, sh.range[0][w]);
+      top = fmaxf(top, sh.range[1][w]);
     }
-    int count = hi - lo + 1;  // candidates in least .. most
-    while (count > kRanked && least != most && count != wanted) {
-      const int bits = 64 - __clzll((long long)(most - least));
-      const int shift = bits > 9 ? bits - 9 : 0;
-      bins[tid] = 0;
-      __syncthreads();
-      for (int n = lo + tid; n <= hi; n += kChoose) {
-        const uint64_t key = key_at(n);
-        if (key >= least && key <= most) atomicAdd(&bins[(key - least) >> shift], 1);
-      }
-      __syncthreads();
-      if (wave == 0) {  // lane i: parts 8i .. 8i+7, and how many keys lie above those
-        int own[8], sum = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          own[k] = bins[8 * lane + k];
-          sum += own[k];
-        }
-        int above = sum;
-#pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-          const int o = __shfl_down(above, m);
-          above += lane + m < 64 ? o : 0;
-        }
-        above -= sum;
-#pragma unroll
-        for (int k = 7; k >= 0; --k) {
-          if (above < wanted && above + own[k] >= wanted) {
-            found[0] = 8 * lane + k;
-            found[1] = above;
-            found[2] = own[k];
-          }
-          above += own[k];
-        }
-      }
-      __syncthreads();
-      least += (uint64_t)found[0] << shift;
-      const uint64_t width = ((uint64_t)1 << shift) - 1;
-      most = most - least > width ? least + width : most;
-      wanted -= found[1];
-      count = found[2];
-      __syncthreads();  // found and bins are written again
+    const uint32_t least = key_of(-bottom), highest = key_of(top), most = highest < least ? least : highest;
+    const int bits = most == least ? 0 : 32 - __clz((int)(most - least));
+    const int shift = bits > 9 ? bits - 9 : 0;
+    auto part = [&](uint32_t key) { return key <= least ? 0 : ((key < most ? key : most) - least) >> shift; };
+    for (int n = lo + tid; n <= hi; n += kChoose) {
+      const Interval v = interval(word_at(n));
+      atomicAdd(&sh.bins[0][part(key_of(v.lo))], 1);
+      atomicAdd(&sh.bins[1][part(key_of(v.hi))], 1);
     }
-    if (count == wanted) {  // all that are left
-      cut = least;
-      cut_at = INT32_MAX;
-    } else if (least == most) {  // one value: the first `wanted` blocks that have it
-      cut = least;
-      const int each = (hi - lo + kChoose) / kChoose, n0 = lo + tid * each;
-      int mine = 0, all;
-      for (int n = n0; n < n0 + each && n <= hi; ++n) mine += key_at(n) == least;
-      int before = sum_before(mine, sums[0], all);
-      for (int n = n0; n < n0 + each && n <= hi; ++n) {
-        if (key_at(n) == least && ++before == wanted) border_at = n;
+    __syncthreads();
+    if (wave < 2) find_part(sh.bins[wave], wanted, sh.found[wave]);
+    __syncthreads();
+    // (the first part holds whatever lies below it, the last one whatever lies above)
+    open_from = sh.found[0][0] == 0 ? 0u : least + ((uint32_t)sh.found[0][0] << shift);
+    const uint32_t past = least + ((uint32_t)(sh.found[1][0] + 1) << shift);  // first key of the next part
+    sure_above = sh.found[1][0] == (int)part(most) ? kNone : past - 1;
+    int sures = 0;  // of the wavefront
+    for (int n = lo + tid; n <= hi; n += kChoose) {
+      const uint64_t w = word_at(n);
+      sures += __popcll(__ballot(sure(w)));
+      if (undecided(w)) {
+        const int i = atomicAdd(&sh.left, 1);  // (in any order: ranks do not depend on it)
+        if (i < kRanked) sh.ranked_at[i] = n;
       }
-      __syncthreads();
-      cut_at = border_at;
-    } else {  // few: the one that wanted - 1 of them come before
-      if (tid == 0) left = 0;
-      __syncthreads();
-      for (int n = lo + tid; n <= hi; n += kChoose) {
-        const uint64_t key = key_at(n);
-        if (key >= least && key <= most) {
-          const int i = atomicAdd(&left, 1);  // (in any order: ranks do not depend on it)
-          ranked_key[i] = key;
-          ranked_at[i] = n;
+    }
+    if (lane == 0 && sures) atomicAdd(&sh.sure, sures);  // (lane 0 is in every round that the wavefront is in)
+    __syncthreads();
+    open = sh.left;
+    open_taken = wanted - sh.sure;
+    if (open > kRanked) {
+      // keys instead of intervals: decided blocks above or below all others
+      for (int i = tid >> 4; i <= hi - lo; i += kChoose / 16) {
+        const uint64_t w = word_at(lo + i);
+        uint64_t key = sure(w) ? ~(uint64_t)0 : 0;
+        if (undecided(w)) key = exact_key<D>(p, sh.q, b, hkv, phys_at(lo + i));
+        if ((lane & 15) == 0) {
+          scores[lo + i] = key;
+          if (cached) sh.cache[i] = key;
         }
       }
       __syncthreads();
-      if (tid < count) {
-        const uint64_t key = ranked_key[tid];
-        const int n = ranked_at[tid];
+      by_key = true;
+      search_border(sh, word_at, lo, hi, wanted, cut, cut_at);
+    } else if (open != open_taken) {
+      for (int i = tid >> 4; i < open; i += kChoose / 16) {
+        const uint64_t key = exact_key<D>(p, sh.q, b, hkv, phys_at(sh.ranked_at[i]));
+        if ((lane & 15) == 0) sh.ranked_key[i] = key;
+      }
+      __syncthreads();
+      if (tid < open) {
+        const uint64_t key = sh.ranked_key[tid];
+        const int n = sh.ranked_at[tid];
         int rank = 0;
-        for (int i = 0; i < count; ++i) rank += ranked_key[i] > key || (ranked_key[i] == key && ranked_at[i] < n);
-        if (rank == wanted - 1) {
-          border = key;
-          border_at = n;
+        for (int i = 0; i < open; ++i) rank += sh.ranked_key[i] > key || (sh.ranked_key[i] == key && sh.ranked_at[i] < n);
+        if (rank < open_taken) {
+          if (cached) sh.cache[n - lo] = 0x7FFFFFFFu;  // (key_of() of that is kSure)
+          else scores[n] = 0x7FFFFFFFu;
         }
       }
       __syncthreads();
-      cut = border;
-      cut_at = border_at;
     }
   }
-  // In ascending order: every thread the blocks of one run.
-  const int each = (newest + kChoose) / kChoose, n0 = tid * each;
+  // In ascending order.
   auto chosen = [&](int n) {
     if (n > newest) return false;
     if (n < lo || n > hi) return true;
-    const uint64_t key = key_at(n);
-    return key > cut || (key == cut && n <= cut_at);
+    if (wanted == 0) return false;
+    const uint64_t w = word_at(n);
+    if (by_key) return w > cut || (w == cut && n <= cut_at);
+    return sure(w) || (open == open_taken && undecided(w));
   };
-  int mine = 0, all;
-  for (int n = n0; n < n0 + each; ++n) mine += chosen(n);
-  int place = sum_before(mine, sums[1], all);
-  for (int n = n0; n < n0 + each; ++n) {
-    if (chosen(n) && place < p.pick) out[place++] = n;
+  int place = 0;
+  for (int n0 = 0, round = 0; n0 <= newest; n0 += kChoose, round ^= 1) {
+    const bool take = chosen(n0 + tid);
+    const uint64_t takes = __ballot(take);
+    if (lane == 0) sh.sums[round][wave] = __popcll(takes);
+    __syncthreads();  // (the other round's sums are written before, read after it)
+    int before = place + __popcll(takes & (((uint64_t)1 << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      before += w < wave ? sh.sums[round][w] : 0;
+      place += sh.sums[round][w];
+    }
+    if (take && before < p.pick) out[before] = n0 + tid;
   }
 }
 
@@ -461,7 +656,8 @@ hipError_t launch_select_blocks(const ChooseParams& p, const StoreParams* store,
   else if (dtype == TEMPO_E4M3) e = D == 128 ? launch_score<128, 2>(p, *store, k_new, v_new, batch, stream) : launch_score<64, 2>(p, *store, k_new, v_new, batch, stream);
   else e = D == 128 ? launch_score<128, 1>(p, *store, k_new, v_new, batch, stream) : launch_score<64, 1>(p, *store, k_new, v_new, batch, stream);
   if (e != hipSuccess) return e;
-  return launch(choose_blocks, dim3((unsigned)p.Hkv, (unsigned)batch), dim3(kChoose), 0, stream, p);
+  const dim3 pairs((unsigned)p.Hkv, (unsigned)batch);
+  return D == 128 ? launch(choose_blocks<128>, pairs, dim3(kChoose), 0, stream, p) : launch(choose_blocks<64>, pairs, dim3(kChoose), 0, stream, p);
 }
 
 }  // namespace tempo

@@ -161,6 +161,30 @@ def test_choice_between_scores_that_fp32_does_not_tell_apart():
     assert got[0, 0].tolist() == best
 
 
+@pytest.mark.parametrize("close", [5, 40, 63, 64, 65, 150])
+def test_choice_among_blocks_that_are_closer_than_fp32_sums_tell(close):
+    """`close` blocks with scores of 2^12 + k 2^-8 in random order around the border, the others clearly above or below."""
+    D, Z, blocks, pick = 128, 32, 400, 100
+    st = make_store(34, T.TEMPO_BF16, 2, 4, 2, D, Z, blocks * Z - 1)
+    rng = np.random.default_rng(close)
+    edge = np.zeros((st.num_blocks, 2, 2, D))
+    table = st.block_table.cpu().numpy()
+    above = pick - 2 - close // 2
+    for b in range(2):
+        for h in range(2):
+            order = rng.permutation(np.arange(1, blocks - 1))
+            place = edge[table[b], h]
+            place[order, 1, 5] = 3000.0
+            place[order[:above], 1, 5] = 6000.0
+            near = order[above:above + close]
+            place[near, 1, 5], place[near, 1, 77] = 4096.0, rng.permutation(close) / 256.0
+            edge[table[b], h] = place
+    q = np.zeros((2, 4, D))
+    q[:, :, 5] = q[:, :, 77] = 1.0
+    q[:, 1::2] *= 0.5
+    assert_choice(st, bf16(edge), q, blocks * Z - 1, None, pick, 1, 1)
+
+
 def test_choice_of_nan_infinite_and_extreme_bounds():
     D, Z, blocks, B = 64, 32, 100, 2
     st = make_store(26, T.TEMPO_BF16, B, 2, 1, D, Z, blocks * Z - 1)
