@@ -182,36 +182,44 @@ __device__ __forceinline__ void merge_units(const AttnParams& p, const float* sm
   const float* sm_m = smem;
   const float* sm_l = smem + NW * 16;
   const float* sm_acc = smem + NW * 32;
-  for (int idx = threadIdx.x; idx < ncols * D; idx += 64 * NW) {
-    const int j = idx / D, d = idx - j * D;
-    float mw[NW], lw[NW], aw[NW];
+  // A thread takes 4 dims of a column at a time (one by one, a single wavefront's 16 columns of 128 took 9.5 us a launch of
+  // one group, 5.6 now).
+  for (int idx = threadIdx.x; idx < ncols * (D / 4); idx += 64 * NW) {
+    const int j = idx / (D / 4), d = 4 * (idx % (D / 4));
+    float mw[NW], lw[NW];
+    f32x4 aw[NW];
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       mw[w] = sm_m[w * 16 + j];
       lw[w] = sm_l[w * 16 + j];
-      aw[w] = sm_acc[(w * ncols + j) * D + d];
+      aw[w] = *reinterpret_cast<const f32x4*>(sm_acc + (w * ncols + j) * D + d);
     }
     float M = mw[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) M = fmaxf(M, mw[w]);
     const float ref = M == -INFINITY ? 0.f : M;  // nothing seen, or nothing but NaN, which has to show
-    float num = 0.f, den = 0.f;
+    f32x4 num = {0.f, 0.f, 0.f, 0.f};
+    float den = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       const bool seen = lw[w] != 0.f;  // (a column's largest weight is 1)
       const float wgt = fast_exp2(mw[w] - ref);
-      num += seen ? wgt * aw[w] : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] += seen ? wgt * aw[w][e] : 0.f;
       den += seen ? wgt * lw[w] : 0.f;
     }
     const int jc = (first_col + j) / p.G, jg = first_col + j - jc * p.G;
     if (p.direct) {
       const int64_t orow = ((int64_t)b * p.io_steps + jc) * p.Hq + (int64_t)hkv * p.G + jg;
-      const float o = kSelect && den == 0.f ? 0.f : num / den;  // a list may name no key of this step
-      static_cast<__bf16*>(p.out)[orow * D + d] = (__bf16)o;
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (__bf16)(kSelect && den == 0.f ? 0.f : num[e] / den);  // (a list may name no key)
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + orow * D + d) = o;
     } else {
       const int64_t row = ((int64_t)b * p.queries + jc) * p.Hq + (int64_t)hkv * p.G + jg;
       const int64_t part = row * p.num_splits + split;
-      p.ws_acc[part * D + d] = num;
+      *reinterpret_cast<f32x4*>(p.ws_acc + part * D + d) = num;
       if (d == 0) {
         p.ws_ml[part * 2] = M;
         p.ws_ml[part * 2 + 1] = den;

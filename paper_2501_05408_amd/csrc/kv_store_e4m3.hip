@@ -66,13 +66,14 @@ __device__ inline uint32_t values_of(uint32_t codes, bool high, float scale) {
 }
 
 // ---- by 32-slot groups ------------------------------------------------------------------
-// One wavefront per (sequence, head, group).  A lane works on blocks of 4 consecutive slots x 8 consecutive dims, D/8
-// lanes side by side on the same slots: 16-byte pieces of 4 rows in the caller's arrays, and in the store 8 codes of each
-// key row and, of the values, 4 codes (the 4 slots) of each dim, between which a block is turned in registers.  The group's
-// image passes through LDS, so that the store is read and written in whole units of 1 KiB, the rows in runs of D elements.
-// Bound by memory: 8 x 2047 rows in 8 heads of 128 are written in 24.6 us (101 MB, 4.1 TB/s; a large copy moves 4.9) and
-// read back in 16.3; row by row and element by element it was 52.6 and 73.2.
-
+// One workgroup per (sequence, head, group), half of its wavefronts for the keys, half for the values.  A lane works on a block
+// of 4 consecutive slots x 8 consecutive dims, D/8 lanes side by side on the same slots: 16-byte pieces of 4 rows in the
+// caller's arrays, and in the store 8 codes of each key row or, of the values, 4 codes (the 4 slots) of each dim, between which
+// a block is turned in registers.  The group's images pass through LDS, so that the store is read and written in whole units of
+// 1 KiB, the rows in runs of D elements.
+// Bound by memory: 8 x 2047 rows in 8 heads of 128 are written in 20.3 us (101 MB, 5.0 TB/s; a large copy moves 4.9) and read
+// back in 16.2; by one wavefront a group 24.6 and 16.3 (2 x 1104 rows 8.9 and 6.0, now 6.9 and 4.4); row by row and element by
+// element 52.6 and 73.2.
 // 4 words of 4 bytes, a[i] = byte i of every column: columns to rows.
 __device__ inline void turn4(uint32_t* a) {
   const uint32_t t0 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400), t1 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602);
@@ -83,15 +84,14 @@ __device__ inline void turn4(uint32_t* a) {
   a[3] = __builtin_amdgcn_perm(t3, t1, 0x07060302);
 }
 
-// Maximum of both 16-bit halves over the D/8 lanes that hold a row.
+// Maximum over the D/8 lanes that hold a row.
 template <int D>
 __device__ inline uint32_t row_max(uint32_t v) {
-  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-  auto step = [&](uint32_t o) { v = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v), __builtin_bit_cast(u16x2, o))); };
-  step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lanes 1, 0, 3, 2 of four
-  step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // 2, 3, 0, 1
-  step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));  // eight lanes reversed
-  if (D == 128) step((uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));  // sixteen
+  auto step = [&](int o) { v = (uint32_t)o > v ? (uint32_t)o : v; };
+  step(__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lanes 1, 0, 3, 2 of four
+  step(__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // 2, 3, 0, 1
+  step(__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));  // eight lanes reversed
+  if (D == 128) step(__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));  // sixteen
   return v;
 }
 
@@ -111,10 +111,12 @@ __device__ inline int value_piece(int sg, int part, int k) {
 __host__ __device__ constexpr int in_lds(int at) { return at + (at >> 8) * 16; }
 
 template <int D>
-__global__ __launch_bounds__(64) void kv_append_groups_e4m3(StoreParams p, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new) {
-  constexpr int PARTS = D / 8, BLOCKS = 8 * PARTS / 64;  // blocks a lane works on
-  __shared__ __align__(16) uint8_t image[in_lds(32 * D)];
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(2 * D) void kv_append_groups_e4m3(StoreParams p, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new) {
+  constexpr int PARTS = D / 8, HALF = D;  // blocks of a group, and threads, for keys and for values
+  __shared__ __align__(16) uint8_t images[2][in_lds(32 * D)];
+  const int tid = threadIdx.x % HALF;
+  const bool value = __builtin_amdgcn_readfirstlane(threadIdx.x >= HALF);
+  uint8_t* const image = images[value];
   const int g = blockIdx.x, head = blockIdx.y, b = blockIdx.z;
   const int rows_b = rows_of(p, b) < p.count ? rows_of(p, b) : p.count;
   const int t0 = ((p.t >> 5) + g) << 5;  // first step of this group
@@ -125,164 +127,116 @@ __global__ __launch_bounds__(64) void kv_append_groups_e4m3(StoreParams p, const
   const bool whole = lo == 0 && hi == 32;
   const int64_t slot0 = tile_slot(p, b, head, t0) + (t0 & ((1 << p.z_log2) - 1)), scales = all_slots(p) * D + slot0;
   const int64_t row0 = ((int64_t)b * p.src_steps + first_row) * p.Hkv + head;  // (rows are Hkv apart)
+  const int part = tid % PARTS, sg = tid / PARTS;
+  const uint16_t* const rows = value ? v_new : k_new;
+  uint8_t* const pool = static_cast<uint8_t*>(value ? p.v_pool : p.k_pool);
 
   // The caller's pieces; rows outside the call are read as its nearest row and not written.
-  u32x4 k[BLOCKS][4], v[BLOCKS][4];
+  auto row_at = [&](int slot) { return row0 + (int64_t)(slot < lo ? lo : (slot < hi ? slot : hi - 1)) * p.Hkv; };
+  u32x4 x[4];
 #pragma unroll
-  for (int n = 0; n < BLOCKS; ++n) {
-    const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int slot = 4 * sg + i;
-      const int64_t at = (row0 + (int64_t)(slot < lo ? lo : (slot < hi ? slot : hi - 1)) * p.Hkv) * D + 8 * part;
-      k[n][i] = *reinterpret_cast<const u32x4*>(k_new + at);
-      v[n][i] = *reinterpret_cast<const u32x4*>(v_new + at);
-    }
-  }
-  if (p.rope_cos) {  // a piece and its partner D/2 dims away are turned together, each lane for its own
-#pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) {
-      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
-      const int other = part < PARTS / 2 ? part + PARTS / 2 : part - PARTS / 2;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int slot = 4 * sg + i, from = slot < lo ? lo : (slot < hi ? slot : hi - 1);
-        u32x4 o = *reinterpret_cast<const u32x4*>(k_new + (row0 + (int64_t)from * p.Hkv) * D + 8 * other);
-        if (part < PARTS / 2) rotate_pieces(p.rope_cos, p.rope_sin, t0 + from, D / 2, 8 * part, k[n][i], o);
-        else rotate_pieces(p.rope_cos, p.rope_sin, t0 + from, D / 2, 8 * other, o, k[n][i]);
-      }
-    }
-  }
-
-  uint8_t* const k_pool = static_cast<uint8_t*>(p.k_pool);
-  uint8_t* const v_pool = static_cast<uint8_t*>(p.v_pool);
-  uint32_t vc[BLOCKS][2][4];  // values: codes of slot i, dims 0..3 and 4..7 of the block; turned: of dim k, slots 0..3
-#pragma unroll
-  for (int n = 0; n < BLOCKS; ++n) {
-    const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+  for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(rows + row_at(4 * sg + i) * D + 8 * part);
+  if (p.rope_cos && !value) {  // a piece and its partner D/2 dims away are turned together, each lane for its own
+    const int other = part < PARTS / 2 ? part + PARTS / 2 : part - PARTS / 2;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint32_t kt = 0, vt = 0;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        kt = top_of(k[n][i][e], kt);
-        vt = top_of(v[n][i][e], vt);
-      }
-      const uint32_t top = row_max<D>(kt | (vt << 16));
-      const uint32_t Ek = (uint32_t)scale_byte(top & 0xFFFFu), Ev = (uint32_t)scale_byte(top >> 16);
-      const float ki = inverse_scale_of(Ek), vi = inverse_scale_of(Ev), km = largest_code(Ek), vm = largest_code(Ev);
-      const u32x4 a = k[n][i], z = v[n][i];
-      *reinterpret_cast<uint2*>(image + in_lds(key_piece<D>(sg, part, i))) =
-          uint2{codes_of(a.x, ki, km) | (codes_of(a.y, ki, km) << 16), codes_of(a.z, ki, km) | (codes_of(a.w, ki, km) << 16)};
-      vc[n][0][i] = codes_of(z.x, vi, vm) | (codes_of(z.y, vi, vm) << 16);
-      vc[n][1][i] = codes_of(z.z, vi, vm) | (codes_of(z.w, vi, vm) << 16);
-      const int slot = 4 * sg + i;
-      if (part == 0 && slot >= lo && slot < hi) {
-        k_pool[scales + scale_off_k(slot)] = (uint8_t)Ek;
-        v_pool[scales + scale_off_v(slot)] = (uint8_t)Ev;
-      }
+      const int slot = 4 * sg + i, t = t0 + (slot < lo ? lo : (slot < hi ? slot : hi - 1));
+      u32x4 o = *reinterpret_cast<const u32x4*>(rows + row_at(slot) * D + 8 * other);
+      if (part < PARTS / 2) rotate_pieces(p.rope_cos, p.rope_sin, t, D / 2, 8 * part, x[i], o);
+      else rotate_pieces(p.rope_cos, p.rope_sin, t, D / 2, 8 * other, o, x[i]);
     }
   }
-  __syncthreads();
-  // keys: a unit's 16 bytes belong to one slot
+  uint32_t codes[2][4];  // of slot i, dims 0..3 and 4..7 of the block; values, turned: of dim k, slots 0..3
 #pragma unroll
-  for (int u = 0; u < D / 32; ++u) {
-    const int slot = 16 * (u / (D / 64)) + (lane & 15), at = u * 1024 + lane * 16;
-    if (slot >= lo && slot < hi) *reinterpret_cast<u32x4*>(k_pool + slot0 * D + at) = *reinterpret_cast<const u32x4*>(image + in_lds(at));
+  for (int i = 0; i < 4; ++i) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = top_of(x[i][e], top);
+    const uint32_t E = (uint32_t)scale_byte(row_max<D>(top));
+    const float inverse = inverse_scale_of(E), most = largest_code(E);
+    codes[0][i] = codes_of(x[i].x, inverse, most) | (codes_of(x[i].y, inverse, most) << 16);
+    codes[1][i] = codes_of(x[i].z, inverse, most) | (codes_of(x[i].w, inverse, most) << 16);
+    const int slot = 4 * sg + i;
+    if (part == 0 && slot >= lo && slot < hi) pool[scales + (value ? scale_off_v(slot) : scale_off_k(slot))] = (uint8_t)E;
+    if (!value) *reinterpret_cast<uint2*>(image + in_lds(key_piece<D>(sg, part, i))) = uint2{codes[0][i], codes[1][i]};
   }
-  if (!whole) {  // this call's slots only, byte by byte: another launch may write the others at the same time
+  if (value && !whole) {  // this call's slots only, byte by byte: another launch may write the others at the same time
 #pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) {
-      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+    for (int i = 0; i < 4; ++i) {
+      if (4 * sg + i < lo || 4 * sg + i >= hi) continue;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (4 * sg + i < lo || 4 * sg + i >= hi) continue;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v_pool[slot0 * D + value_piece<D>(sg, part, e) + i] = (uint8_t)(vc[n][e >> 2][i] >> (8 * (e & 3)));
-      }
+      for (int e = 0; e < 8; ++e) pool[slot0 * D + value_piece<D>(sg, part, e) + i] = (uint8_t)(codes[e >> 2][i] >> (8 * (e & 3)));
     }
-    return;
   }
-  __syncthreads();  // the image is written again
-#pragma unroll
-  for (int n = 0; n < BLOCKS; ++n) {
-    const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
+  if (value && whole) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      turn4(vc[n][q]);
+      turn4(codes[q]);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(image + in_lds(value_piece<D>(sg, part, 4 * q + e))) = vc[n][q][e];
+      for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(image + in_lds(value_piece<D>(sg, part, 4 * q + e))) = codes[q][e];
     }
   }
   __syncthreads();
+  if (value && !whole) return;
 #pragma unroll
-  for (int u = 0; u < D / 32; ++u) {
-    const int at = u * 1024 + lane * 16;
-    *reinterpret_cast<u32x4*>(v_pool + slot0 * D + at) = *reinterpret_cast<const u32x4*>(image + in_lds(at));
+  for (int u = 0; u < 32 * D / (16 * HALF); ++u) {
+    const int at = (u * HALF + tid) * 16, slot = 16 * (at / (16 * D)) + (tid & 15);  // (a key unit's 16 bytes belong to one slot)
+    if (value || (slot >= lo && slot < hi)) *reinterpret_cast<u32x4*>(pool + slot0 * D + at) = *reinterpret_cast<const u32x4*>(image + in_lds(at));
   }
 }
 
 // Read-back of steps j0 .. j0+count-1: out[b][j - j0][head][d].
 template <int D>
-__global__ __launch_bounds__(64) void kv_gather_e4m3(StoreParams p, uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out, int j0, int count) {
-  constexpr int PARTS = D / 8, BLOCKS = 8 * PARTS / 64, UNITS = D / 32;
-  __shared__ __align__(16) uint8_t image[in_lds(32 * D)];
-  const int lane = threadIdx.x;
+__global__ __launch_bounds__(2 * D) void kv_gather_e4m3(StoreParams p, uint16_t* __restrict__ k_out, uint16_t* __restrict__ v_out, int j0, int count) {
+  constexpr int PARTS = D / 8, HALF = D;
+  __shared__ __align__(16) uint8_t images[2][in_lds(32 * D)];
+  const int tid = threadIdx.x % HALF;
+  const bool value = __builtin_amdgcn_readfirstlane(threadIdx.x >= HALF);
+  uint8_t* const image = images[value];
   const int g = blockIdx.x, head = blockIdx.y, b = blockIdx.z;
   const int t0 = ((j0 >> 5) + g) << 5, first_row = t0 - j0;
   const int lo = first_row < 0 ? -first_row : 0, hi = count - first_row < 32 ? count - first_row : 32;
   const int64_t slot0 = tile_slot(p, b, head, t0) + (t0 & ((1 << p.z_log2) - 1)), scales = all_slots(p) * D + slot0;
   const int64_t row0 = ((int64_t)b * count + first_row) * p.Hkv + head;
-  const uint8_t* const k_pool = static_cast<const uint8_t*>(p.k_pool);
-  const uint8_t* const v_pool = static_cast<const uint8_t*>(p.v_pool);
-  u32x4 k[UNITS], v[UNITS];
-  if (k_out) {
+  const uint8_t* const pool = static_cast<const uint8_t*>(value ? p.v_pool : p.k_pool);
+  uint16_t* const out = value ? v_out : k_out;
+  const int part = tid % PARTS, sg = tid / PARTS;
+  uint32_t scale[4] = {};  // of the block's slots
+  if (out) {
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) k[u] = *reinterpret_cast<const u32x4*>(k_pool + slot0 * D + u * 1024 + lane * 16);
-  }
-  if (v_out) {
+    for (int u = 0; u < 32 * D / (16 * HALF); ++u) {
+      const int at = (u * HALF + tid) * 16;
+      *reinterpret_cast<u32x4*>(image + in_lds(at)) = *reinterpret_cast<const u32x4*>(pool + slot0 * D + at);
+    }
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) v[u] = *reinterpret_cast<const u32x4*>(v_pool + slot0 * D + u * 1024 + lane * 16);
+    for (int i = 0; i < 4; ++i) scale[i] = pool[scales + (value ? scale_off_v(4 * sg + i) : scale_off_k(4 * sg + i))];
   }
-  auto piece_out = [&](uint16_t* out, int sg, int part, int i, uint32_t a, uint32_t z, float scale) {
+  __syncthreads();
+  if (!out) return;
+  uint32_t codes[2][4];
+  if (value) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) codes[q][e] = *reinterpret_cast<const uint32_t*>(image + in_lds(value_piece<D>(sg, part, 4 * q + e)));
+      turn4(codes[q]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint2 piece = *reinterpret_cast<const uint2*>(image + in_lds(key_piece<D>(sg, part, i)));
+      codes[0][i] = piece.x;
+      codes[1][i] = piece.y;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
     const int slot = 4 * sg + i;
-    if (slot < lo || slot >= hi) return;
-    const u32x4 o = {values_of(a, false, scale), values_of(a, true, scale), values_of(z, false, scale), values_of(z, true, scale)};
+    if (slot < lo || slot >= hi) continue;
+    const float s = scale_of(scale[i]);
+    const uint32_t a = codes[0][i], z = codes[1][i];
+    const u32x4 o = {values_of(a, false, s), values_of(a, true, s), values_of(z, false, s), values_of(z, true, s)};
     *reinterpret_cast<u32x4*>(out + (row0 + (int64_t)slot * p.Hkv) * D + 8 * part) = o;
-  };
-  if (k_out) {
-#pragma unroll
-    for (int u = 0; u < UNITS; ++u) *reinterpret_cast<u32x4*>(image + in_lds(u * 1024 + lane * 16)) = k[u];
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) {
-      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint2 x = *reinterpret_cast<const uint2*>(image + in_lds(key_piece<D>(sg, part, i)));
-        piece_out(k_out, sg, part, i, x.x, x.y, scale_of(k_pool[scales + scale_off_k(4 * sg + i)]));
-      }
-    }
-    __syncthreads();
-  }
-  if (v_out) {
-#pragma unroll
-    for (int u = 0; u < UNITS; ++u) *reinterpret_cast<u32x4*>(image + in_lds(u * 1024 + lane * 16)) = v[u];
-    __syncthreads();
-#pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) {
-      const int part = (lane + 64 * n) % PARTS, sg = (lane + 64 * n) / PARTS;
-      uint32_t x[2][4];  // of dim k, slots 0..3; turned: of slot i, dims 0..3 and 4..7
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[q][e] = *reinterpret_cast<const uint32_t*>(image + in_lds(value_piece<D>(sg, part, 4 * q + e)));
-        turn4(x[q]);
-      }
-      const uint32_t s4 = *reinterpret_cast<const uint32_t*>(v_pool + scales + scale_off_v(4 * sg));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) piece_out(v_out, sg, part, i, x[0][i], x[1][i], scale_of((s4 >> (8 * i)) & 0xFFu));
-    }
   }
 }
 
@@ -359,8 +313,8 @@ hipError_t launch_append_e4m3(const StoreParams& p, const void* k_new, const voi
   const int64_t ring_slots = p.tile_mask == INT32_MAX ? INT64_MAX : ((int64_t)p.tile_mask + 1) << p.z_log2;
   if (!p.t_per_seq && past_whole > first_whole && (int64_t)groups * 32 <= ring_slots) {
     const dim3 grid(groups, p.Hkv, p.batch);
-    if (D == 128) return launch(kv_append_groups_e4m3<128>, grid, dim3(64), 0, stream, p, k, v);
-    return launch(kv_append_groups_e4m3<64>, grid, dim3(64), 0, stream, p, k, v);
+    if (D == 128) return launch(kv_append_groups_e4m3<128>, grid, dim3(256), 0, stream, p, k, v);
+    return launch(kv_append_groups_e4m3<64>, grid, dim3(128), 0, stream, p, k, v);
   }
   const int64_t threads = (int64_t)p.batch * p.count * p.Hkv * (D / 4);
   const dim3 grid((unsigned)((threads + 255) / 256));
@@ -373,8 +327,8 @@ hipError_t launch_gather_e4m3(const StoreParams& p, void* k_out, void* v_out, in
   const dim3 grid((unsigned)((int)(((int64_t)j0 + count - 1) >> 5) - (j0 >> 5) + 1), (unsigned)p.Hkv, (unsigned)p.batch);
   uint16_t* k = static_cast<uint16_t*>(k_out);
   uint16_t* v = static_cast<uint16_t*>(v_out);
-  if (D == 128) return launch(kv_gather_e4m3<128>, grid, dim3(64), 0, stream, p, k, v, j0, count);
-  return launch(kv_gather_e4m3<64>, grid, dim3(64), 0, stream, p, k, v, j0, count);
+  if (D == 128) return launch(kv_gather_e4m3<128>, grid, dim3(256), 0, stream, p, k, v, j0, count);
+  return launch(kv_gather_e4m3<64>, grid, dim3(128), 0, stream, p, k, v, j0, count);
 }
 
 }  // namespace tempo
