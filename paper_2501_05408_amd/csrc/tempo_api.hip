@@ -185,6 +185,44 @@ double plan_cost_ns(int64_t pairs, int64_t splits, int64_t keys_per_split, int b
          (splits > 8 && pairs >= kManyPairs ? kCombineManyNs : splits > 1 ? kCombineNs : 0.0);
 }
 
+// The same for 8-bit stores, whose kernel has 4 wavefronts' registers on a SIMD: more workgroups share a unit, so a further
+// round costs less, and a workgroup's own stream, half the bytes a key, is slower.  Fitted to 1020 measured shapes (1 to 64
+// sequences, 150 to 65536 keys, half of them ragged, a third with windows): 1.4% from the fastest plan on the mean for uniform
+// steps, 3.0% for ragged ones, 35% at most; bf16's constants 2.1% and 6.5%, 69%.
+// Ragged: splits of at most 2048 keys, the bytes of bf16's 1024; windows of up to 4096 keys, all of which end near their own
+// step, in as long ones as fit (48 sequences of 32/8 heads of 64 at steps up to 8191, window 1000: 2 splits 15.3 us, 1 11.1).
+// In a ragged batch of up to 8 sequences a third of the workgroups are taken to exist (3.5% from the fastest plan on the mean for
+// 2 and 3 sequences, all of them 5.2%); of more sequences the longest ones decide.
+void make_plan_e4m3(const tempo_kv* kv, int32_t batch, int32_t t_max, int32_t window, bool ragged, int64_t max_splits, tempo_plan* plan) {
+  constexpr double kBytesPerNs = 6700.0, kUnit = 31.0, kRound = 400.0, kFew = 4000.0, kMany = 4500.0, kWhole = 0.3;
+  const int64_t len = (window > 0 && window < (int64_t)t_max + 1) ? window : (int64_t)t_max + 1;
+  const int k_max = ragged && !(window > 0 && window <= 4096) ? 11 : 30;
+  const int64_t pairs = (int64_t)batch * kv->num_kv_heads, expected = ragged && window == 0 && batch <= 8 ? (7 * pairs + 19) / 20 : pairs;
+  double costs[31], best = -1.0;
+  int last = 5;
+  for (int k = 5; k <= k_max; ++k) {
+    const int64_t splits = splits_bound(t_max, window, k), per_split = ((int64_t)1 << k) < len ? (int64_t)1 << k : len;
+    const int64_t workgroups = expected * splits, busy = workgroups < kComputeUnits ? workgroups : kComputeUnits;
+    const double share = kBytesPerNs / (double)busy, rate = share < kUnit ? share : kUnit;
+    const int64_t whole = (workgroups + kComputeUnits - 1) / kComputeUnits;
+    const double rounds = whole == 1 ? 1.0 : kWhole * (double)whole + (1.0 - kWhole) * (double)workgroups / kComputeUnits;
+    costs[k] = kLaunchNs + rounds * (kRound + (double)per_split * 2 * kv->head_dim / rate) + (splits > 8 ? kMany : splits > 1 ? kFew : 0.0);
+    last = k;
+    if (splits <= max_splits && (best < 0.0 || costs[k] < best)) best = costs[k];
+    if (splits == 1) break;
+  }
+  int chosen = last;
+  while (splits_bound(t_max, window, chosen) > max_splits && chosen < 30) ++chosen;
+  for (int k = 5; k <= last; ++k) {  // the longest within 1% of the best
+    if (splits_bound(t_max, window, k) <= max_splits && costs[k] <= best * 1.01) chosen = k;
+  }
+  plan->tokens_per_split = 1 << chosen;
+  plan->num_splits = splits_bound(t_max, window, chosen);
+  const int64_t groups = plan->tokens_per_split / 32, held = plan->tokens_per_split < len ? groups : (len + 31) / 32;
+  if ((pairs * plan->num_splits <= kComputeUnits && groups >= 8) || (ragged && held >= 32)) plan->waves = 8;
+  else plan->waves = groups >= 4 ? 4 : (int32_t)groups;
+}
+
 // Ragged batches (per-sequence steps below t_max) hold less work than the model
 // assumes and it is unevenly spread, so their splits are capped at 1024 keys to
 // keep the long sequences from becoming single long-running workgroups.
@@ -197,15 +235,9 @@ void make_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int
                             ? (int64_t)batch * Hq
                             : (int64_t)batch * kv->num_kv_heads * (kv->dtype == TEMPO_F32 ? (columns + 15) / 16 : 1);
   const int64_t len = (window > 0 && window < (int64_t)t_max + 1) ? window : (int64_t)t_max + 1;
-  const bool k8 = kv->dtype == TEMPO_E4M3;
-  const int bytes_per_key = 2 * kv->head_dim * (kv->dtype == TEMPO_E4M3 ? 1 : kv->dtype == TEMPO_BF16 ? 2 : 4);  // K and V of one head
-  // (8 bits: the same bytes are twice the keys; and a window of so many is not cut at all, us a call for 48 sequences of
-  // 32/8 heads of 64 at steps up to 8191, window 1000: 2 splits of 1024 15.3, one 11.1; 64 of 24/8 heads of 128, causal, at
-  // steps up to 2000: 2 splits of 1024 30.6, one of 2048 27.6)
-  const int k_max = !ragged || (k8 && window > 0 && window <= 2048) ? 30 : k8 ? 11 : 10;
-  // (8 bits: half of a ragged batch's splits are taken to exist: 2 sequences of 32/4 heads of 128 at steps up to 55224
-  // 21.7 us with splits of 2048 keys, 13.9 of 1024)
-  const int64_t expected = ragged && k8 && window == 0 ? (pairs + 1) / 2 : pairs;
+  if (kv->dtype == TEMPO_E4M3) return make_plan_e4m3(kv, batch, t_max, window, ragged, max_splits, plan);
+  const int bytes_per_key = 2 * kv->head_dim * (kv->dtype == TEMPO_BF16 ? 2 : 4);  // K and V of one head
+  const int k_max = ragged ? 10 : 30;
   int best_k = -1;
   double best_cost = -1.0;
   double costs[26];
@@ -215,7 +247,7 @@ void make_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int
     if (splits > max_splits) continue;
     const int64_t tps = (int64_t)1 << k;
     const int64_t per_split = tps < len ? tps : len;  // a split never holds more than the range
-    costs[k - 5] = plan_cost_ns(expected, splits, per_split, bytes_per_key);
+    costs[k - 5] = plan_cost_ns(pairs, splits, per_split, bytes_per_key);
     if (best_cost < 0.0 || costs[k - 5] < best_cost) best_cost = costs[k - 5];
     if (splits == 1) break;  // longer splits change nothing
   }
@@ -834,9 +866,9 @@ int tempo_decode_step_causal_noalloc(const tempo_kv* kv, const void* q, const vo
   int64_t max_splits = kMaxSplits;
   tempo_plan plan;
   make_block_plan(kv, batch, num_q_heads, t, 0, t_per_seq != nullptr, 1, &plan, max_splits);
-  // (fp32, and the kernels for bf16 groups of more than 16 heads, want more splits than fit there
+  // (fp32, 8 bits, and the kernels for bf16 groups of more than 16 heads, want more splits than fit there
   // for many heads and long ranges: then the best plan that fits)
-  if (plan_bytes(kv, rows, plan.num_splits) > kScratchBytes && (kv->dtype == TEMPO_F32 || num_q_heads / kv->num_kv_heads > kNarrowColumns)) {
+  if (plan_bytes(kv, rows, plan.num_splits) > kScratchBytes && (kv->dtype != TEMPO_BF16 || num_q_heads / kv->num_kv_heads > kNarrowColumns)) {
     while (max_splits > 1 && plan_bytes(kv, rows, (int32_t)max_splits) > kScratchBytes) --max_splits;
     make_block_plan(kv, batch, num_q_heads, t, 0, t_per_seq != nullptr, 1, &plan, max_splits);
   }
