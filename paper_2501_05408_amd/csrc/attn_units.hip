@@ -12,8 +12,8 @@
 //   Lists (kSelect).  The positions of a split run over the blocks of a list, [batch][Hkv][pick] block numbers, not over
 //     the sequence: position v is slot v mod Z of block list[v div Z].  Entries that name no block at or before the
 //     step's are passed over.
-// More than 16 (step, head) columns: further workgroups along grid.x take the next 16 over the same keys, next to
-// each other in dispatch order, so that all but one of them read from a die's L2.
+// More than 16 (step, head) columns: a wavefront takes 32 (8-bit stores), further workgroups along grid.x the next ones over
+// the same keys, next to each other in dispatch order, so that all but one of them read from a die's L2.
 #include "attn_bf16_common.h"
 #include "attn_units.h"
 #include "store_e4m3.h"
@@ -56,32 +56,42 @@ __device__ __forceinline__ bf16x8 operand_of(uint32_t a, uint32_t b, float scale
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// Logits of the group's two row tiles, in base-2 units.
-template <int D, bool k8>
-__device__ __forceinline__ void image_logits(const AttnParams& p, const u32x4* qreg, const Image<D, k8>& g, float* x) {
+// Logits of the group's two row tiles for CT tiles of 16 columns, in base-2 units.
+template <int D, bool k8, int CT>
+__device__ __forceinline__ void image_logits(const AttnParams& p, const u32x4 (*qreg)[D / 32], const Image<D, k8>& g, float (*x)[8]) {
   constexpr int KS = D / 32;
-  f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = {0.f, 0.f, 0.f, 0.f};
+  f32x4 sa[CT], sb[CT];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) sa[ct] = sb[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float ka = 1.f, kb = 1.f;
   if constexpr (k8) {
-    const float ka = scale_of(g.k_scales & 0xFFu), kb = scale_of(g.k_scales >> 8);
+    ka = scale_of(g.k_scales & 0xFFu);
+    kb = scale_of(g.k_scales >> 8);
+  }
 #pragma unroll
-    for (int w = 0; w < KS / 2; ++w) {
-      const u32x4 a = g.k[w], b = g.k[KS / 2 + w];
-      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(a.x, a.y, ka), as_bf16x8(qreg[2 * w]), sa, 0, 0, 0);
-      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(b.x, b.y, kb), as_bf16x8(qreg[2 * w]), sb, 0, 0, 0);
-      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(a.z, a.w, ka), as_bf16x8(qreg[2 * w + 1]), sa, 0, 0, 0);
-      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(b.z, b.w, kb), as_bf16x8(qreg[2 * w + 1]), sb, 0, 0, 0);
+  for (int s = 0; s < KS; ++s) {
+    bf16x8 a, b;
+    if constexpr (k8) {
+      const u32x4 u = g.k[s / 2], v = g.k[KS / 2 + s / 2];
+      a = s & 1 ? operand_of(u.z, u.w, ka) : operand_of(u.x, u.y, ka);
+      b = s & 1 ? operand_of(v.z, v.w, kb) : operand_of(v.x, v.y, kb);
+    } else {
+      a = as_bf16x8(g.k[s]);
+      b = as_bf16x8(g.k[KS + s]);
     }
-  } else {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      sa = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(g.k[s]), as_bf16x8(qreg[s]), sa, 0, 0, 0);
-      sb = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(g.k[KS + s]), as_bf16x8(qreg[s]), sb, 0, 0, 0);
+    for (int ct = 0; ct < CT; ++ct) {
+      sa[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, as_bf16x8(qreg[ct][s]), sa[ct], 0, 0, 0);
+      sb[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, as_bf16x8(qreg[ct][s]), sb[ct], 0, 0, 0);
     }
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    x[r] = sa[r] * p.scale_log2e;
-    x[4 + r] = sb[r] * p.scale_log2e;
+  for (int ct = 0; ct < CT; ++ct) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      x[ct][r] = sa[ct][r] * p.scale_log2e;
+      x[ct][4 + r] = sb[ct][r] * p.scale_log2e;
+    }
   }
 }
 
@@ -228,14 +238,15 @@ __device__ __forceinline__ void merge_units(const AttnParams& p, const float* sm
   }
 }
 
-template <int D, bool k8, bool kSelect, bool kRope>
+// CT: tiles of 16 columns that a wavefront takes, over the same operands.
+template <int D, bool k8, bool kSelect, bool kRope, int CT>
 __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
   constexpr int KS = D / 32, DT = D / 16;
   extern __shared__ float smem[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nwaves = blockDim.x >> 6;
-  const int hkv = (int)(blockIdx.x % (unsigned)p.Hkv), first_col = 16 * (int)(blockIdx.x / (unsigned)p.Hkv);
+  const int hkv = (int)(blockIdx.x % (unsigned)p.Hkv), first_col = 16 * CT * (int)(blockIdx.x / (unsigned)p.Hkv);
   const int b = blockIdx.y;
   int t_b = p.t_per_seq ? ((const_i32_ptr)p.t_per_seq)[b] : p.t;
   t_b = t_b > p.t ? p.t : (t_b < 0 ? 0 : t_b);
@@ -290,35 +301,36 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
   }
 
   // Columns and their ranges, as in attn_partial_bf16.hip.
-  const int all_cols = p.queries * p.G - first_col, ncols = all_cols < 16 ? all_cols : 16;
+  const int all_cols = p.queries * p.G - first_col;  // from this workgroup's first on
   const int t_end = t_b + p.queries - 1;
   const int lo_last = (p.window > 0 && t_end - p.window + 1 > 0) ? t_end - p.window + 1 : 0;
   const int all_lo = lo_last > from ? lo_last : from;
   const int all_hi = t_b < upto ? t_b : upto;
   const int seen_hi = t_end < upto ? t_end : upto;
-  const int col = lane & 15;
-  const int cq = col < ncols ? (first_col + col) / p.G : p.queries - 1;
-  const int gq = col < ncols ? first_col + col - cq * p.G : 0;
-  const int hi_col = (t_b + cq) < upto ? (t_b + cq) : upto;
-  const int lo_q = (p.window > 0 && t_b + cq - p.window + 1 > 0) ? t_b + cq - p.window + 1 : 0;
-  const int lo_col = lo_q > from ? lo_q : from;
-  u32x4 qreg[KS];
-  {
-    const int c = lane >> 4;
+  int lo_col[CT], hi_col[CT];
+  u32x4 qreg[CT][KS];
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const int col = 16 * ct + (lane & 15);
+    const int cq = col < all_cols ? (first_col + col) / p.G : p.queries - 1;
+    const int gq = col < all_cols ? first_col + col - cq * p.G : 0;
+    hi_col[ct] = (t_b + cq) < upto ? (t_b + cq) : upto;
+    const int lo_q = (p.window > 0 && t_b + cq - p.window + 1 > 0) ? t_b + cq - p.window + 1 : 0;
+    lo_col[ct] = lo_q > from ? lo_q : from;
     const uint16_t* qp = static_cast<const uint16_t*>(p.q) +
-                         (((int64_t)b * p.io_steps + cq) * p.Hq + (int64_t)hkv * p.G + gq) * D + 8 * c;
+                         (((int64_t)b * p.io_steps + cq) * p.Hq + (int64_t)hkv * p.G + gq) * D + 8 * (lane >> 4);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const u32x4 zero = {0u, 0u, 0u, 0u};
       const u32x4 v = *reinterpret_cast<const u32x4*>(qp + 32 * s);
-      qreg[s] = col < ncols ? v : zero;
+      qreg[ct][s] = col < all_cols ? v : zero;
     }
+    if (kRope) rotate_query<D>(p, t_b + cq, lane, qreg[ct]);
   }
-  if (kRope) rotate_query<D>(p, t_b + cq, lane, qreg);
 
   // A fused write lands in group t_b >> 5, which only the newest split holds.
   int key_new = -1;  // first key of that group, in the wavefront that will reach it
-  uint8_t* const stage = reinterpret_cast<uint8_t*>(smem + nwaves * (32 + ncols * D));
+  uint8_t* const stage = reinterpret_cast<uint8_t*>(smem + nwaves * (32 + (all_cols < 16 ? all_cols : 16) * D));
   if constexpr (k8 && !kSelect) {
     const int grp_new = t_b >> 5;
     if (p.k_new && blockIdx.z == 0 && grp_new >= grp && (grp_new - grp) % nwaves == 0) {
@@ -328,11 +340,14 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
     }
   }
 
-  WaveState<D> st;
-  st.m = -INFINITY;
-  st.l = 0.f;
+  WaveState<D> st[CT];
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) st.acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int ct = 0; ct < CT; ++ct) {
+    st[ct].m = -INFINITY;
+    st[ct].l = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) st[ct].acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
   // The group in the registers; `more`: and request the one whose first key is key_nxt.
   auto group = [&](int key_nxt, bool more) __attribute__((always_inline)) {
@@ -340,36 +355,41 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
     if constexpr (k8 && !kSelect) {
       if (key == key_new) patch_keys<D>(t_b, lane, stage, g);
     }
-    float x[8];
-    image_logits<D, k8>(p, qreg, g, x);
+    float x[CT][8];
+    image_logits<D, k8, CT>(p, qreg, g, x);
     if (more) load_image_keys<D, k8>(p, slot_nxt, slots, lane, g);
     // Slots that no step of the call sees may be unwritten: codes and scales of 0, bf16 values of 0, under the weight of 0.
     uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};               // bf16 values: masks of the lane's 8 slots
     uint2 keep8 = {~0u, ~0u};                              // codes
     if (key < all_lo || key > all_hi - 31) {               // wave-uniform: a group that some column's range cuts
-      mask_logits(key >> 5, lo_col, hi_col, lane, x);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) mask_logits(key >> 5, lo_col[ct], hi_col[ct], lane, x[ct]);
       if constexpr (k8) keep8 = seen_bytes(key, from, seen_hi, lane);
       else value_masks(key >> 5, from, seen_hi, lane, keep);
     }
-    bf16x8 pa = softmax_update<D>(x, lane, st);
+    bf16x8 pa[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) pa[ct] = softmax_update<D>(x[ct], lane, st[ct]);
     if constexpr (k8 && !kSelect) {
       if (key == key_new) patch_values<D>(t_b, lane, stage, g);
     }
     if constexpr (k8) {
-      pa = scaled_weights(pa, uint2{g.v_scales.x & keep8.x, g.v_scales.y & keep8.y});
 #pragma unroll
-      for (int w = 0; w < DT / 2; ++w) {
-        const u32x4 v = g.v[w];
-        st.acc[2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, operand_of(v.x & keep8.x, v.y & keep8.y, 1.f), st.acc[2 * w], 0, 0, 0);
-        st.acc[2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, operand_of(v.z & keep8.x, v.w & keep8.y, 1.f), st.acc[2 * w + 1], 0, 0, 0);
-      }
-    } else {
+      for (int ct = 0; ct < CT; ++ct) pa[ct] = scaled_weights(pa[ct], uint2{g.v_scales.x & keep8.x, g.v_scales.y & keep8.y});
+    }
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        u32x4 v = g.v[dt];
-        v.x &= keep[0]; v.y &= keep[1]; v.z &= keep[2]; v.w &= keep[3];
-        st.acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, as_bf16x8(v), st.acc[dt], 0, 0, 0);
+    for (int dt = 0; dt < DT; ++dt) {
+      bf16x8 v;
+      if constexpr (k8) {
+        const u32x4 u = g.v[dt / 2];
+        v = dt & 1 ? operand_of(u.z & keep8.x, u.w & keep8.y, 1.f) : operand_of(u.x & keep8.x, u.y & keep8.y, 1.f);
+      } else {
+        u32x4 u = g.v[dt];
+        u.x &= keep[0]; u.y &= keep[1]; u.z &= keep[2]; u.w &= keep[3];
+        v = as_bf16x8(u);
       }
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) st[ct].acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[ct], v, st[ct].acc[dt], 0, 0, 0);
     }
     if (more) load_image_values<D, k8>(p, slot_nxt, slots, lane, g);
   };
@@ -387,39 +407,54 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
     group(0, false);
   }
 
-  const float l_tot = column_sum(st.l);
-  float* sm_m = smem;                  // [nwaves][16]
-  float* sm_l = smem + nwaves * 16;    // [nwaves][16]
-  float* sm_acc = smem + nwaves * 32;  // [nwaves][ncols][D]
-  if (lane < 16) {
-    sm_m[wave * 16 + lane] = st.m;
-    sm_l[wave * 16 + lane] = l_tot;
-  }
-  {
-    const int n = lane & 15, c = lane >> 4;
+  // The wavefronts' results are merged a tile of columns at a time.
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int j = 4 * c + r;
-      if (j < ncols) {
+  for (int ct = 0; ct < CT; ++ct) {
+    const int tile_cols = all_cols - 16 * ct, ncols = tile_cols < 16 ? tile_cols : 16;
+    if (ncols <= 0) break;       // uniform over the workgroup
+    if (ct > 0) __syncthreads();
+    const float l_tot = column_sum(st[ct].l);
+    float* sm_m = smem;                  // [nwaves][16]
+    float* sm_l = smem + nwaves * 16;    // [nwaves][16]
+    float* sm_acc = smem + nwaves * 32;  // [nwaves][ncols][D]
+    if (lane < 16) {
+      sm_m[wave * 16 + lane] = st[ct].m;
+      sm_l[wave * 16 + lane] = l_tot;
+    }
+    {
+      const int n = lane & 15, c = lane >> 4;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) sm_acc[(wave * ncols + j) * D + 16 * dt + n] = st.acc[dt][r];
+      for (int r = 0; r < 4; ++r) {
+        const int j = 4 * c + r;
+        if (j < ncols) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) sm_acc[(wave * ncols + j) * D + 16 * dt + n] = st[ct].acc[dt][r];
+        }
       }
     }
+    __syncthreads();
+    const int first = first_col + 16 * ct;
+    if (nwaves == 8) merge_units<D, 8, kSelect>(p, smem, first, ncols, b, hkv, split);
+    else if (nwaves == 4) merge_units<D, 4, kSelect>(p, smem, first, ncols, b, hkv, split);
+    else if (nwaves == 2) merge_units<D, 2, kSelect>(p, smem, first, ncols, b, hkv, split);
+    else merge_units<D, 1, kSelect>(p, smem, first, ncols, b, hkv, split);
   }
-  __syncthreads();
-  if (nwaves == 8) merge_units<D, 8, kSelect>(p, smem, first_col, ncols, b, hkv, split);
-  else if (nwaves == 4) merge_units<D, 4, kSelect>(p, smem, first_col, ncols, b, hkv, split);
-  else if (nwaves == 2) merge_units<D, 2, kSelect>(p, smem, first_col, ncols, b, hkv, split);
-  else merge_units<D, 1, kSelect>(p, smem, first_col, ncols, b, hkv, split);
 }
 
+template <bool k8, bool kSelect, bool kRope, int CT>
+hipError_t launch_tiles(const SelectParams& p, int batch, int D, int grid_splits, int waves, hipStream_t stream) {
+  const int columns = p.queries * p.G;
+  const dim3 grid((unsigned)(p.Hkv * ((columns + 16 * CT - 1) / (16 * CT))), (unsigned)batch, (unsigned)grid_splits), block(64 * waves);
+  const size_t lds = units_lds_bytes(waves, columns, D);
+  if (D == 128) return launch((attn_units<128, k8, kSelect, kRope, CT>), grid, block, lds, stream, p);
+  return launch((attn_units<64, k8, kSelect, kRope, CT>), grid, block, lds, stream, p);
+}
+
+// More than 16 columns: 8-bit operands are turned into bf16 once for two tiles.
 template <bool k8, bool kSelect, bool kRope>
 hipError_t launch_units(const SelectParams& p, int batch, int D, int grid_splits, int waves, hipStream_t stream) {
-  const int columns = p.queries * p.G;
-  const dim3 grid((unsigned)(p.Hkv * ((columns + 15) / 16)), (unsigned)batch, (unsigned)grid_splits), block(64 * waves);
-  const size_t lds = units_lds_bytes(waves, columns, D);
-  if (D == 128) return launch((attn_units<128, k8, kSelect, kRope>), grid, block, lds, stream, p);
-  return launch((attn_units<64, k8, kSelect, kRope>), grid, block, lds, stream, p);
+  if (k8 && p.queries * p.G > 16) return launch_tiles<k8, kSelect, kRope, k8 ? 2 : 1>(p, batch, D, grid_splits, waves, stream);
+  return launch_tiles<k8, kSelect, kRope, 1>(p, batch, D, grid_splits, waves, stream);
 }
 
 }  // namespace

@@ -193,8 +193,17 @@ double plan_cost_ns(int64_t pairs, int64_t splits, int64_t keys_per_split, int b
 // step, in as long ones as fit (48 sequences of 32/8 heads of 64 at steps up to 8191, window 1000: 2 splits 15.3 us, 1 11.1).
 // In a ragged batch of up to 8 sequences a third of the workgroups are taken to exist (3.5% from the fastest plan on the mean for
 // 2 and 3 sequences, all of them 5.2%); of more sequences the longest ones decide.
-void make_plan_e4m3(const tempo_kv* kv, int32_t batch, int32_t t_max, int32_t window, bool ragged, int64_t max_splits, tempo_plan* plan) {
-  constexpr double kBytesPerNs = 6700.0, kUnit = 31.0, kRound = 400.0, kFew = 4000.0, kMany = 4500.0, kWhole = 0.3;
+// More than 16 columns: a workgroup for every 32, which read a key from one die's cache up to 4 times; what a wavefront computes
+// may take longer than its stream, and the combine reads a partial per column.  Fitted to 500 shapes of 17 to 128 columns: 2.9%
+// from the fastest plan on the mean, 28% at most (without tiles, work and partials 16%, 150%).
+void make_plan_e4m3(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int32_t window, bool ragged, int32_t queries,
+                    int64_t max_splits, tempo_plan* plan) {
+  const int columns = queries * (Hq / kv->num_kv_heads), D = kv->head_dim;
+  const bool wide = columns > kNarrowColumns;
+  const int64_t tiles = wide ? (columns + 31) / 32 : 1;
+  const double kBytesPerNs = 6700.0 * (double)(tiles < 4 ? tiles : 4), kUnit = wide ? 20.0 : 31.0, kRound = wide ? 700.0 : 400.0;
+  const double kFew = 4000.0, kMany = wide ? 6000.0 : 4500.0, kWhole = wide ? 0.5 : 0.3, kNear = wide ? 1.02 : 1.01;
+  const double kGroup = wide ? (D == 128 ? 1600.0 : 800.0) : 0.0, kPartial = wide ? 2.0 * batch * queries * Hq * D * 4 / 4800.0 : 0.0;
   const int64_t len = (window > 0 && window < (int64_t)t_max + 1) ? window : (int64_t)t_max + 1;
   const int k_max = ragged && !(window > 0 && window <= 4096) ? 11 : 30;
   const int64_t pairs = (int64_t)batch * kv->num_kv_heads, expected = ragged && window == 0 && batch <= 8 ? (7 * pairs + 19) / 20 : pairs;
@@ -202,25 +211,27 @@ void make_plan_e4m3(const tempo_kv* kv, int32_t batch, int32_t t_max, int32_t wi
   int last = 5;
   for (int k = 5; k <= k_max; ++k) {
     const int64_t splits = splits_bound(t_max, window, k), per_split = ((int64_t)1 << k) < len ? (int64_t)1 << k : len;
-    const int64_t workgroups = expected * splits, busy = workgroups < kComputeUnits ? workgroups : kComputeUnits;
+    const int64_t workgroups = expected * splits * tiles, busy = workgroups < kComputeUnits ? workgroups : kComputeUnits;
     const double share = kBytesPerNs / (double)busy, rate = share < kUnit ? share : kUnit;
+    const double stream = (double)per_split * 2 * D / rate, work = (double)((per_split + 255) / 256) * kGroup;
     const int64_t whole = (workgroups + kComputeUnits - 1) / kComputeUnits;
     const double rounds = whole == 1 ? 1.0 : kWhole * (double)whole + (1.0 - kWhole) * (double)workgroups / kComputeUnits;
-    costs[k] = kLaunchNs + rounds * (kRound + (double)per_split * 2 * kv->head_dim / rate) + (splits > 8 ? kMany : splits > 1 ? kFew : 0.0);
+    costs[k] = (wide ? 1000.0 : kLaunchNs) + rounds * (kRound + (stream > work ? stream : work));
+    if (splits > 1) costs[k] += (splits > 8 ? kMany : kFew) + kPartial * (double)splits;
     last = k;
     if (splits <= max_splits && (best < 0.0 || costs[k] < best)) best = costs[k];
     if (splits == 1) break;
   }
   int chosen = last;
   while (splits_bound(t_max, window, chosen) > max_splits && chosen < 30) ++chosen;
-  for (int k = 5; k <= last; ++k) {  // the longest within 1% of the best
-    if (splits_bound(t_max, window, k) <= max_splits && costs[k] <= best * 1.01) chosen = k;
+  for (int k = 5; k <= last; ++k) {  // the longest within 1 or 2% of the best
+    if (splits_bound(t_max, window, k) <= max_splits && costs[k] <= best * kNear) chosen = k;
   }
   plan->tokens_per_split = 1 << chosen;
   plan->num_splits = splits_bound(t_max, window, chosen);
   const int64_t groups = plan->tokens_per_split / 32, held = plan->tokens_per_split < len ? groups : (len + 31) / 32;
-  if ((pairs * plan->num_splits <= kComputeUnits && groups >= 8) || (ragged && held >= 32)) plan->waves = 8;
-  else plan->waves = groups >= 4 ? 4 : (int32_t)groups;
+  const bool eight = wide ? held >= 64 : (pairs * plan->num_splits <= kComputeUnits && groups >= 8) || (ragged && held >= 32);
+  plan->waves = eight ? 8 : groups >= 4 ? 4 : (int32_t)groups;
 }
 
 // Ragged batches (per-sequence steps below t_max) hold less work than the model
@@ -235,7 +246,7 @@ void make_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int
                             ? (int64_t)batch * Hq
                             : (int64_t)batch * kv->num_kv_heads * (kv->dtype == TEMPO_F32 ? (columns + 15) / 16 : 1);
   const int64_t len = (window > 0 && window < (int64_t)t_max + 1) ? window : (int64_t)t_max + 1;
-  if (kv->dtype == TEMPO_E4M3) return make_plan_e4m3(kv, batch, t_max, window, ragged, max_splits, plan);
+  if (kv->dtype == TEMPO_E4M3) return make_plan_e4m3(kv, batch, Hq, t_max, window, ragged, queries, max_splits, plan);
   const int bytes_per_key = 2 * kv->head_dim * (kv->dtype == TEMPO_BF16 ? 2 : 4);  // K and V of one head
   const int k_max = ragged ? 10 : 30;
   int best_k = -1;
@@ -340,6 +351,7 @@ size_t plan_bytes(const tempo_kv* kv, int64_t rows, int32_t S) {
 // The decode kernel's wave-merge area: a limit of its launch.  (The fp32 kernel asks for up to 68,608
 // bytes, the prompt kernel for up to 128 KiB, of the 160 KiB a compute unit has.)
 constexpr size_t kMaxLds = 64 * 1024;
+constexpr size_t kMaxUnitsLds = 72 * 1024;  // of attn_units.hip: 8 wavefronts of 16 columns of 128; two workgroups to a unit
 
 AttnParams attn_params(const tempo_kv* kv, const void* q, void* out, int32_t Hq, int32_t t,
                        const int32_t* t_per_seq, int32_t window, float scale,
@@ -429,7 +441,7 @@ int check_attn(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, int32_t
     // more than 16 columns go to the kernels for wide blocks, whose launch shapes are fixed
     if (columns <= kNarrowColumns && partial_bf16_lds_bytes(plan->waves, columns, kv->head_dim) > kMaxLds) return TEMPO_ERR_SHAPE;
   }
-  if (kv->dtype == TEMPO_E4M3 && units_lds_bytes(plan->waves, queries * (Hq / kv->num_kv_heads), kv->head_dim) > kMaxLds) return TEMPO_ERR_SHAPE;
+  if (kv->dtype == TEMPO_E4M3 && units_lds_bytes(plan->waves, queries * (Hq / kv->num_kv_heads), kv->head_dim) > kMaxUnitsLds) return TEMPO_ERR_SHAPE;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
   if (workspace_bytes < plan_bytes(kv, (int64_t)batch * queries * Hq, plan->num_splits)) return TEMPO_ERR_WORKSPACE;
   return TEMPO_OK;
@@ -532,7 +544,7 @@ void make_block_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, i
   make_plan(kv, batch, Hq, last_step(t, queries), union_window(window, queries), ragged, queries, max_splits, plan);
   const int columns = queries * (Hq / kv->num_kv_heads);
   if (kv->dtype == TEMPO_E4M3) {
-    while (plan->waves > 1 && units_lds_bytes(plan->waves, columns, kv->head_dim) > kMaxLds) plan->waves /= 2;
+    while (plan->waves > 1 && units_lds_bytes(plan->waves, columns, kv->head_dim) > kMaxUnitsLds) plan->waves /= 2;
     return;
   }
   if (kv->dtype != TEMPO_BF16) return;
@@ -1854,7 +1866,7 @@ static void selected_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t
   while (splits_bound(count * kv->block_size - 1, 0, longer) > kMaxSplits) ++longer;
   plan->tokens_per_split = 1 << longer;
   plan->num_splits = splits_bound(count * kv->block_size - 1, 0, longer);
-  while (plan->waves > 1 && units_lds_bytes(plan->waves, Hq / kv->num_kv_heads, kv->head_dim) > kMaxLds) plan->waves /= 2;
+  while (plan->waves > 1 && units_lds_bytes(plan->waves, Hq / kv->num_kv_heads, kv->head_dim) > kMaxUnitsLds) plan->waves /= 2;
 }
 
 // For any step: as tempo_attn_workspace_bytes, of a step of so many keys.
