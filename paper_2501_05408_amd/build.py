@@ -71,6 +71,7 @@ MIN_OCCUPANCY = [
     ("attn_partial_bf16ILi128E", 3),           # decode kernel, D = 128: <= 170 VGPRs
     ("attn_block_bf16ILi128ELi8E", 4),         # LDS-staged block kernel, D = 128: two workgroups of 8 per compute unit
     ("attn_stream_bf16ILi128E", 2),            # stream kernel, D = 128: one workgroup of 8 wavefronts per compute unit
+    ("attn_unitsILi128ELb1ELb0ELb0ELi1E", 3),  # 8-bit decode kernel, D = 128: its plans expect three wavefronts to a SIMD
     ("attn_prefill_bf16ILi128E", 2),           # prompt kernel, D = 128: two wavefronts of 32 columns per SIMD
 ]
 

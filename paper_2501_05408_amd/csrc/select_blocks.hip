@@ -218,6 +218,7 @@ __device__ __forceinline__ void write_and_bound(const StoreParams& p, const void
 // Blocks whose interval leaves it open whether they are chosen are scored again, in 64 bits (exact_key), by the kernel that
 // chooses: one or two of hundreds.  All of them in 64 bits took 11.7 us for 16 sequences of 512 blocks and 24 heads of 128.
 constexpr float kOff = 1.0625f / 16384.f;
+constexpr float kLeast = 1e-30f;  // (products below the normal fp32 range)
 
 struct Interval {
   float lo, hi;
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(256) void score_blocks(ChooseParams p, StoreParams 
     // lane (column + 16c): blocks n0 + 4c .. +3 for head g0 + column
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const float off = size[r] * kOff, l = sum[r] - off, u = sum[r] + off;
+      const float off = fmaf(size[r], kOff, kLeast), l = sum[r] - off, u = sum[r] + off;
       const bool fine = u - l < INFINITY;  // false too where NaN or infinite: left to exact_key
       low[r] = g0 + row < p.G && fine ? fmaxf(low[r], l) : low[r];
       high[r] = g0 + row < p.G ? (fine ? fmaxf(high[r], u) : INFINITY) : high[r];

@@ -227,9 +227,11 @@ class BlockStore:
     def _selected_ws(self, nbytes):
         if nbytes == 0:
             raise T.TempoError(T.TEMPO_ERR_SHAPE, "workspace of the attention over selected blocks")
-        if getattr(self, "_sel_ws", None) is None or self._sel_ws.numel() < nbytes:
-            self._sel_ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        return self._sel_ws, self._sel_ws.numel()
+        if getattr(self, "_sel_ws", None) is None or self._sel_ws[-1].numel() < nbytes:
+            # (smaller ones are kept: a captured graph may hold their address)
+            self._sel_ws = getattr(self, "_sel_ws", None) or []
+            self._sel_ws.append(torch.empty(nbytes, dtype=torch.uint8, device=self.device))
+        return self._sel_ws[-1], self._sel_ws[-1].numel()
 
     def select_blocks(self, bounds, q, t, count, first=1, last=1, t_per_seq=None, selected=None):
         """The `count` blocks that step t of every (sequence, kv head) attends over, int32 [batch][Hkv][count]."""

@@ -142,6 +142,36 @@ def test_written_rows_come_back_and_others_stay(D, Z, B, t, count, ragged):
         assert (~left[:codes]).sum() <= B * count * Hkv * D
 
 
+@pytest.mark.parametrize("t", [0, 1, 31, 40, 100])
+@pytest.mark.parametrize("count", [128, 127, 97, 64])
+def test_calls_that_fill_a_ring(t, count):
+    """From any step on, the last group's slots among the first group's."""
+    B, Hkv, D, Z, ring = 2, 2, 64, 64, 2
+    st = make_store(9, B, Hkv, Hkv, D, Z, 0, ring)
+    K, V = normal(9, 1, (B, count, Hkv, D)), normal(9, 2, (B, count, Hkv, D))
+    st.append_block(bf16(K), bf16(V), t, count)
+    k, v = st.gather(t, count)
+    np.testing.assert_array_equal(np64(k), held(K))
+    np.testing.assert_array_equal(np64(v), held(V))
+
+
+@pytest.mark.parametrize("D,Z", [(64, 32), (128, 256)])
+def test_offsets_beyond_32_bits(D, Z):
+    """The last blocks of pools of more than 2^32 bytes."""
+    Hq, Hkv, B, t = 6, 2, 1, 700
+    blocks = (1 << 32) // (Hkv * Z * D) + 40
+    pools = [torch.empty(blocks * Hkv * Z * (D + 1), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    table = torch.arange(blocks - 1, blocks - 1 - (t // Z + 1), -1, dtype=torch.int32).reshape(1, -1)
+    st = BlockStore(B, Hq, Hkv, D, Z, t, E4M3, device=DEV, num_blocks=blocks, block_table=table, pools=pools)
+    q, K, V = normal(10, 1, (B, Hq, D)), normal(10, 2, (B, t + 1, Hkv, D)), normal(10, 3, (B, t + 1, Hkv, D))
+    st.append_block(bf16(K[:, :t]), bf16(V[:, :t]), 0, t)
+    out = st.step_causal(bf16(q), bf16(K[:, t]), bf16(V[:, t]), st.new_out(), t)
+    k, v = st.gather(0, t + 1)
+    np.testing.assert_array_equal(np64(k), held(K))
+    np.testing.assert_array_equal(np64(v), held(V))
+    assert_attention(out, q, held(K), held(V), t, 0, st.scale, "far blocks")
+
+
 @pytest.mark.parametrize("ring,Z,start", [(2, 32, 100), (4, 64, 1000)])
 def test_ring_stores(ring, Z, start):
     B, Hq, Hkv, D = 2, 4, 2, 128
@@ -261,9 +291,9 @@ def test_fused_steps_are_the_write_and_the_attention(Hq, Hkv, D, B, t, ragged, w
         assert torch.equal(three, two) and torch.equal(a.k_pool, c.k_pool) and torch.equal(a.v_pool, c.v_pool)
 
 
-@pytest.mark.parametrize("D,window", [(64, 0), (128, 0), (128, 40)])
-def test_rotary_steps_and_blocks(D, window):
-    Hq, Hkv, Z, B, t, C = 6, 2, 64, 2, 150, 4
+@pytest.mark.parametrize("D,window,Hq,C", [(64, 0, 6, 4), (128, 0, 6, 4), (128, 40, 6, 4), (64, 0, 36, 7), (128, 33, 80, 3)])
+def test_rotary_steps_and_blocks(D, window, Hq, C):
+    Hkv, Z, B, t = 2, 64, 2, 150
     st, q, K, V, first, _ = filled(15, Hq, Hkv, D, Z, B, t, window, False, C)
     cos, sin = (torch.from_numpy(x.astype(np.float32)).to(DEV) for x in oracle.rope_table(t + C, D, 500000.0))
     st.set_rope(cos, sin)

@@ -199,6 +199,15 @@ def test_choice_of_nan_infinite_and_extreme_bounds():
         assert {0, 10, 90, blocks - 1} <= set(got[b, 0].tolist()) and (np.diff(got[b, 0]) > 0).all()
 
 
+@pytest.mark.parametrize("bound,query", [(2.0 ** -130, 1.0), (2.0 ** -130, 2.0 ** 100), (2.0 ** -70, 2.0 ** -75), (2.0 ** 60, 2.0 ** 60), (1.0, 2.0 ** -20)])
+def test_choice_at_the_ends_of_the_range(bound, query):
+    """Bounds that bf16 holds as subnormals, products that fp32 does, and large ones."""
+    st = make_store(35, T.TEMPO_BF16, 2, 6, 2, 64, 32, 32 * 300 - 1)
+    spread = normal(35, 7, (2, 6, 64))
+    bounds = (random_bounds(st, 35).double() * 4).round().clamp(-16, 16) * bound     # whole multiples: exact
+    assert_choice(st, bounds.to(torch.bfloat16), np64(bf16(spread)) * query, 32 * 300 - 1, None, 20, 1, 2)
+
+
 # ---- attention over lists ------------------------------------------------------------------------------
 
 def assert_attend(got, q, K, V, lists, Z, steps, scale, what):
@@ -285,6 +294,26 @@ def test_all_blocks_are_the_dense_attention(dtype):
     dense = np64(st.attend_causal(bf16(q), st.new_out(), t))
     size = oracle.attend(q, K, np.abs(V), t, 0, st.scale)
     assert (np.abs(np64(out) - dense) <= 2 * 1.03 * 2.0 ** -8 * (size + 2 * np.abs(dense))).all()
+
+
+def test_offsets_beyond_32_bits():
+    """The last blocks of a pool of more than 2^32 elements: bounds, choice, attention over a list, a whole step."""
+    Hq, Hkv, D, Z, B, t = 6, 2, 128, 256, 1, 2047
+    blocks = (1 << 32) // (Hkv * Z * D) + 40
+    pools = [torch.empty((blocks, Hkv, Z * D), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    table = torch.arange(blocks - 1, blocks - 1 - (t // Z + 1), -1, dtype=torch.int32).reshape(1, -1)
+    st = BlockStore(B, Hq, Hkv, D, Z, t, T.TEMPO_BF16, device=DEV, num_blocks=blocks, block_table=table, pools=pools)
+    q, K, V = normal(36, 1, (B, Hq, D)), normal(36, 2, (B, t + 1, Hkv, D)), normal(36, 3, (B, t + 1, Hkv, D))
+    st.append_block(bf16(K[:, :t]), bf16(V[:, :t]), 0, t)
+    bounds = st.new_bounds()
+    st.update_bounds(bounds, 0, t)
+    selected = torch.empty((B, Hkv, 5), dtype=torch.int32, device=DEV)
+    out = st.step_selected(bounds, bf16(q), bf16(K[:, t]), bf16(V[:, t]), st.new_out(), t, 5, selected=selected)
+    lists = selected.cpu().numpy()
+    for h in range(Hkv):
+        keys = K[0, :, h].reshape(-1, Z, D)
+        np.testing.assert_array_equal(lists[0, h], choose(q[0, 3 * h:3 * h + 3], keys.min(1), keys.max(1), t // Z, 5, 1, 1))
+    assert_attend(out, q, K, V, lists, Z, np.full(B, t), st.scale, "far blocks")
 
 
 # ---- together ---------------------------------------------------------------------------------------------
