@@ -39,7 +39,7 @@
  *  - The result never depends on pool contents outside the visible range (of a call
  *    that answers several steps: outside the union of their ranges): masking is by
  *    index (the paper's -inf mask under max, 0 mask under sums).  Inside that union a
- *    bf16 value that a step does not see is multiplied by a weight of 0, so one that is
+ *    bf16 or e4m3 value that a step does not see is multiplied by a weight of 0, so one that is
  *    not finite may show in steps of the call that do not see it (fp32: it does not).
  *
  * Supported shapes: head_dim in {64, 128}; block_size a power of two, >= 32

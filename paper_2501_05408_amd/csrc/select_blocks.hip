@@ -247,22 +247,25 @@ __global__ __launch_bounds__(256) void score_blocks(ChooseParams p, StoreParams 
   const int n = n0 + row <= newest - p.last ? n0 + row : n0;
   const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
   const uint16_t* const at = static_cast<const uint16_t*>(p.bounds) + ((int64_t)phys * p.Hkv + hkv) * 2 * D + 8 * c;
+  const uint16_t* const q = static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D + 8 * c;
+  u32x4 x[KS];  // of the first 16 heads; asked for before the bounds, which wait for the table (16 sequences of 512 blocks: 14.9 -> 14.5 us)
+#pragma unroll
+  for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const u32x4*>(q + (int64_t)(row < p.G ? row : p.G - 1) * D + 32 * s);
   u32x4 lo[KS], hi[KS], far[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
     lo[s] = *reinterpret_cast<const u32x4*>(at + 32 * s);
     hi[s] = *reinterpret_cast<const u32x4*>(at + D + 32 * s);
   }
-  const uint16_t* const q = static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D + 8 * c;
   float low[4], high[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) low[r] = high[r] = -INFINITY;
   for (int g0 = 0; g0 < p.G; g0 += 16) {
     const int g = g0 + row < p.G ? g0 + row : p.G - 1;
-    u32x4 x[KS];
+    if (g0 > 0) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const u32x4*>(q + (int64_t)g * D + 32 * s);
-    if (g0 == 0) {
+      for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const u32x4*>(q + (int64_t)g * D + 32 * s);
+    } else {
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
 #pragma unroll

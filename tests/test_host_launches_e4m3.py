@@ -130,6 +130,35 @@ def test_prompts_are_written_and_answered_once_within_the_promised_workspace(lib
             assert not any(n == "unpack" for n, _ in launches) or ring
 
 
+def test_prompts_keep_to_the_smallest_workspace_that_is_taken(lib):
+    r = random.Random(4)
+    up = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    for _ in range(250):
+        Hkv, G, D, Z = r.choice([1, 2, 8]), r.choice([1, 3, 4, 17, 100]), r.choice([64, 128]), r.choice([32, 64, 256])
+        batch, count, t = r.choice([1, 2, 16]), int(2 ** r.uniform(0, 11)), r.choice([0, 0, int(2 ** r.uniform(0, 14))])
+        window, block, Hq = r.choice([0, int(2 ** r.uniform(0, 12))]), 128 // G, G * Hkv
+        ring = T.tempo_ring_blocks(window, Z, min(block, count)) * r.choice([1, 2]) if window and r.random() < 0.7 else 0
+        counts = AT if not ring and r.random() < 0.3 else None
+        kv = store(Hkv, D, Z, ring or (t + count - 1) // Z + 1, ring)
+        low, high = 0, lib.tempo_prefill_workspace_bytes(ctypes.byref(kv), batch, Hq, ring * Z + 128 if ring else t + count - 1)
+        while low < high:                # (enough)
+            middle = (low + high) // 2
+            taken_at = prefill(lib, kv, batch, Hq, t, count, window, counts, middle)[0] == T.TEMPO_OK
+            low, high = (low, middle) if taken_at else (middle + 1, high)
+        for nbytes in (low, low + 1, low + 300):
+            rc, launches = prefill(lib, kv, batch, Hq, t, count, window, counts, nbytes)
+            assert rc == T.TEMPO_OK
+            room = nbytes
+            for name, f in launches:
+                if name == "unpack":
+                    assert f["end"] <= AT + nbytes
+                    room = f["table"] - AT
+                elif name in ("partial_e4m3", "prompt", "short_prompt"):
+                    rows = batch * f["queries"] * Hq * f["num_splits"]
+                    assert f["direct"] or up(rows * 8) + up(rows * D * 4) <= room
+                    room = nbytes
+
+
 def test_prompts_beyond_one_launchs_index_range_are_written_whole_before_answers(lib):
     Hkv, G, D, Z, batch, count = 8, 3, 128, 256, 64, 70000
     kv = store(Hkv, D, Z, count // Z + 1)
