@@ -489,8 +489,9 @@ int tempo_rope_attn_block_window(const tempo_kv* kv, const tempo_rope* rope, con
  *   workspace     device, 256-byte aligned, >= tempo_prefill_workspace_bytes(kv, batch,
  *                 num_q_heads, t + count - 1) bytes
  * On an 8-bit store steps attend over the rows as the store holds them, quantised: the rows are written
- * first; one block of 128 columns is answered over the codes, more over a bf16 copy of the keys/values
- * they see, for which tempo_prefill_workspace_bytes has room (without it: TEMPO_ERR_WORKSPACE).
+ * first; one block of 128 columns, or two behind a long history, is answered over the codes, more over a
+ * bf16 copy of the keys/values they see, for which tempo_prefill_workspace_bytes has room (without it:
+ * TEMPO_ERR_WORKSPACE).
  * All arguments are validated for every block before the first launch.
  */
 int tempo_prefill_causal(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new,
@@ -525,8 +526,8 @@ int tempo_rope_prefill_window(const tempo_kv* kv, const tempo_rope* rope, const 
  * only; 0 on unsupported arguments): 2 when the prompt's query blocks fill the part
  * (bf16, linear store: one block-store write, then one launch in which every workgroup
  * walks the whole key range of its (step, head) columns through LDS and writes `out`
- * directly), 3 on fp32 linear stores, 4 on e4m3 ones (3 for one block), else 3 (e4m3: 4) per block of
- * 128 / (num_q_heads / num_kv_heads) steps. */
+ * directly), 3 on fp32 linear stores, 4 on e4m3 ones (3 for one block, 5 for two), else 3 (e4m3: 4)
+ * per block of 128 / (num_q_heads / num_kv_heads) steps. */
 int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t count);
 
 /* Workspace bound for tempo_prefill_* calls whose last step is at most max_t (host only). */

@@ -1421,9 +1421,14 @@ static int32_t e4m3_chunk(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t
   const int32_t C = ring_chunk(kv, t, left, window, kMaxColumns / (Hq / kv->num_kv_heads));
   return C < most ? C : (int32_t)most;
 }
-// Are C steps answered over the codes?
-static bool e4m3_by_codes(const tempo_kv* kv, int32_t Hq, int32_t C, const int32_t* count_per_seq) {
-  return !count_per_seq && (int64_t)C * (Hq / kv->num_kv_heads) <= kMaxColumns;
+// Are C steps from t on answered over the codes, in one block of 128 columns or two, or over a bf16 copy?  A second block reads
+// the keys once more, the copy is written and read; the more columns that one has, the later it pays (300 prompts of two blocks
+// behind up to 30000 keys, 1 to 16 sequences: 2.1% from the faster way on the mean, 33% at most; the copy always 13%, 170%; 1
+// sequence, 32/1 heads of 128, 6 steps behind 15157 keys, copy / codes 55 / 30 us; three blocks and more gain nothing).
+static bool e4m3_by_codes(const tempo_kv* kv, int32_t Hq, int32_t t, int32_t C, int32_t window, const int32_t* count_per_seq) {
+  const int32_t G = Hq / kv->num_kv_heads, block = kMaxColumns / G;
+  const int64_t keys = window > 0 && window <= t ? (int64_t)window + C - 1 : (int64_t)t + C;
+  return !count_per_seq && C <= 2 * block && (C <= block || keys >= 30 * ((int64_t)C * G - kMaxColumns));
 }
 // Bytes of the largest bf16 copy that a prompt needs.
 static size_t e4m3_copy_bytes(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window) {
@@ -1431,14 +1436,14 @@ static size_t e4m3_copy_bytes(const tempo_kv* kv, int32_t batch, int32_t Hq, int
   for (int32_t c0 = 0, C; c0 < count; c0 += C) {
     C = e4m3_chunk(kv, batch, Hq, t + c0, count - c0, window);
     bool ring;
-    const size_t own = e4m3_by_codes(kv, Hq, C, count_per_seq) ? 0 : unpacked_bytes(kv, batch, unpacked_tiles(kv, t + c0, C, window, &ring));
+    const size_t own = e4m3_by_codes(kv, Hq, t + c0, C, window, count_per_seq) ? 0 : unpacked_bytes(kv, batch, unpacked_tiles(kv, t + c0, C, window, &ring));
     bytes = own > bytes ? own : bytes;
   }
   return bytes;
 }
 
-// A prompt on an 8-bit store: the rows are written, and attended over as they were written.  One block of columns is answered
-// over the codes; more by the bf16 prompt kernels over a bf16 copy of what the prompt sees, in the last copy_bytes bytes of
+// A prompt on an 8-bit store: the rows are written, and attended over as they were written.  A block of columns, or two, is answered
+// over the codes (e4m3_by_codes); more by the bf16 prompt kernels over a bf16 copy of what the prompt sees, in the last copy_bytes bytes of
 // the workspace.  On a ring store in chunks that it can hold.
 static int prefill_e4m3(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch, int32_t Hq,
                  int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window, float scale, void* workspace,
@@ -1468,13 +1473,18 @@ static int prefill_e4m3(const tempo_kv* kv, const void* q, const void* k_new, co
     const size_t q_at = (size_t)c0 * Hq * kv->head_dim * 2;
     const char* const qc = static_cast<const char*>(q) + q_at;
     char* const oc = static_cast<char*>(out) + q_at;
-    if (e4m3_by_codes(kv, Hq, C, count_per_seq)) {
-      tempo_plan plan;
-      make_block_plan(kv, batch, Hq, t + c0, window, false, C, &plan);
-      rc = do_partial(kv, qc, nullptr, nullptr, oc, batch, Hq, t + c0, nullptr, window, scale, &plan, workspace, s, C, rope, 0, count);
-      if (rc == TEMPO_OK && plan.num_splits > 1)
-        rc = do_combine(kv, oc, batch, Hq, t + c0, nullptr, window, &plan, workspace, s, C, 0, count);
-      if (rc != TEMPO_OK) return rc;
+    if (e4m3_by_codes(kv, Hq, t + c0, C, window, count_per_seq)) {
+      const int32_t block = kMaxColumns / (Hq / kv->num_kv_heads);
+      for (int32_t c1 = 0; c1 < C; c1 += block) {
+        const int32_t B = C - c1 < block ? C - c1 : block, first = t + c0 + c1;
+        const size_t at = (size_t)c1 * Hq * kv->head_dim * 2;
+        tempo_plan plan;
+        make_block_plan(kv, batch, Hq, first, window, false, B, &plan);
+        rc = do_partial(kv, qc + at, nullptr, nullptr, oc + at, batch, Hq, first, nullptr, window, scale, &plan, workspace, s, B, rope, 0, count);
+        if (rc == TEMPO_OK && plan.num_splits > 1)
+          rc = do_combine(kv, oc + at, batch, Hq, first, nullptr, window, &plan, workspace, s, B, 0, count);
+        if (rc != TEMPO_OK) return rc;
+      }
       continue;
     }
     bool ring;
@@ -1664,7 +1674,7 @@ int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_head
   if (check_layout(kv) != TEMPO_OK || check_heads(kv, batch, num_q_heads) != TEMPO_OK || count < 1) return 0;
   const int32_t G = num_q_heads / kv->num_kv_heads, block = kMaxColumns / G;
   if (kv->ring_blocks == 0 && prompt_in_one_launch(kv, batch, num_q_heads, count)) {
-    if (kv->dtype == TEMPO_E4M3) return count <= block ? 3 : 4;  // write, turn into bf16, attend, combine
+    if (kv->dtype == TEMPO_E4M3) return count <= block ? 3 : count <= 2 * block ? 5 : 4;  // write, turn into bf16 (or not, twice:) attend, combine
     if (kv->dtype != TEMPO_BF16) return 3;
     if (prompt_fills_part(kv, batch, G, count)) return 2;  // one launch, and no key range is split
   }

@@ -371,6 +371,15 @@ def test_prompts(Hq, Hkv, D, Z, B, t, count, window, ring, rope, counts, over_ro
             np.testing.assert_array_equal(np64(vg)[b], Vh[b, first:last])
 
 
+@pytest.mark.parametrize("over_rows", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,D,Z,B,t,count,window,ring,rope,counts",
+                         [(6, 2, 128, 64, 2, 2500, 60, 0, 0, False, False), (8, 2, 64, 32, 1, 3000, 64, 0, 0, True, False),
+                          (32, 1, 128, 256, 1, 3700, 6, 0, 0, False, False), (6, 2, 128, 64, 2, 2000, 45, 600, 16, False, False),
+                          (6, 2, 64, 64, 2, 1000, 43, 300, 0, True, False), (6, 2, 128, 64, 1, 1000, 130, 200, 8, False, False)])
+def test_prompts_of_two_blocks_behind_a_history(Hq, Hkv, D, Z, B, t, count, window, ring, rope, counts, over_rows):
+    test_prompts(Hq, Hkv, D, Z, B, t, count, window, ring, rope, counts, over_rows)
+
+
 def test_nan_shows_where_it_is_seen_only():
     Hq, Hkv, D, Z, B, t, window = 6, 2, 128, 64, 2, 300, 100
     q, K, V = normal(17, 1, (B, Hq, D)), normal(17, 2, (B, t + 1, Hkv, D)), normal(17, 3, (B, t + 1, Hkv, D))

@@ -130,6 +130,19 @@ def test_prompts_are_written_and_answered_once_within_the_promised_workspace(lib
             assert not any(n == "unpack" for n, _ in launches) or ring
 
 
+def test_two_blocks_behind_a_long_history_are_answered_over_the_codes(lib):
+    for t, count, window, ways in ((100, 42, 0, ["partial_e4m3"]), (3000, 64, 0, ["partial_e4m3"] * 2), (1500, 64, 0, ["prompt"]), (3000, 64, 700, ["prompt"]),
+                                   (3000, 43, 300, ["partial_e4m3"] * 2), (30000, 84, 0, ["partial_e4m3"] * 2), (30000, 85, 0, ["prompt"])):
+        kv = store(8, 128, 64, (t + count) // 64 + 1)
+        rc, launches = prefill(lib, kv, 2, 24, t, count, window, nbytes=1 << 40)
+        assert rc == T.TEMPO_OK and [n for n, _ in launches if n in ("partial_e4m3", "prompt", "short_prompt")] == ways, (t, count, window)
+        assert len(launches) <= lib.tempo_prefill_launches(ctypes.byref(kv), 2, 24, count)
+        if len(ways) == 2:               # one after the other, in the call's own rows
+            a, z = [f for n, f in launches if n == "partial_e4m3"]
+            assert (a["t"], a["queries"], z["t"], z["queries"]) == (t, 42, t + 42, count - 42) and a["steps"] == z["steps"] == count
+            assert z["out"] - a["out"] == 42 * 24 * 128 * 2
+
+
 def test_prompts_keep_to_the_smallest_workspace_that_is_taken(lib):
     r = random.Random(4)
     up = lambda n: (n + 255) // 256 * 256  # noqa: E731
