@@ -71,9 +71,10 @@ __device__ inline uint32_t values_of(uint32_t codes, bool high, float scale) {
 // caller's arrays, and in the store 8 codes of each key row or, of the values, 4 codes (the 4 slots) of each dim, between which
 // a block is turned in registers.  The group's images pass through LDS, so that the store is read and written in whole units of
 // 1 KiB, the rows in runs of D elements.
-// Bound by memory: 8 x 2047 rows in 8 heads of 128 are written in 20.3 us (101 MB, 5.0 TB/s; a large copy moves 4.9) and read
-// back in 16.2; by one wavefront a group 24.6 and 16.3 (2 x 1104 rows 8.9 and 6.0, now 6.9 and 4.4); row by row and element by
-// element 52.6 and 73.2.
+// Bound by memory: 8 x 2047 rows in 8 heads of 128 are written in 21.4 us (101 MB, 4.7 TB/s; a large copy moves 4.9) and read
+// back in 15.8; by one wavefront a group 4.3 more to write, row by row and element by element 52.6 and 73.2.  What is read once
+// or written for good passes the caches by: the caller's rows on the way in (27.4 us without) and on the way out (16 x 4000 rows of
+// 8 heads of 64 read back 30.4 us, 198 MB, without 41.2; a sum over them right behind it loses 1.8 of 33).
 // 4 words of 4 bytes, a[i] = byte i of every column: columns to rows.
 __device__ inline void turn4(uint32_t* a) {
   const uint32_t t0 = __builtin_amdgcn_perm(a[1], a[0], 0x05010400), t1 = __builtin_amdgcn_perm(a[1], a[0], 0x07030602);
@@ -82,17 +83,6 @@ __device__ inline void turn4(uint32_t* a) {
   a[1] = __builtin_amdgcn_perm(t2, t0, 0x07060302);
   a[2] = __builtin_amdgcn_perm(t3, t1, 0x05040100);
   a[3] = __builtin_amdgcn_perm(t3, t1, 0x07060302);
-}
-
-// Maximum over the D/8 lanes that hold a row.
-template <int D>
-__device__ inline uint32_t row_max(uint32_t v) {
-  auto step = [&](int o) { v = (uint32_t)o > v ? (uint32_t)o : v; };
-  step(__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lanes 1, 0, 3, 2 of four
-  step(__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // 2, 3, 0, 1
-  step(__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true));  // eight lanes reversed
-  if (D == 128) step(__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true));  // sixteen
-  return v;
 }
 
 // Offsets of a block inside a group's image: of 8 codes of key slot 4 sg + i, dims 8 part ..; of the 4 codes of dim
@@ -135,7 +125,7 @@ __global__ __launch_bounds__(2 * D) void kv_append_groups_e4m3(StoreParams p, co
   auto row_at = [&](int slot) { return row0 + (int64_t)(slot < lo ? lo : (slot < hi ? slot : hi - 1)) * p.Hkv; };
   u32x4 x[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const u32x4*>(rows + row_at(4 * sg + i) * D + 8 * part);
+  for (int i = 0; i < 4; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(rows + row_at(4 * sg + i) * D + 8 * part));
   if (p.rope_cos && !value) {  // a piece and its partner D/2 dims away are turned together, each lane for its own
     const int other = part < PARTS / 2 ? part + PARTS / 2 : part - PARTS / 2;
 #pragma unroll
@@ -149,15 +139,11 @@ __global__ __launch_bounds__(2 * D) void kv_append_groups_e4m3(StoreParams p, co
   uint32_t codes[2][4];  // of slot i, dims 0..3 and 4..7 of the block; values, turned: of dim k, slots 0..3
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) top = top_of(x[i][e], top);
-    const uint32_t E = (uint32_t)scale_byte(row_max<D>(top));
-    const float inverse = inverse_scale_of(E), most = largest_code(E);
-    codes[0][i] = codes_of(x[i].x, inverse, most) | (codes_of(x[i].y, inverse, most) << 16);
-    codes[1][i] = codes_of(x[i].z, inverse, most) | (codes_of(x[i].w, inverse, most) << 16);
+    const RowPiece r = quantise_piece<D>(x[i]);
+    codes[0][i] = r.lo;
+    codes[1][i] = r.hi;
     const int slot = 4 * sg + i;
-    if (part == 0 && slot >= lo && slot < hi) pool[scales + (value ? scale_off_v(slot) : scale_off_k(slot))] = (uint8_t)E;
+    if (part == 0 && slot >= lo && slot < hi) pool[scales + (value ? scale_off_v(slot) : scale_off_k(slot))] = (uint8_t)r.scale;
     if (!value) *reinterpret_cast<uint2*>(image + in_lds(key_piece<D>(sg, part, i))) = uint2{codes[0][i], codes[1][i]};
   }
   if (value && !whole) {  // this call's slots only, byte by byte: another launch may write the others at the same time
@@ -236,7 +222,7 @@ __global__ __launch_bounds__(2 * D) void kv_gather_e4m3(StoreParams p, uint16_t*
     const float s = scale_of(scale[i]);
     const uint32_t a = codes[0][i], z = codes[1][i];
     const u32x4 o = {values_of(a, false, s), values_of(a, true, s), values_of(z, false, s), values_of(z, true, s)};
-    *reinterpret_cast<u32x4*>(out + (row0 + (int64_t)slot * p.Hkv) * D + 8 * part) = o;
+    __builtin_nontemporal_store(o, reinterpret_cast<u32x4*>(out + (row0 + (int64_t)slot * p.Hkv) * D + 8 * part));
   }
 }
 

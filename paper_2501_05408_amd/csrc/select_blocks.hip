@@ -84,12 +84,12 @@ __device__ inline i16x2 reduce_row(i16x2 v, F f) {
 
 // Bounds of the block of one kv head whose first slot has number `first` among the store's; wavefronts w < D/64 (8-bit store)
 // or D/32 (bf16) read the 1 KiB units of their part of the dims, 16 or 8 of them a lane.  Lane (row + 16c) goes through the
-// rows row, 16 + row, ... of the block, then the 16 lanes of equal c are reduced.  fresh: the block's last row is not in the
+// rows row, 16 + row, ... of the block, then the 16 lanes of equal c are reduced.  kFresh: the block's last row is not in the
 // store yet; the lane's part of it is in `last` (8 bits: codes, with scale byte last_scale).
 // Bound by memory, as long as the comparisons are whole words' (8 x 4096 keys of 4 heads of 128 in blocks of 64, 34 MB:
-// 7.4 us; one value at a time in fp32 10.2).
-template <int D, bool k8>
-__device__ __forceinline__ void bounds_of_block(const StoreParams& p, int64_t first, int w, int lane, uint16_t* __restrict__ to, bool fresh, u32x4 last,
+// 6.7 us, 5.1 TB/s; one value at a time in fp32 10.2; loads that leave the keys in the caches 7.4).
+template <int D, bool k8, bool kFresh>
+__device__ __forceinline__ void bounds_of_block(const StoreParams& p, int64_t first, int w, int lane, uint16_t* __restrict__ to, u32x4 last,
                                                 uint32_t last_scale) {
   constexpr int PER_TILE = k8 ? D / 64 : D / 32;  // units of a row-tile
   constexpr int N = k8 ? 8 : 4;                   // words of two values
@@ -109,9 +109,13 @@ __device__ __forceinline__ void bounds_of_block(const StoreParams& p, int64_t fi
     u32x4 u[2];
     uint32_t both = 0;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) u[r] = *reinterpret_cast<const u32x4*>(at + (int64_t)(2 * t + r) * PER_TILE * 1024);
+    for (int r = 0; r < 2; ++r) {
+      const u32x4* const unit = reinterpret_cast<const u32x4*>(at + (int64_t)(2 * t + r) * PER_TILE * 1024);
+      if constexpr (kFresh) u[r] = *unit;  // (a step's own block is read again by its attention)
+      else u[r] = __builtin_nontemporal_load(unit);
+    }
     if constexpr (k8) both = *reinterpret_cast<const uint16_t*>(scales + 32 * t);
-    if (fresh && t == groups - 1 && (lane & 15) == 15) {
+    if (kFresh && t == groups - 1 && (lane & 15) == 15) {
       u[1] = last;
       both = (both & 0xFFu) | (last_scale << 8);
     }
@@ -168,7 +172,7 @@ __global__ __launch_bounds__(k8 ? D : 2 * D) void block_bounds(StoreParams p, ui
   if (last < t_b || last > (int64_t)t_b + rows - 1) return;  // not completed by the call's steps; uniform
   const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
   const int64_t pair = (int64_t)phys * p.Hkv + head;
-  bounds_of_block<D, k8>(p, pair << p.z_log2, threadIdx.x >> 6, threadIdx.x & 63, bounds + pair * 2 * D, false, u32x4{0u, 0u, 0u, 0u}, 0u);
+  bounds_of_block<D, k8, false>(p, pair << p.z_log2, threadIdx.x >> 6, threadIdx.x & 63, bounds + pair * 2 * D, u32x4{0u, 0u, 0u, 0u}, 0u);
 }
 
 // A step's row of one (sequence, kv head) into the store, and the bounds of its block if the step is the block's last.  All
@@ -206,7 +210,7 @@ __device__ __forceinline__ void write_and_bound(const StoreParams& p, const void
     for (int i = 0; i < 4; ++i) last[i] = (uint32_t)__shfl((int)x[i], (4 * wave + c) % LANES);
   }
   if (slot != (1 << p.z_log2) - 1) return;  // uniform
-  if (wave < (k8 ? D / 64 : D / 32)) bounds_of_block<D, k8>(p, first, wave, lane, bounds + pair * 2 * D, true, last, last_scale);
+  if (wave < (k8 ? D / 64 : D / 32)) bounds_of_block<D, k8, true>(p, first, wave, lane, bounds + pair * 2 * D, last, last_scale);
 }
 
 // ---- scores -----------------------------------------------------------------------------------
