@@ -88,6 +88,34 @@ def test_every_bf16_value_is_quantised_as_defined(D):
             np.testing.assert_array_equal(CODES[code], held(x[0, j, h])[d] / 2.0 ** float(e))
 
 
+@pytest.mark.parametrize("by_rows", [False, True])
+@pytest.mark.parametrize("E", [16, 17, 60, 126, 127, 128, 200, 246, 247])
+@pytest.mark.parametrize("D", [64, 128])
+def test_values_of_every_size_beside_a_rows_largest(D, E, by_rows):
+    """Rows without NaN: every mantissa and sign from the largest exponent of a scale down to what rounds to 0, each row with
+    one element that fixes its scale."""
+    top = E + 8 if E < 247 else 254                   # largest exponent field of a row with this scale byte
+    bits = np.array([(s << 15) | (x << 7) | m for s in (0, 1) for x in range(max(0, top - 21), top + 1) for m in range(128)
+                     if x < top or m <= (0x60 if E < 247 else 0x7F)], dtype=np.uint16)
+    bits = bits[synth.permutation(9, 1, len(bits))]
+    bits = np.concatenate([bits, bits[:-len(bits) % (D - 1)]]).reshape(-1, D - 1)
+    most = np.full((len(bits), 1), (top << 7) | (0x60 if E < 247 else 0x7F), dtype=np.uint16)
+    rows = np.concatenate([bits[:, :D // 3], most, bits[:, D // 3:]], axis=1)
+    x = torch.from_numpy(rows.view(np.int16)).view(torch.bfloat16).double().numpy()
+    assert (scale_exponents(x) == E - 127).all()
+    K = x.reshape(1, -1, 1, D)
+    V = K[:, ::-1].copy()
+    n = K.shape[1]
+    st = make_store(2, 1, 1, 1, D, 32, n - 1)
+    if by_rows:                                       # (a call with steps of its own for each sequence writes row by row)
+        T.tempo_kv_append_block(st.kv, bf16(K), bf16(V), 1, 0, torch.zeros(1, dtype=torch.int32, device=DEV), n)
+    else:
+        st.append_block(bf16(K), bf16(V), 0, n)
+    k, v = st.gather(0, n)
+    np.testing.assert_array_equal(np64(k), held(K))
+    np.testing.assert_array_equal(np64(v), held(V))
+
+
 @pytest.mark.parametrize("D", [64, 128])
 def test_every_code_and_scale_is_read_back(D):
     """The 256 codes under every scale a row can have, put into the pools by hand."""
@@ -289,6 +317,38 @@ def test_fused_steps_are_the_write_and_the_attention(Hq, Hkv, D, B, t, ragged, w
     if not window:
         three = c.step_causal_noalloc(qd, k, v, a.new_out(), t, tps)
         assert torch.equal(three, two) and torch.equal(a.k_pool, c.k_pool) and torch.equal(a.v_pool, c.v_pool)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_unusual_rows_are_held_the_same_whichever_call_writes_them(D):
+    """NaN, infinities, the largest values, zeros and rows of very different sizes, side by side in the heads of one step."""
+    Hkv, B, Z, t = 8, 2, 32, 95                       # (step 95 completes its block)
+    big = 3.3895313892515355e38                       # the largest bf16
+    k = normal(61, 1, (B, Hkv, D))
+    k[0, 1, 5], k[0, 2, D - 1], k[0, 3, 0], k[0, 4], k[0, 5] = np.nan, np.inf, -np.inf, 0.0, -big
+    k[1, 0], k[1, 1, 7], k[1, 2], k[1, 3, 3], k[1, 4] = np.nan, big, k[1, 2] * 2.0 ** -125, 2.0 ** -133, np.inf
+    k[1, 5, 1], k[1, 5, 2] = np.nan, big
+    v = k[::-1, ::-1].copy()
+    k, v, q = bf16(k), bf16(v), bf16(normal(61, 2, (B, Hkv, D)))
+    before = bf16(normal(61, 3, (B, t, Hkv, D)))
+
+    def written(call):
+        st = make_store(61, B, Hkv, Hkv, D, Z, t)
+        st.append_block(before, before, 0, t)
+        call(st)
+        return st.k_pool, st.v_pool
+
+    pools = [written(lambda st: st.append(k, v, t)), written(lambda st: st.step_causal(q, k, v, st.new_out(), t)),
+             written(lambda st: st.step_window(q, k, v, st.new_out(), t, 40)),
+             written(lambda st: st.step_selected(st.new_bounds(), q, k, v, st.new_out(), t, 3)),
+             written(lambda st: st.prefill_attend(q[:, None].contiguous(), k[:, None].contiguous(), v[:, None].contiguous(), st.new_out()[:, None].contiguous(), t, 1))]
+    whole = make_store(61, B, Hkv, Hkv, D, Z, t)
+    whole.append_block(torch.cat([before, k[:, None]], 1), torch.cat([before, v[:, None]], 1), 0, t + 1)  # by groups
+    for kp, vp in pools:
+        assert torch.equal(kp, whole.k_pool) and torch.equal(vp, whole.v_pool)
+    got = whole.gather(t, 1)
+    for x, row in zip(got, (k, v)):
+        np.testing.assert_array_equal(np64(x)[:, 0], held(np64(row)))
 
 
 @pytest.mark.parametrize("D,window,Hq,C", [(64, 0, 6, 4), (128, 0, 6, 4), (128, 40, 6, 4), (64, 0, 36, 7), (128, 33, 80, 3)])
