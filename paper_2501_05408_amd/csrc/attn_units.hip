@@ -56,9 +56,9 @@ __device__ __forceinline__ bf16x8 operand_of(uint32_t a, uint32_t b, float scale
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// Logits of the group's two row tiles for CT tiles of 16 columns, in base-2 units.
+// Products of the group's two row tiles with CT tiles of 16 columns; not scaled yet.
 template <int D, bool k8, int CT>
-__device__ __forceinline__ void image_logits(const AttnParams& p, const u32x4 (*qreg)[D / 32], const Image<D, k8>& g, float (*x)[8]) {
+__device__ __forceinline__ void image_logits(const u32x4 (*qreg)[D / 32], const Image<D, k8>& g, float (*x)[8]) {
   constexpr int KS = D / 32;
   f32x4 sa[CT], sb[CT];
 #pragma unroll
@@ -89,8 +89,8 @@ __device__ __forceinline__ void image_logits(const AttnParams& p, const u32x4 (*
   for (int ct = 0; ct < CT; ++ct) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      x[ct][r] = sa[ct][r] * p.scale_log2e;
-      x[ct][4 + r] = sb[ct][r] * p.scale_log2e;
+      x[ct][r] = sa[ct][r];
+      x[ct][4 + r] = sb[ct][r];
     }
   }
 }
@@ -108,12 +108,57 @@ __device__ __forceinline__ uint2 seen_bytes(int key0, int v_lo, int v_hi, int la
   return keep;
 }
 
-// The weights of a group's slots, times the scales of their values.
-__device__ __forceinline__ bf16x8 scaled_weights(bf16x8 pa, uint2 scales) {
+__device__ __forceinline__ float low_of(uint32_t pair) { return __builtin_bit_cast(float, pair << 16); }
+__device__ __forceinline__ float high_of(uint32_t pair) { return __builtin_bit_cast(float, pair & 0xFFFF0000u); }
+
+constexpr float kUnseen = -3e38f;  // reference of a column that has seen no key: finite, so that masked logits of -inf get the weight 0
+
+// Online-softmax update of a column's reference, sum and accumulators, and the group's weights, 2^(x scale - reference) in bf16,
+// as four words of two.  The sum is that of the rounded weights.  The reference is set 2^kSlack above a maximum that exceeds
+// it, the first one's above all, so weights are at most 1 and the accumulators are hardly ever rescaled.  (That, the scale inside
+// the exponent and values masked only where a range cuts their group, us: 48 ragged sequences of 32/8 heads of 64, window 1000
+// 12.45 -> 12.05; 32 sequences of 1000 keys, 24/8 heads of 128 12.1 -> 11.5; 16 of 4000, 63 and 126 columns 38 -> 34, 70 -> 61.)
+template <int D>
+__device__ __forceinline__ u32x4 softmax_weights(const float* x, float scale, int lane, WaveState<D>& st) {
+  float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+  mx = column_max(mx) * scale;
+  const bool above = mx > st.m;
+  if (__any(above && st.m != kUnseen)) {
+    const float alpha = above ? fast_exp2(st.m - (mx + kSlack)) : 1.f;
+    float a[4];
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    pa[r] = (__bf16)((float)pa[r] * scale_of((scales.x >> (8 * r)) & 0xFFu));
-    pa[4 + r] = (__bf16)((float)pa[4 + r] * scale_of((scales.y >> (8 * r)) & 0xFFu));
+    for (int r = 0; r < 4; ++r) a[r] = __shfl(alpha, 4 * (lane >> 4) + r);
+    st.l *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.acc[dt][r] *= a[r];
+    }
+  }
+  st.m = above ? mx + kSlack : st.m;
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 pair = {(__bf16)fast_exp2(fmaf(x[2 * i], scale, -st.m)), (__bf16)fast_exp2(fmaf(x[2 * i + 1], scale, -st.m))};
+    w[i] = __builtin_bit_cast(uint32_t, pair);
+    st.l += low_of(w[i]) + high_of(w[i]);
+  }
+  return w;
+}
+
+// The weights of a group's slots, times the scales of their values.
+__device__ __forceinline__ bf16x8 scaled_weights(u32x4 w, uint2 scales) {
+  uint32_t shift = 23;  // (unknown to the compiler, so that a byte is taken and shifted by one instruction)
+  asm("" : "+v"(shift));
+  bf16x8 pa;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t four = i < 2 ? scales.x : scales.y;
+    const float a = __builtin_bit_cast(float, ((four >> (16 * (i & 1))) & 0xFFu) << shift);
+    const float z = __builtin_bit_cast(float, ((four >> (16 * (i & 1) + 8)) & 0xFFu) << shift);
+    pa[2 * i] = (__bf16)(low_of(w[i]) * a);
+    pa[2 * i + 1] = (__bf16)(high_of(w[i]) * z);
   }
   return pa;
 }
@@ -212,7 +257,7 @@ __device__ __forceinline__ void merge_units(const AttnParams& p, const float* sm
     float den = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const bool seen = lw[w] != 0.f;  // (a column's largest weight is 1)
+      const bool seen = lw[w] != 0.f;  // (a column's largest weight is at least 2^-kSlack)
       const float wgt = fast_exp2(mw[w] - ref);
 #pragma unroll
       for (int e = 0; e < 4; ++e) num[e] += seen ? wgt * aw[w][e] : 0.f;
@@ -239,8 +284,9 @@ __device__ __forceinline__ void merge_units(const AttnParams& p, const float* sm
 }
 
 // CT: tiles of 16 columns that a wavefront takes, over the same operands.
+// (D = 64, two tiles: 134 registers without the bound, 3 wavefronts to a SIMD; 128 columns 47.9 us, with it 40.6)
 template <int D, bool k8, bool kSelect, bool kRope, int CT>
-__global__ __launch_bounds__(512) void attn_units(SelectParams p) {
+__global__ __launch_bounds__(512, D == 64 && CT == 2 ? 4 : 1) void attn_units(SelectParams p) {
   constexpr int KS = D / 32, DT = D / 16;
   extern __shared__ float smem[];
   const int lane = threadIdx.x & 63;
@@ -343,7 +389,7 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
   WaveState<D> st[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    st[ct].m = -INFINITY;
+    st[ct].m = kUnseen;
     st[ct].l = 0.f;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) st[ct].acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -356,37 +402,51 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
       if (key == key_new) patch_keys<D>(t_b, lane, stage, g);
     }
     float x[CT][8];
-    image_logits<D, k8, CT>(p, qreg, g, x);
+    image_logits<D, k8, CT>(qreg, g, x);
     if (more) load_image_keys<D, k8>(p, slot_nxt, slots, lane, g);
-    // Slots that no step of the call sees may be unwritten: codes and scales of 0, bf16 values of 0, under the weight of 0.
-    uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};               // bf16 values: masks of the lane's 8 slots
-    uint2 keep8 = {~0u, ~0u};                              // codes
-    if (key < all_lo || key > all_hi - 31) {               // wave-uniform: a group that some column's range cuts
+    const bool cut = key < all_lo || key > all_hi - 31;  // wave-uniform: some column's range cuts the group
+    if (cut) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) mask_logits(key >> 5, lo_col[ct], hi_col[ct], lane, x[ct]);
-      if constexpr (k8) keep8 = seen_bytes(key, from, seen_hi, lane);
-      else value_masks(key >> 5, from, seen_hi, lane, keep);
     }
-    bf16x8 pa[CT];
+    u32x4 w[CT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) pa[ct] = softmax_update<D>(x[ct], lane, st[ct]);
+    for (int ct = 0; ct < CT; ++ct) w[ct] = softmax_weights<D>(x[ct], p.scale_log2e, lane, st[ct]);
     if constexpr (k8 && !kSelect) {
       if (key == key_new) patch_values<D>(t_b, lane, stage, g);
     }
-    if constexpr (k8) {
+    if (cut) {  // slots that no step of the call sees may be unwritten: codes and scales of 0, bf16 values of 0, under the weight of 0
+      if constexpr (k8) {
+        const uint2 keep = seen_bytes(key, from, seen_hi, lane);
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) pa[ct] = scaled_weights(pa[ct], uint2{g.v_scales.x & keep8.x, g.v_scales.y & keep8.y});
+        for (int i = 0; i < D / 32; ++i) {
+          g.v[i].x &= keep.x; g.v[i].y &= keep.y; g.v[i].z &= keep.x; g.v[i].w &= keep.y;
+        }
+        g.v_scales.x &= keep.x;
+        g.v_scales.y &= keep.y;
+      } else {
+        uint32_t keep[4];
+        value_masks(key >> 5, from, seen_hi, lane, keep);
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+          g.v[i].x &= keep[0]; g.v[i].y &= keep[1]; g.v[i].z &= keep[2]; g.v[i].w &= keep[3];
+        }
+      }
+    }
+    bf16x8 pa[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      if constexpr (k8) pa[ct] = scaled_weights(w[ct], g.v_scales);
+      else pa[ct] = as_bf16x8(w[ct]);
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
       bf16x8 v;
       if constexpr (k8) {
         const u32x4 u = g.v[dt / 2];
-        v = dt & 1 ? operand_of(u.z & keep8.x, u.w & keep8.y, 1.f) : operand_of(u.x & keep8.x, u.y & keep8.y, 1.f);
+        v = dt & 1 ? operand_of(u.z, u.w, 1.f) : operand_of(u.x, u.y, 1.f);
       } else {
-        u32x4 u = g.v[dt];
-        u.x &= keep[0]; u.y &= keep[1]; u.z &= keep[2]; u.w &= keep[3];
-        v = as_bf16x8(u);
+        v = as_bf16x8(g.v[dt]);
       }
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) st[ct].acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[ct], v, st[ct].acc[dt], 0, 0, 0);
@@ -418,7 +478,7 @@ __global__ __launch_bounds__(512) void attn_units(SelectParams p) {
     float* sm_l = smem + nwaves * 16;    // [nwaves][16]
     float* sm_acc = smem + nwaves * 32;  // [nwaves][ncols][D]
     if (lane < 16) {
-      sm_m[wave * 16 + lane] = st[ct].m;
+      sm_m[wave * 16 + lane] = st[ct].m == kUnseen ? -INFINITY : st[ct].m;
       sm_l[wave * 16 + lane] = l_tot;
     }
     {

@@ -465,6 +465,22 @@ def test_far_from_one():
         assert_attention(out, q, held(K), held(V), t, 0, st.scale, f"values of 2^{power}")
 
 
+@pytest.mark.parametrize("queries", [1, 30])
+def test_values_at_the_end_of_the_range(queries):
+    """Averages of values of up to 3e38 over 200 keys of nearly the same weight: sums of weights times values stay finite."""
+    B, Hq, Hkv, D, Z, n = 2, 6, 2, 128, 64, 200
+    q, K = normal(71, 1, (B, queries, Hq, D)) * 2.0 ** -6, normal(71, 2, (B, n, Hkv, D))
+    V = np.abs(normal(71, 3, (B, n, Hkv, D)))
+    V = np64(bf16(np.minimum(1 + V, 1.99) * 2.0 ** 127))
+    st = make_store(71, B, Hq, Hkv, D, Z, n - 1)
+    st.append_block(bf16(K), bf16(V), 0, n)
+    out = torch.empty((B, queries, Hq, D), dtype=torch.bfloat16, device=DEV)
+    t = n - queries
+    st.attend_block(bf16(q), out, t, queries)
+    for c in sorted({0, queries - 1}):
+        assert_attention(out[:, c], q[:, c], held(K), held(V), t + c, 0, st.scale, f"step {c}")
+
+
 def test_captured_and_replayed_and_on_another_stream():
     Hq, Hkv, D, Z, B, t = 24, 8, 128, 64, 2, 1500
     st, q, K, V, first, _ = filled(19, Hq, Hkv, D, Z, B, t, 0, False, 1)
