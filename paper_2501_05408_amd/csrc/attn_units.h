@@ -47,6 +47,7 @@ struct ChooseParams {
 #define TEMPO_LAUNCHER __attribute__((weak)) hipError_t
 TEMPO_LAUNCHER launch_append_e4m3(const StoreParams& p, const void* k_new, const void* v_new, int D, hipStream_t stream);
 TEMPO_LAUNCHER launch_gather_e4m3(const StoreParams& p, void* k_out, void* v_out, int D, int j0, int count, hipStream_t stream);
+TEMPO_LAUNCHER launch_append_copy_e4m3(const StoreParams& p, const UnpackParams& u, const void* k_new, const void* v_new, int D, hipStream_t stream);
 TEMPO_LAUNCHER launch_unpack_e4m3(const StoreParams& p, const UnpackParams& u, int groups, int D, hipStream_t stream);
 TEMPO_LAUNCHER launch_partial_e4m3(const AttnParams& p, int batch, int D, int grid_splits, int waves, hipStream_t stream);
 TEMPO_LAUNCHER launch_partial_selected(const SelectParams& p, int batch, int D, int dtype, int grid_splits, int waves, hipStream_t stream);

@@ -100,14 +100,34 @@ __device__ inline int value_piece(int sg, int part, int k) {
 // The image in LDS: 16 bytes more for every 256, so that the pieces that lanes touch together lie in different banks.
 __host__ __device__ constexpr int in_lds(int at) { return at + (at >> 8) * 16; }
 
+// The same pieces in the image of a bf16 group: 8 dims of key slot 4 sg + i; dim 8 part + k of slots 4 sg .. +3.
 template <int D>
-__global__ __launch_bounds__(2 * D) void kv_append_groups_e4m3(StoreParams p, const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new) {
+__device__ inline int wide_key_piece(int sg, int part, int i) {
+  return (((sg >> 2) * (D >> 5) + (part >> 2)) * 64 + (part & 3) * 16 + 4 * (sg & 3) + i) * 16;
+}
+template <int D>
+__device__ inline int wide_value_piece(int sg, int part, int k) {
+  const int d = 8 * part + k;
+  return ((d >> 4) * 64 + (sg & 3) * 16 + (d & 15)) * 16 + (sg >> 2) * 8;
+}
+
+// kCopy: of a prompt from step 0 on, whose rows are also put into the bf16 store u, as they are held, by the same launch (a prompt
+// of 499 steps, 24/8 heads of 128, 20.5 us; by a launch of kv_unpack_e4m3 behind it 23.2).
+template <int D, bool kCopy>
+__global__ __launch_bounds__(2 * D) void kv_append_groups_e4m3(StoreParams p, UnpackParams u, const uint16_t* __restrict__ k_new,
+                                                               const uint16_t* __restrict__ v_new) {
   constexpr int PARTS = D / 8, HALF = D;  // blocks of a group, and threads, for keys and for values
   __shared__ __align__(16) uint8_t images[2][in_lds(32 * D)];
+  __shared__ __align__(16) uint8_t wides[2][kCopy ? in_lds(64 * D) : 16];
   const int tid = threadIdx.x % HALF;
   const bool value = __builtin_amdgcn_readfirstlane(threadIdx.x >= HALF);
   uint8_t* const image = images[value];
   const int g = blockIdx.x, head = blockIdx.y, b = blockIdx.z;
+  if constexpr (kCopy) {
+    if (g == 0 && head == 0) {
+      for (int n = threadIdx.x; n < u.tiles; n += 2 * D) u.table[(int64_t)b * u.tiles + n] = b * u.tiles + n;
+    }
+  }
   const int rows_b = rows_of(p, b) < p.count ? rows_of(p, b) : p.count;
   const int t0 = ((p.t >> 5) + g) << 5;  // first step of this group
   const int first_row = t0 - p.t;        // source row of slot 0 (negative: before the call)
@@ -136,12 +156,19 @@ __global__ __launch_bounds__(2 * D) void kv_append_groups_e4m3(StoreParams p, co
       else rotate_pieces(p.rope_cos, p.rope_sin, t, D / 2, 8 * other, o, x[i]);
     }
   }
+  uint8_t* const wide = wides[value];
+  u32x4 held[4];         // (kCopy) what the codes stand for
   uint32_t codes[2][4];  // of slot i, dims 0..3 and 4..7 of the block; values, turned: of dim k, slots 0..3
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const RowPiece r = quantise_piece<D>(x[i]);
     codes[0][i] = r.lo;
     codes[1][i] = r.hi;
+    if constexpr (kCopy) {
+      const float scale = scale_of(r.scale);
+      held[i] = u32x4{values_of(r.lo, false, scale), values_of(r.lo, true, scale), values_of(r.hi, false, scale), values_of(r.hi, true, scale)};
+      if (!value) *reinterpret_cast<u32x4*>(wide + in_lds(wide_key_piece<D>(sg, part, i))) = held[i];
+    }
     const int slot = 4 * sg + i;
     if (part == 0 && slot >= lo && slot < hi) pool[scales + (value ? scale_off_v(slot) : scale_off_k(slot))] = (uint8_t)r.scale;
     if (!value) *reinterpret_cast<uint2*>(image + in_lds(key_piece<D>(sg, part, i))) = uint2{codes[0][i], codes[1][i]};
@@ -162,11 +189,30 @@ __global__ __launch_bounds__(2 * D) void kv_append_groups_e4m3(StoreParams p, co
       for (int e = 0; e < 4; ++e) *reinterpret_cast<uint32_t*>(image + in_lds(value_piece<D>(sg, part, 4 * q + e))) = codes[q][e];
     }
   }
+  if constexpr (kCopy) {
+    if (value) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+        *reinterpret_cast<uint2*>(wide + in_lds(wide_value_piece<D>(sg, part, e))) =
+            uint2{__builtin_amdgcn_perm(held[1][e >> 1], held[0][e >> 1], sel), __builtin_amdgcn_perm(held[3][e >> 1], held[2][e >> 1], sel)};
+      }
+    }
+  }
   __syncthreads();
+  if constexpr (kCopy) {
+    const int64_t to = ((((int64_t)b * u.tiles + (t0 >> p.z_log2)) * p.Hkv + head) << p.z_log2) + (t0 & ((1 << p.z_log2) - 1));
+    uint8_t* const copy = static_cast<uint8_t*>(value ? u.v : u.k) + to * 2 * D;
+#pragma unroll
+    for (int i = 0; i < 64 * D / (16 * HALF); ++i) {
+      const int at = (i * HALF + tid) * 16;
+      *reinterpret_cast<u32x4*>(copy + at) = *reinterpret_cast<const u32x4*>(wide + in_lds(at));
+    }
+  }
   if (value && !whole) return;
 #pragma unroll
-  for (int u = 0; u < 32 * D / (16 * HALF); ++u) {
-    const int at = (u * HALF + tid) * 16, slot = 16 * (at / (16 * D)) + (tid & 15);  // (a key unit's 16 bytes belong to one slot)
+  for (int i = 0; i < 32 * D / (16 * HALF); ++i) {
+    const int at = (i * HALF + tid) * 16, slot = 16 * (at / (16 * D)) + (tid & 15);  // (a key unit's 16 bytes belong to one slot)
     if (value || (slot >= lo && slot < hi)) *reinterpret_cast<u32x4*>(pool + slot0 * D + at) = *reinterpret_cast<const u32x4*>(image + in_lds(at));
   }
 }
@@ -289,6 +335,14 @@ hipError_t launch_unpack_e4m3(const StoreParams& p, const UnpackParams& u, int g
   return launch(kv_unpack_e4m3<64>, grid, dim3(64), 0, stream, p, u);
 }
 
+hipError_t launch_append_copy_e4m3(const StoreParams& p, const UnpackParams& u, const void* k_new, const void* v_new, int D, hipStream_t stream) {
+  const uint16_t* k = static_cast<const uint16_t*>(k_new);
+  const uint16_t* v = static_cast<const uint16_t*>(v_new);
+  const dim3 grid((unsigned)((p.count + 31) >> 5), (unsigned)p.Hkv, (unsigned)p.batch);
+  if (D == 128) return launch((kv_append_groups_e4m3<128, true>), grid, dim3(256), 0, stream, p, u, k, v);
+  return launch((kv_append_groups_e4m3<64, true>), grid, dim3(128), 0, stream, p, u, k, v);
+}
+
 hipError_t launch_append_e4m3(const StoreParams& p, const void* k_new, const void* v_new, int D, hipStream_t stream) {
   const uint16_t* k = static_cast<const uint16_t*>(k_new);
   const uint16_t* v = static_cast<const uint16_t*>(v_new);
@@ -299,8 +353,9 @@ hipError_t launch_append_e4m3(const StoreParams& p, const void* k_new, const voi
   const int64_t ring_slots = p.tile_mask == INT32_MAX ? INT64_MAX : ((int64_t)p.tile_mask + 1) << p.z_log2;
   if (!p.t_per_seq && past_whole > first_whole && (int64_t)groups * 32 <= ring_slots) {
     const dim3 grid(groups, p.Hkv, p.batch);
-    if (D == 128) return launch(kv_append_groups_e4m3<128>, grid, dim3(256), 0, stream, p, k, v);
-    return launch(kv_append_groups_e4m3<64>, grid, dim3(128), 0, stream, p, k, v);
+    const UnpackParams none = {};
+    if (D == 128) return launch((kv_append_groups_e4m3<128, false>), grid, dim3(256), 0, stream, p, none, k, v);
+    return launch((kv_append_groups_e4m3<64, false>), grid, dim3(128), 0, stream, p, none, k, v);
   }
   const int64_t threads = (int64_t)p.batch * p.count * p.Hkv * (D / 4);
   const dim3 grid((unsigned)((threads + 255) / 256));

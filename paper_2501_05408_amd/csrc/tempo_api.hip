@@ -1449,7 +1449,8 @@ static int prefill_e4m3(const tempo_kv* kv, const void* q, const void* k_new, co
                  int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window, float scale, void* workspace,
                  size_t workspace_bytes, size_t copy_bytes, hipStream_t s, const tempo_rope* rope) {
   const size_t partials = (workspace_bytes - copy_bytes) & ~(size_t)255;
-  const auto write = [&](int32_t c0, int32_t C) {
+  // (copy: and put into a bf16 store as they are held)
+  const auto write = [&](int32_t c0, int32_t C, const UnpackParams* copy = nullptr) {
     const size_t at = (size_t)c0 * kv->num_kv_heads * kv->head_dim * 2;
     StoreParams sp = store_params(kv, batch, t + c0, nullptr, C);
     sp.src_steps = count;
@@ -1458,14 +1459,32 @@ static int prefill_e4m3(const tempo_kv* kv, const void* q, const void* k_new, co
       sp.rope_cos = rope->cos;
       sp.rope_sin = rope->sin;
     }
-    return launch_status(launch_append(sp, static_cast<const char*>(k_new) + at, static_cast<const char*>(v_new) + at, kv->head_dim, kv->dtype, s),
+    const char* const k = static_cast<const char*>(k_new) + at;
+    const char* const v = static_cast<const char*>(v_new) + at;
+    return launch_status(copy ? launch_append_copy_e4m3(sp, *copy, k, v, kv->head_dim, s) : launch_append(sp, k, v, kv->head_dim, kv->dtype, s),
                          "kv_append_block");
   };
+  const auto copy_of = [&](int32_t c0, int32_t C, bool* ring) {
+    UnpackParams u;
+    u.tiles = unpacked_tiles(kv, t + c0, C, window, ring);
+    u.tile_mask = *ring ? u.tiles - 1 : INT32_MAX;
+    char* const at = static_cast<char*>(workspace) + partials;
+    u.table = reinterpret_cast<int32_t*>(at);
+    u.k = at + align_up((size_t)batch * u.tiles * sizeof(int32_t), 256);
+    u.v = static_cast<char*>(u.k) + unpacked_pool_bytes(kv, batch, u.tiles);
+    u.first_group = (window > 0 && t + c0 - window + 1 > 0 ? t + c0 - window + 1 : 0) >> 5;
+    return u;
+  };
   int rc;
+  bool ring;
+  // all the prompt sees is its own rows: they are written into the store and the copy at once
+  const bool both = !kv->ring_blocks && t == 0 && count >= 32 && e4m3_chunk(kv, batch, Hq, t, count, window) == count &&
+                    !e4m3_by_codes(kv, Hq, t, count, window, count_per_seq);
   // a linear store takes all rows first (answers may lie over rows)
   for (int32_t c0 = 0, C; c0 < count && !kv->ring_blocks; c0 += C) {
     C = e4m3_chunk(kv, batch, Hq, t + c0, count - c0, window);
-    if ((rc = write(c0, C)) != TEMPO_OK) return rc;
+    const UnpackParams u = copy_of(c0, C, &ring);
+    if ((rc = write(c0, C, both ? &u : nullptr)) != TEMPO_OK) return rc;
   }
   for (int32_t c0 = 0, C; c0 < count; c0 += C) {
     C = e4m3_chunk(kv, batch, Hq, t + c0, count - c0, window);
@@ -1487,19 +1506,12 @@ static int prefill_e4m3(const tempo_kv* kv, const void* q, const void* k_new, co
       }
       continue;
     }
-    bool ring;
-    UnpackParams u;
-    u.tiles = unpacked_tiles(kv, t + c0, C, window, &ring);
-    u.tile_mask = ring ? u.tiles - 1 : INT32_MAX;
-    char* const at = static_cast<char*>(workspace) + partials;
-    u.table = reinterpret_cast<int32_t*>(at);
-    u.k = at + align_up((size_t)batch * u.tiles * sizeof(int32_t), 256);
-    u.v = static_cast<char*>(u.k) + unpacked_pool_bytes(kv, batch, u.tiles);
-    const int32_t lo = window > 0 && t + c0 - window + 1 > 0 ? t + c0 - window + 1 : 0;
-    u.first_group = lo >> 5;
-    const int groups = ((t + c0 + C - 1) >> 5) - (lo >> 5) + 1;
-    rc = launch_status(launch_unpack_e4m3(store_params(kv, batch, 0, nullptr), u, groups, kv->head_dim, s), "kv_unpack");
-    if (rc != TEMPO_OK) return rc;
+    const UnpackParams u = copy_of(c0, C, &ring);
+    const int groups = ((t + c0 + C - 1) >> 5) - u.first_group + 1;
+    if (!both) {
+      rc = launch_status(launch_unpack_e4m3(store_params(kv, batch, 0, nullptr), u, groups, kv->head_dim, s), "kv_unpack");
+      if (rc != TEMPO_OK) return rc;
+    }
     tempo_kv copy = *kv;
     copy.k_pool = u.k;
     copy.v_pool = u.v;

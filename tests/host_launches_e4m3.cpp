@@ -6,6 +6,12 @@ hipError_t launch_append_e4m3(const StoreParams& p, const void* k, const void* v
   return say("append t=%d count=%d steps=%d k=%zu v=%zu", p.t, p.count, p.src_steps, (size_t)k, (size_t)v);
 }
 hipError_t launch_gather_e4m3(const StoreParams&, void*, void*, int, int j0, int count, hipStream_t) { return say("gather t=%d count=%d", j0, count); }
+hipError_t launch_append_copy_e4m3(const StoreParams& p, const UnpackParams& u, const void* k, const void* v, int D, hipStream_t) {
+  say("append t=%d count=%d steps=%d k=%zu v=%zu", p.t, p.count, p.src_steps, (size_t)k, (size_t)v);
+  const int groups = (p.count + 31) >> 5;
+  return say("unpack first=%d groups=%d tiles=%d mask=%d table=%zu k=%zu v=%zu end=%zu", u.first_group, groups, u.tiles, u.tile_mask, (size_t)u.table,
+             (size_t)u.k, (size_t)u.v, (size_t)u.v + ((size_t)p.batch * u.tiles * p.Hkv << p.z_log2) * D * 2);
+}
 hipError_t launch_unpack_e4m3(const StoreParams& p, const UnpackParams& u, int groups, int D, hipStream_t) {
   return say("unpack first=%d groups=%d tiles=%d mask=%d table=%zu k=%zu v=%zu end=%zu", u.first_group, groups, u.tiles, u.tile_mask, (size_t)u.table,
              (size_t)u.k, (size_t)u.v, (size_t)u.v + ((size_t)p.batch * u.tiles * p.Hkv << p.z_log2) * D * 2);

@@ -31,6 +31,10 @@ def bf16(x):
     return torch.from_numpy(np.ascontiguousarray(x)).to(torch.bfloat16).to(DEV)
 
 
+def ints(x):
+    return torch.from_numpy(np.asarray(x).astype(np.int32)).to(DEV)
+
+
 def normal(seed, which, shape):
     return synth.normal_as(seed, which, shape, "bf16").astype(np.float64)
 
@@ -429,6 +433,42 @@ def test_prompts(Hq, Hkv, D, Z, B, t, count, window, ring, rope, counts, over_ro
             kg, vg = st.gather(first, last - first)
             np.testing.assert_array_equal(np64(kg)[b], Kh[b, first:last])
             np.testing.assert_array_equal(np64(vg)[b], Vh[b, first:last])
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,Z,B,count,window,counts", [(6, 2, 128, 64, 2, 150, 0, False), (6, 2, 64, 32, 3, 200, 0, True), (8, 2, 64, 256, 2, 301, 50, False)])
+def test_rotary_prompts_from_the_first_step_on(Hq, Hkv, D, Z, B, count, window, counts):
+    for over_rows in (False, True):
+        test_prompts(Hq, Hkv, D, Z, B, 0, count, window, 0, True, counts, over_rows)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,Z,t,count,window", [(6, 2, 128, 64, 0, 200, 0), (8, 2, 64, 32, 0, 333, 0), (6, 2, 128, 64, 0, 300, 77), (6, 2, 128, 32, 70, 150, 0),
+                                                     (8, 8, 64, 64, 0, 33, 0)])
+def test_prompts_do_not_depend_on_what_the_workspace_held(Hq, Hkv, D, Z, t, count, window):
+    """Prompts of different lengths side by side; a workspace of zeros, of NaN, and what the calls before left."""
+    own = np.array([count, 0, count // 3, 1, count - 1, 32])
+    B = len(own)
+    q, K, V = normal(57, 1, (B, count, Hq, D)), normal(57, 2, (B, t + count, Hkv, D)), normal(57, 3, (B, t + count, Hkv, D))
+    answers = []
+    ws = None
+    for fill in (0, 255, None):
+        st = make_store(57, B, Hq, Hkv, D, Z, t + count - 1)
+        if t:
+            st.append_block(bf16(K[:, :t]), bf16(V[:, :t]), 0, t)
+        need = T.tempo_prefill_workspace_bytes(st.kv, B, Hq, t + count - 1)
+        ws = torch.full((need,), fill, dtype=torch.uint8, device=DEV) if fill is not None else ws
+        out = torch.zeros((B, count, Hq, D), dtype=torch.bfloat16, device=DEV)
+        args = (B, Hq, t, count, ints(own)) + ((window,) if window else ())
+        call = T.tempo_prefill_window if window else T.tempo_prefill_causal
+        call(st.kv, bf16(q), bf16(K[:, t:]), bf16(V[:, t:]), out, *args, st.scale, ws, need)
+        answers.append(out)
+    assert all(torch.equal(a, answers[0]) for a in answers)
+    Kh, Vh = held(K), held(V)
+    for c in sorted({0, 31, 32, count // 3 - 1, count - 1}):
+        live = [b for b in range(B) if c < own[b]]
+        if live:
+            assert_attention(answers[0][live, c], q[live, c], Kh[live], Vh[live], t + c, window, D ** -0.5, f"step {c}")
+    for b in range(B):
+        assert not answers[0][b, own[b]:].any()
 
 
 @pytest.mark.parametrize("over_rows", [False, True])
