@@ -645,8 +645,9 @@ size_t tempo_attn_plan_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_
  *                           count * block_size <= 2^30 (TEMPO_ERR_SHAPE otherwise, here and above).
  *                           Workspace: 256-byte aligned, tempo_attn_selected_workspace_bytes.
  * tempo_decode_step_selected  a whole step: tempo_kv_append, tempo_block_bounds, tempo_select_blocks and
- *                           tempo_attn_selected with these arguments, and their results, in three or four
- *                           launches (write, bounds and scores are one); `selected` returns the choice.
+ *                           tempo_attn_selected with these arguments, and their results, in two to four
+ *                           launches (write, bounds and scores, for few blocks the choice too, are one);
+ *                           `selected` returns the choice.
  *                           Workspace: 256-byte aligned, tempo_step_selected_workspace_bytes.
  */
 size_t tempo_block_bounds_bytes(const tempo_kv* kv);

@@ -228,33 +228,21 @@ struct Interval {
   float lo, hi;
 };
 
-// A wavefront scores 16 blocks: lane (row + 16c) holds dims 32s + 8c .. +7 of block `row`, and of the query head that is
-// column `row` of a product.
-// kStore: of a whole step, whose row is written, and its block's bounds if it completes it, by the first workgroup of
-// every (sequence, kv head): no score reads either, as the newest block is chosen anyway (0: neither; 1: bf16 store; 2: 8-bit).
-template <int D, int kStore>
-__global__ __launch_bounds__(256) void score_blocks(ChooseParams p, StoreParams store, const void* __restrict__ k_new, const void* __restrict__ v_new) {
+// A wavefront scores 16 blocks, n0 .. n0+15, of those up to newest - last: lane (row + 16c) holds dims 32s + 8c .. +7 of block
+// `row` (phys: its number in the pool), and of the query head that is column `row` of a product.  Lanes row < 4 return the
+// interval of block n0 + 4c + row, as a word.
+template <int D>
+__device__ __forceinline__ uint64_t score_sixteen(const ChooseParams& p, int b, int hkv, int n0, int newest, int& phys) {
   constexpr int KS = D / 32;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, c = lane >> 4;
-  const int hkv = blockIdx.y, b = blockIdx.z;
-  int part = blockIdx.x;
-  if constexpr (kStore != 0) {
-    if (part == 0) {
-      write_and_bound<D, kStore == 2>(store, k_new, v_new, static_cast<uint16_t*>(p.bounds), b, hkv);
-      return;
-    }
-    --part;
-  }
-  const int newest = step_of(p.t_per_seq, p.t, b) >> p.z_log2;
-  const int n0 = (part * 4 + wave) * 16;
-  if (newest < p.pick || n0 > newest - p.last) return;  // all blocks are taken; or only blocks that are taken anyway
+  const int lane = threadIdx.x & 63, row = lane & 15, c = lane >> 4;
   const int n = n0 + row <= newest - p.last ? n0 + row : n0;
-  const int phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
+  phys = clamp_block(p.block_table[(int64_t)b * p.max_blocks_per_seq + n], p.num_blocks);
   const uint16_t* const at = static_cast<const uint16_t*>(p.bounds) + ((int64_t)phys * p.Hkv + hkv) * 2 * D + 8 * c;
   const uint16_t* const q = static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D + 8 * c;
   u32x4 x[KS];  // of the first 16 heads; asked for before the bounds, which wait for the table (16 sequences of 512 blocks: 14.9 -> 14.5 us)
 #pragma unroll
   for (int s = 0; s < KS; ++s) x[s] = *reinterpret_cast<const u32x4*>(q + (int64_t)(row < p.G ? row : p.G - 1) * D + 32 * s);
+  __builtin_amdgcn_sched_barrier(0);  // (or the scheduler puts them behind)
   u32x4 lo[KS], hi[KS], far[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
@@ -308,11 +296,32 @@ __global__ __launch_bounds__(256) void score_blocks(ChooseParams p, StoreParams 
     low[r] = row_maximum(low[r]);
     high[r] = row_maximum(high[r]);
   }
-  const int mine = n0 + 4 * c + row;  // lanes row < 4 write one block each
   const float l = row == 0 ? low[0] : row == 1 ? low[1] : row == 2 ? low[2] : low[3];
   const float u = row == 0 ? high[0] : row == 1 ? high[1] : row == 2 ? high[2] : high[3];
-  if (row < 4 && mine <= newest - p.last)
-    p.scores[((int64_t)b * p.Hkv + hkv) * p.tiles + mine] = (uint64_t)__builtin_bit_cast(uint32_t, u) << 32 | __builtin_bit_cast(uint32_t, l);
+  return (uint64_t)__builtin_bit_cast(uint32_t, u) << 32 | __builtin_bit_cast(uint32_t, l);
+}
+
+// kStore: of a whole step, whose row is written, and its block's bounds if it completes it, by the first workgroup of
+// every (sequence, kv head): no score reads either, as the newest block is chosen anyway (0: neither; 1: bf16 store; 2: 8-bit).
+template <int D, int kStore>
+__global__ __launch_bounds__(256) void score_blocks(ChooseParams p, StoreParams store, const void* __restrict__ k_new, const void* __restrict__ v_new) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15;
+  const int hkv = blockIdx.y, b = blockIdx.z;
+  int part = blockIdx.x;
+  if constexpr (kStore != 0) {
+    if (part == 0) {
+      write_and_bound<D, kStore == 2>(store, k_new, v_new, static_cast<uint16_t*>(p.bounds), b, hkv);
+      return;
+    }
+    --part;
+  }
+  const int newest = step_of(p.t_per_seq, p.t, b) >> p.z_log2;
+  const int n0 = (part * 4 + wave) * 16;
+  if (newest < p.pick || n0 > newest - p.last) return;  // all blocks are taken; or only blocks that are taken anyway
+  int phys;
+  const uint64_t word = score_sixteen<D>(p, b, hkv, n0, newest, phys);
+  const int mine = n0 + 4 * (lane >> 4) + row;
+  if (row < 4 && mine <= newest - p.last) p.scores[((int64_t)b * p.Hkv + hkv) * p.tiles + mine] = word;
 }
 
 // Bits of a score in an order that whole numbers share; NaN above all, 0 below all.
@@ -380,9 +389,10 @@ __device__ inline void find_part(const int* bins, int wanted, int* found) {
   }
 }
 
-// Score of block `phys` of the pool in 64 bits, by 16 lanes, in all of them.  ahead: the group's first kHeads query heads.
+// Score of block `phys` of the pool in 64 bits for the heads first, first + step, ..., by 16 lanes, in all of them.  ahead: the
+// group's first kHeads query heads.
 template <int D>
-__device__ inline uint64_t exact_key(const ChooseParams& p, const uint16_t* ahead, int b, int hkv, int phys) {
+__device__ inline uint64_t exact_key(const ChooseParams& p, const uint16_t* ahead, int b, int hkv, int phys, int first = 0, int step = 1) {
   const int d = 8 * (threadIdx.x & 15);
   const bool live = d < D;
   const uint16_t* const at = static_cast<const uint16_t*>(p.bounds) + ((int64_t)clamp_block(phys, p.num_blocks) * p.Hkv + hkv) * 2 * D + (live ? d : 0);
@@ -391,7 +401,7 @@ __device__ inline uint64_t exact_key(const ChooseParams& p, const uint16_t* ahea
   unpack8(*reinterpret_cast<const u32x4*>(at), l);
   unpack8(*reinterpret_cast<const u32x4*>(at + D), h);
   uint64_t best = 0;
-  for (int g = 0; g < p.G; ++g) {
+  for (int g = first; g < p.G; g += step) {
     float x[8];
     unpack8(g < kHeads ? *reinterpret_cast<const u32x4*>(ahead + g * D + (live ? d : 0)) : *reinterpret_cast<const u32x4*>(q + (int64_t)g * D), x);
     double sum = 0.0;
@@ -486,11 +496,19 @@ __device__ void search_border(ChooseShared& sh, Key key_at, int lo, int hi, int 
   }
 }
 
-template <int D>
-__global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
+// kScore: few blocks, which the workgroup scores itself; with kStore (score_blocks) as many workgroups more write the rows.
+template <int D, bool kScore, int kStore>
+__global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p, StoreParams store, const void* __restrict__ k_new, const void* __restrict__ v_new) {
   __shared__ ChooseShared sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int hkv = blockIdx.x, b = blockIdx.y;
+  const int b = blockIdx.y;
+  int hkv = blockIdx.x;
+  if constexpr (kStore != 0) {
+    if (hkv >= p.Hkv) {
+      write_and_bound<D, kStore == 2>(store, k_new, v_new, static_cast<uint16_t*>(p.bounds), b, hkv - p.Hkv);
+      return;
+    }
+  }
   const int newest = step_of(p.t_per_seq, p.t, b) >> p.z_log2;
   const int64_t pair = (int64_t)b * p.Hkv + hkv;
   uint64_t* const scores = p.scores + pair * p.tiles;
@@ -504,7 +522,7 @@ __global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
     reinterpret_cast<u32x4*>(sh.q)[i] = reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(p.q) + ((int64_t)b * p.Hq + (int64_t)hkv * p.G) * D)[i];
   const int lo = p.first, hi = newest - p.last;     // candidates
   const int wanted = p.pick - p.first - p.last;     // of them; fewer than there are
-  const bool cached = hi - lo < kCached;
+  const bool cached = kScore || hi - lo < kCached;
   auto word_at = [&](int n) { return cached ? sh.cache[n - lo] : scores[n]; };
   auto phys_at = [&](int n) { return cached ? sh.phys[n - lo] : table[n]; };
   auto interval = [&](uint64_t w) {
@@ -518,10 +536,20 @@ __global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
   auto sure = [&](uint64_t w) { return key_of(interval(w).lo) > sure_above; };
   auto undecided = [&](uint64_t w) { return key_of(interval(w).hi) >= open_from && key_of(interval(w).lo) <= sure_above; };
   if (wanted > 0) {
+    if constexpr (kScore) {
+      for (int n0 = 16 * wave; n0 <= hi; n0 += 16 * kWaves) {
+        int phys;
+        const uint64_t word = score_sixteen<D>(p, b, hkv, n0, newest, phys);
+        const int row = lane & 15, mine = n0 + 4 * (lane >> 4) + row;
+        if (row < 4 && mine >= lo && mine <= hi) sh.cache[mine - lo] = word;
+        if (lane < 16 && n0 + lane >= lo && n0 + lane <= hi) sh.phys[n0 + lane - lo] = phys;
+      }
+      __syncthreads();
+    }
     float bottom = -INFINITY, top = -INFINITY;  // the largest finite -L and U
     for (int n = lo + tid; n <= hi; n += kChoose) {
-      const uint64_t w = scores[n];
-      if (cached) {
+      const uint64_t w = kScore ? sh.cache[n - lo] : scores[n];
+      if (!kScore && cached) {
         sh.cache[n - lo] = w;
         sh.phys[n - lo] = table[n];
       }
@@ -537,6 +565,7 @@ __global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
     }
     sh.bins[0][tid] = sh.bins[1][tid] = 0;
     if (tid == 0) sh.left = sh.sure = 0;
+    if (tid < kRanked) sh.ranked_key[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
@@ -587,9 +616,13 @@ __global__ __launch_bounds__(kChoose) void choose_blocks(ChooseParams p) {
       by_key = true;
       search_border(sh, word_at, lo, hi, wanted, cut, cut_at);
     } else if (open != open_taken) {
-      for (int i = tid >> 4; i < open; i += kChoose / 16) {
-        const uint64_t key = exact_key<D>(p, sh.q, b, hkv, phys_at(sh.ranked_at[i]));
-        if ((lane & 15) == 0) sh.ranked_key[i] = key;
+      // a block's heads are shared out among as many groups of 16 lanes as there are (64 heads, 4 sequences of 192 blocks: 24.6 -> 12 us)
+      const int share = open <= 2 ? 16 : open <= 4 ? 8 : open <= 8 ? 4 : open <= 16 ? 2 : 1;
+      for (int i = tid >> 4; i < open * share; i += kChoose / 16) {
+        const int at = i / share, first = i % share;
+        if (first >= p.G) continue;
+        const uint64_t key = exact_key<D>(p, sh.q, b, hkv, phys_at(sh.ranked_at[at]), first, share);
+        if ((lane & 15) == 0) atomicMax(reinterpret_cast<unsigned long long*>(&sh.ranked_key[at]), (unsigned long long)key);
       }
       __syncthreads();
       if (tid < open) {
@@ -646,26 +679,38 @@ hipError_t launch_block_bounds(const StoreParams& p, void* bounds, int D, int dt
   return launch((block_bounds<64, false>), grid, dim3(128), 0, stream, p, to);
 }
 
-// k_new, v_new: null, or the rows of the step, which are written (and bounded) by the same launch.
+// Does the workgroup that chooses also score, a launch less?  It streams the bounds of its blocks alone, so they must be few (us, two
+// launches / one, 24/8 heads of 128: 1 sequence of 16 blocks 8.5 / 6.2, 128 blocks 8.6 / 7.4, 192 blocks 8.4 / 8.6, 512 blocks 9.4 / 15;
+// 16 sequences of 192 blocks 11.0 / 9.4; 64/1 heads, 4 sequences of 80 blocks 10.2 / 8.9, 192 blocks 12 / 14); and with rows to write,
+// whose workgroups are as many more and as large, the pairs too (steps of 64 sequences of 192 blocks 55 / 59).
+inline bool scores_itself(const ChooseParams& p, int batch, bool writes) {
+  return p.tiles <= (p.G <= kHeads ? 192 : 96) && !(writes && (int64_t)batch * p.Hkv > 256);
+}
+
+// k_new, v_new: null, or the rows of the step, which are written (and bounded) by the first launch.
 template <int D, int kStore>
-static hipError_t launch_score(const ChooseParams& p, const StoreParams& store, const void* k_new, const void* v_new, int batch, hipStream_t stream) {
+static hipError_t launch_select(const ChooseParams& p, const StoreParams& store, const void* k_new, const void* v_new, int batch, hipStream_t stream) {
   // (no sequence has more blocks than are taken: nothing to score)
   const int parts = p.tiles > p.pick && p.pick > p.first + p.last ? (p.tiles + 63) / 64 : 0;
+  if (scores_itself(p, batch, kStore != 0)) {
+    const dim3 grid((unsigned)(p.Hkv * (kStore != 0 ? 2 : 1)), (unsigned)batch);
+    return launch((choose_blocks<D, true, kStore>), grid, dim3(kChoose), 0, stream, p, store, k_new, v_new);
+  }
   const int workgroups = parts + (kStore != 0 ? 1 : 0);
-  if (workgroups == 0) return hipSuccess;
-  return launch((score_blocks<D, kStore>), dim3((unsigned)workgroups, (unsigned)p.Hkv, (unsigned)batch), dim3(256), 0, stream, p, store, k_new, v_new);
+  if (workgroups > 0) {
+    const dim3 grid((unsigned)workgroups, (unsigned)p.Hkv, (unsigned)batch);
+    const hipError_t e = launch((score_blocks<D, kStore>), grid, dim3(256), 0, stream, p, store, k_new, v_new);
+    if (e != hipSuccess) return e;
+  }
+  return launch((choose_blocks<D, false, 0>), dim3((unsigned)p.Hkv, (unsigned)batch), dim3(kChoose), 0, stream, p, store, nullptr, nullptr);
 }
 
 hipError_t launch_select_blocks(const ChooseParams& p, const StoreParams* store, const void* k_new, const void* v_new, int batch, int D, int dtype,
                                 hipStream_t stream) {
   const StoreParams none = {};
-  hipError_t e;
-  if (!store) e = D == 128 ? launch_score<128, 0>(p, none, nullptr, nullptr, batch, stream) : launch_score<64, 0>(p, none, nullptr, nullptr, batch, stream);
-  else if (dtype == TEMPO_E4M3) e = D == 128 ? launch_score<128, 2>(p, *store, k_new, v_new, batch, stream) : launch_score<64, 2>(p, *store, k_new, v_new, batch, stream);
-  else e = D == 128 ? launch_score<128, 1>(p, *store, k_new, v_new, batch, stream) : launch_score<64, 1>(p, *store, k_new, v_new, batch, stream);
-  if (e != hipSuccess) return e;
-  const dim3 pairs((unsigned)p.Hkv, (unsigned)batch);
-  return D == 128 ? launch(choose_blocks<128>, pairs, dim3(kChoose), 0, stream, p) : launch(choose_blocks<64>, pairs, dim3(kChoose), 0, stream, p);
+  if (!store) return D == 128 ? launch_select<128, 0>(p, none, nullptr, nullptr, batch, stream) : launch_select<64, 0>(p, none, nullptr, nullptr, batch, stream);
+  if (dtype == TEMPO_E4M3) return D == 128 ? launch_select<128, 2>(p, *store, k_new, v_new, batch, stream) : launch_select<64, 2>(p, *store, k_new, v_new, batch, stream);
+  return D == 128 ? launch_select<128, 1>(p, *store, k_new, v_new, batch, stream) : launch_select<64, 1>(p, *store, k_new, v_new, batch, stream);
 }
 
 }  // namespace tempo

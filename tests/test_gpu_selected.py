@@ -353,6 +353,30 @@ def test_a_prompt_and_steps(dtype, Hq, Hkv, D, Z, B, prompt, steps, count, first
 
 
 @pytest.mark.parametrize("dtype", STORES)
+@pytest.mark.parametrize("Hq,Hkv,D,Z,B,t,count,first,last,ragged",
+                         [(6, 2, 128, 32, 2, 32 * 192 - 1, 9, 1, 2, False), (6, 2, 128, 32, 2, 32 * 193 - 1, 9, 1, 2, False), (8, 2, 64, 32, 3, 7000, 40, 1, 2, True),
+                          (20, 1, 64, 32, 2, 32 * 96 - 1, 7, 1, 1, False), (20, 1, 64, 32, 2, 32 * 97 - 1, 7, 1, 1, False), (16, 8, 64, 32, 32, 200, 3, 1, 2, True),
+                          (16, 8, 64, 32, 33, 200, 3, 1, 2, True), (2, 2, 128, 64, 2, 63, 1, 0, 1, False), (6, 2, 128, 32, 1, 319, 5, 2, 3, False),
+                          (128, 1, 128, 32, 2, 1999, 6, 0, 1, False)])
+def test_a_step_is_its_parts(dtype, Hq, Hkv, D, Z, B, t, count, first, last, ragged):
+    """The bits of the calls one by one: rows, bounds, choice and answers."""
+    one, q, K, V = filled(35, dtype, B, Hq, Hkv, D, Z, t)
+    two, *_ = filled(35, dtype, B, Hq, Hkv, D, Z, t)
+    steps = ints(np.where(np.arange(B) % 3 == 1, (synth.integers(35, 9, B, 0, t) + 1) // Z * Z + Z - 1, synth.integers(35, 9, B, 0, t))) if ragged else None
+    k, v = bf16(normal(35, 7, (B, Hkv, D))), bf16(normal(35, 8, (B, Hkv, D)))
+    a, b = random_bounds(one, 35), random_bounds(two, 35)
+    lists = torch.empty((B, Hkv, count), dtype=torch.int32, device=DEV)
+    out = one.step_selected(a, bf16(q), k, v, one.new_out(), t, count, first, last, steps, selected=lists)
+    two.append(k, v, t, steps)
+    two.update_bounds(b, t, 1, steps)
+    chosen = two.select_blocks(b, bf16(q), t, count, first, last, steps)
+    assert torch.equal(lists, chosen) and torch.equal(out, two.attend_selected(bf16(q), two.new_out(), chosen, t, steps))
+    for x, y in ((one.k_pool, two.k_pool), (one.v_pool, two.v_pool), (a, b)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    assert (np.sort(lists.cpu().numpy(), axis=-1) == lists.cpu().numpy()).all() or t // Z < count or ragged
+
+
+@pytest.mark.parametrize("dtype", STORES)
 def test_captured_and_replayed_and_two_streams(dtype):
     Hq, Hkv, D, Z, B, t, count = 24, 8, 128, 64, 2, 4095, 8
     st, q, K, V = filled(33, dtype, B, Hq, Hkv, D, Z, t)
