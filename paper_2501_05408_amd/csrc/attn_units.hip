@@ -114,17 +114,18 @@ __device__ __forceinline__ float high_of(uint32_t pair) { return __builtin_bit_c
 constexpr float kUnseen = -3e38f;  // reference of a column that has seen no key: finite, so that masked logits of -inf get the weight 0
 
 // Online-softmax update of a column's reference, sum and accumulators, and the group's weights, 2^(x scale - reference) in bf16,
-// as four words of two.  The sum is that of the rounded weights.  The reference is set 2^kSlack above a maximum that exceeds
-// it, the first one's above all, so weights are at most 1 and the accumulators are hardly ever rescaled.  (That, the scale inside
-// the exponent and values masked only where a range cuts their group, us: 48 ragged sequences of 32/8 heads of 64, window 1000
-// 12.45 -> 12.05; 32 sequences of 1000 keys, 24/8 heads of 128 12.1 -> 11.5; 16 of 4000, 63 and 126 columns 38 -> 34, 70 -> 61.)
-template <int D>
+// as four words of two.  The sum is that of the rounded weights.  The reference is 2^kSlack above the maximum so far, so that sums
+// of a few hundred of the largest values stay finite; wavefronts of two tiles keep an older one until a logit exceeds it, and
+// hardly ever rescale their accumulators (16 sequences of 4000 keys, 63 and 126 columns 39 -> 34 and 70 -> 62 us; one tile gains
+// 1% at most, and loses a tenth of its accuracy, since the largest weight is a power of two only under its own reference).
+template <int D, bool kKeep>
 __device__ __forceinline__ u32x4 softmax_weights(const float* x, float scale, int lane, WaveState<D>& st) {
   float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
   mx = column_max(mx) * scale;
-  const bool above = mx > st.m;
+  const float top = mx + kSlack;
+  const bool above = (kKeep ? mx : top) > st.m;
   if (__any(above && st.m != kUnseen)) {
-    const float alpha = above ? fast_exp2(st.m - (mx + kSlack)) : 1.f;
+    const float alpha = above ? fast_exp2(st.m - top) : 1.f;
     float a[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) a[r] = __shfl(alpha, 4 * (lane >> 4) + r);
@@ -135,7 +136,7 @@ __device__ __forceinline__ u32x4 softmax_weights(const float* x, float scale, in
       for (int r = 0; r < 4; ++r) st.acc[dt][r] *= a[r];
     }
   }
-  st.m = above ? mx + kSlack : st.m;
+  st.m = above ? top : st.m;
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -411,7 +412,7 @@ __global__ __launch_bounds__(512, D == 64 && CT == 2 ? 4 : 1) void attn_units(Se
     }
     u32x4 w[CT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) w[ct] = softmax_weights<D>(x[ct], p.scale_log2e, lane, st[ct]);
+    for (int ct = 0; ct < CT; ++ct) w[ct] = softmax_weights<D, (CT > 1)>(x[ct], p.scale_log2e, lane, st[ct]);
     if constexpr (k8 && !kSelect) {
       if (key == key_new) patch_values<D>(t_b, lane, stage, g);
     }
