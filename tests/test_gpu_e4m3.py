@@ -544,3 +544,30 @@ def test_captured_and_replayed_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
+
+
+@pytest.mark.parametrize("t,count,window", [(0, 200, 0), (300, 100, 0), (2500, 60, 0), (0, 300, 70)])
+def test_prompts_captured_and_replayed(t, count, window):
+    """Rows written and laid out at once; turned by a launch of their own; two blocks over the codes.  Other rows and queries on
+    every replay, another prompt and its own eager run in between."""
+    Hq, Hkv, D, Z, B = 6, 2, 128, 64, 2
+    st, other = make_store(63, B, Hq, Hkv, D, Z, t + count - 1), make_store(64, B, Hq, Hkv, D, Z, t + count - 1)
+    if t:
+        before = bf16(normal(63, 1, (B, t, Hkv, D)))
+        st.append_block(before, before, 0, t), other.append_block(before, before, 0, t)
+    q, k, v = bf16(normal(63, 2, (B, count, Hq, D))), bf16(normal(63, 3, (B, count, Hkv, D))), bf16(normal(63, 4, (B, count, Hkv, D)))
+    out, eager = torch.empty_like(q), torch.empty_like(q)
+    st.prefill_attend(q, k, v, out, t, count, window)  # (the workspace is there before the capture)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        st.prefill_attend(q, k, v, out, t, count, window)
+    for i in range(4):
+        for x, which in ((q, 5), (k, 6), (v, 7)):
+            x.copy_(bf16(normal(70 + i, which, x.shape)))
+        other.prefill_attend(q, k, v, eager, t, count, window)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+        assert all(torch.equal(a, b) for a, b in zip(st.gather(t, count), other.gather(t, count)))

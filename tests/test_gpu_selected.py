@@ -405,3 +405,40 @@ def test_captured_and_replayed_and_two_streams(dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager) and torch.equal(chosen, selected)
+
+
+@pytest.mark.parametrize("dtype", STORES)
+@pytest.mark.parametrize("t0", [32 * 192 - 4, 90])
+def test_a_captured_step_at_every_sequences_own_position(dtype, t0):
+    """One capture for many steps: the positions are read from the device; blocks are completed on the way, and the number of blocks
+    that the launch is made for lies on either side of what one workgroup scores itself."""
+    Hq, Hkv, D, Z, B, steps, count = 6, 2, 64, 32, 3, 8, 4
+    most = t0 + steps
+    K, V, q = normal(36, 2, (B, most, Hkv, D)), normal(36, 3, (B, most, Hkv, D)), normal(36, 1, (steps, B, Hq, D))
+    st, other = make_store(36, dtype, B, Hq, Hkv, D, Z, most + 40), make_store(36, dtype, B, Hq, Hkv, D, Z, most + 40)
+    a, b = st.new_bounds(), other.new_bounds()
+    lengths = np.array([t0, t0 // 2, 3])
+    for s, bounds in ((st, a), (other, b)):
+        s.append_block(bf16(K[:, :t0]), bf16(V[:, :t0]), 0, t0)
+        s.update_bounds(bounds, 0, t0, count_per_seq=ints(lengths))
+    at, qd = ints(lengths), bf16(q[0])
+    k, v = torch.empty((B, Hkv, D), dtype=torch.bfloat16, device=DEV), torch.empty((B, Hkv, D), dtype=torch.bfloat16, device=DEV)
+    out, chosen, selected = st.new_out(), torch.empty((B, Hkv, count), dtype=torch.int32, device=DEV), torch.empty((B, Hkv, count), dtype=torch.int32, device=DEV)
+    need = T.tempo_step_selected_workspace_bytes(st.kv, B, Hq, most + 40, count)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        T.tempo_decode_step_selected(st.kv, a, qd, k, v, out, chosen, count, 1, 1, B, Hq, most + 40, at, st.scale, ws, need)
+    for i in range(steps):
+        now = lengths + i
+        at.copy_(ints(now)), qd.copy_(bf16(q[i]))
+        k.copy_(bf16(K[np.arange(B), now])), v.copy_(bf16(V[np.arange(B), now]))
+        graph.replay()
+        eager = other.step_selected(b, qd, k, v, other.new_out(), int(now.max()), count, 1, 1, ints(now), selected=selected)
+        torch.cuda.synchronize()
+        assert torch.equal(chosen, selected)
+        err = np.abs(np64(out) - np64(eager))  # (another plan: another order of fp32 sums, and weights rounded under other references)
+        assert (err <= 2 * 1.03 * 2.0 ** -8 * (np.abs(np64(eager)) * 2 + 4)).all()
+    for x, y in ((st.k_pool, other.k_pool), (st.v_pool, other.v_pool)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
