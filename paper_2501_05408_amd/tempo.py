@@ -210,9 +210,10 @@ def load():
 def _ptr(x):
     if x is None:
         return None
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr()
-    return int(x)
+    except AttributeError:
+        return int(x)
 
 
 _raw_stream = None
@@ -225,8 +226,10 @@ def _stream(stream):
         if _raw_stream is None:
             import torch
             fast = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-            if fast is not None:
-                _raw_stream = lambda: fast(torch.cuda.current_device())
+            device = getattr(torch._C, "_cuda_getDevice", None)
+            if fast is not None and device is not None:
+                torch.cuda.current_device()  # (initialises torch's side; what it asks after that is asked directly)
+                _raw_stream = lambda: fast(device())
             else:
                 _raw_stream = lambda: torch.cuda.current_stream().cuda_stream
         return _raw_stream()
