@@ -225,19 +225,25 @@ class BlockStore:
         T.tempo_block_bounds(self.kv, bounds, self.batch, t, t_per_seq, count, count_per_seq)
 
     def _selected_ws(self, nbytes):
+        """A workspace of at least `nbytes`, which the callers size for the store's last step, so that a loop over steps has one.
+        A larger one (for a longer list) is at least twice the last: smaller ones are kept, as a captured graph may hold their
+        address, and all of them together are less than twice the largest."""
         if nbytes == 0:
             raise T.TempoError(T.TEMPO_ERR_SHAPE, "workspace of the attention over selected blocks")
-        if getattr(self, "_sel_ws", None) is None or self._sel_ws[-1].numel() < nbytes:
-            # (smaller ones are kept: a captured graph may hold their address)
-            self._sel_ws = getattr(self, "_sel_ws", None) or []
-            self._sel_ws.append(torch.empty(nbytes, dtype=torch.uint8, device=self.device))
-        return self._sel_ws[-1], self._sel_ws[-1].numel()
+        kept = self.__dict__.setdefault("_sel_ws", [])
+        if not kept or kept[-1].numel() < nbytes:
+            size = max(nbytes, 2 * kept[-1].numel()) if kept else nbytes
+            kept.append(torch.empty(size, dtype=torch.uint8, device=self.device))
+        return kept[-1], kept[-1].numel()
+
+    def _last_step(self):
+        return min(self.max_t, 2 ** 31 - 65)  # the library takes no later one
 
     def select_blocks(self, bounds, q, t, count, first=1, last=1, t_per_seq=None, selected=None):
         """The `count` blocks that step t of every (sequence, kv head) attends over, int32 [batch][Hkv][count]."""
         if selected is None:
             selected = torch.empty((self.batch, self.Hkv, count), dtype=torch.int32, device=self.device)
-        ws, nbytes = self._selected_ws(T.tempo_select_workspace_bytes(self.kv, self.batch, self.Hq, t))
+        ws, nbytes = self._selected_ws(T.tempo_select_workspace_bytes(self.kv, self.batch, self.Hq, self._last_step()))
         T.tempo_select_blocks(self.kv, bounds, q, selected, count, first, last, self.batch, self.Hq, t, t_per_seq, ws, nbytes)
         return selected
 
@@ -254,7 +260,7 @@ class BlockStore:
         """Append step t, keep the bounds, choose `count` blocks and attend over them."""
         if selected is None:
             selected = torch.empty((self.batch, self.Hkv, count), dtype=torch.int32, device=self.device)
-        ws, nbytes = self._selected_ws(T.tempo_step_selected_workspace_bytes(self.kv, self.batch, self.Hq, t, count))
+        ws, nbytes = self._selected_ws(T.tempo_step_selected_workspace_bytes(self.kv, self.batch, self.Hq, self._last_step(), count))
         T.tempo_decode_step_selected(self.kv, bounds, q, k_new, v_new, out, selected, count, first, last, self.batch,
                                      self.Hq, t, t_per_seq, self.scale if scale is None else scale, ws, nbytes)
         return out
