@@ -168,26 +168,33 @@ class BlockStore:
         """Write steps t .. t+count-1 with the keys rotated to their own positions on the way in."""
         T.tempo_rope_kv_append_block(self.kv, self.rope, k_raw, v_new, self.batch, t, t_per_seq, count)
 
+    def _kept_ws(self, name, nbytes, most=None):
+        """A workspace of at least `nbytes`.  A larger one is at least twice the last (but no more than `most()`, what any call can
+        need): smaller ones are kept, as a captured graph may hold their address, and are together less than twice the largest."""
+        kept = self.__dict__.setdefault(name, [])
+        if not kept or kept[-1].numel() < nbytes:
+            size = 2 * kept[-1].numel() if kept else 0
+            size = max(nbytes, size if most is None else min(size, most()))
+            kept.append(torch.empty(size, dtype=torch.uint8, device=self.device))
+        return kept[-1]
+
     def attend_block(self, q, out, t, queries, window=0, t_per_seq=None, scale=None, rope=False):
         """Steps t .. t+queries-1 in one call; q, out are [batch][queries][Hq][D].  With rope=True the
         queries arrive unrotated (set_rope tables)."""
         ws_t = self.ring_blocks * self.Z + 32 if self.ring_blocks else self.max_t
         nbytes = T.tempo_attn_block_workspace_bytes(self.kv, self.batch, self.Hq, queries, ws_t)
-        if getattr(self, "_block_ws", None) is None or self._block_ws.numel() < nbytes:
-            self._block_ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        ws = self._kept_ws("_block_ws", nbytes, lambda: T.tempo_attn_block_workspace_bytes(
+            self.kv, self.batch, self.Hq, 128 // (self.Hq // self.Hkv), ws_t))
         s = self.scale if scale is None else scale
         if rope and window:
             T.tempo_rope_attn_block_window(self.kv, self.rope, q, out, self.batch, self.Hq, queries, t, t_per_seq,
-                                           window, s, self._block_ws, nbytes)
+                                           window, s, ws, nbytes)
         elif rope:
-            T.tempo_rope_attn_block_causal(self.kv, self.rope, q, out, self.batch, self.Hq, queries, t, t_per_seq, s,
-                                           self._block_ws, nbytes)
+            T.tempo_rope_attn_block_causal(self.kv, self.rope, q, out, self.batch, self.Hq, queries, t, t_per_seq, s, ws, nbytes)
         elif window:
-            T.tempo_attn_block_window(self.kv, q, out, self.batch, self.Hq, queries, t, t_per_seq, window, s,
-                                      self._block_ws, nbytes)
+            T.tempo_attn_block_window(self.kv, q, out, self.batch, self.Hq, queries, t, t_per_seq, window, s, ws, nbytes)
         else:
-            T.tempo_attn_block_causal(self.kv, q, out, self.batch, self.Hq, queries, t, t_per_seq, s,
-                                      self._block_ws, nbytes)
+            T.tempo_attn_block_causal(self.kv, q, out, self.batch, self.Hq, queries, t, t_per_seq, s, ws, nbytes)
         return out
 
     def prefill_attend(self, q, k_new, v_new, out, t, count, window=0, scale=None, count_per_seq=None,
@@ -225,16 +232,11 @@ class BlockStore:
         T.tempo_block_bounds(self.kv, bounds, self.batch, t, t_per_seq, count, count_per_seq)
 
     def _selected_ws(self, nbytes):
-        """A workspace of at least `nbytes`, which the callers size for the store's last step, so that a loop over steps has one.
-        A larger one (for a longer list) is at least twice the last: smaller ones are kept, as a captured graph may hold their
-        address, and all of them together are less than twice the largest."""
+        """(The callers size it for the store's last step, so that a loop over steps has one.)"""
         if nbytes == 0:
             raise T.TempoError(T.TEMPO_ERR_SHAPE, "workspace of the attention over selected blocks")
-        kept = self.__dict__.setdefault("_sel_ws", [])
-        if not kept or kept[-1].numel() < nbytes:
-            size = max(nbytes, 2 * kept[-1].numel()) if kept else nbytes
-            kept.append(torch.empty(size, dtype=torch.uint8, device=self.device))
-        return kept[-1], kept[-1].numel()
+        ws = self._kept_ws("_sel_ws", nbytes)
+        return ws, ws.numel()
 
     def _last_step(self):
         return min(self.max_t, 2 ** 31 - 65)  # the library takes no later one

@@ -76,3 +76,11 @@ def test_rings_are_refused(calls):
         with pytest.raises(T.TempoError):
             call()
     assert not calls
+
+
+def test_a_wider_block_leaves_the_workspace_of_a_narrower_one(calls):
+    st = make_store(1000)
+    for queries in (1, 2, 1, 7, 42, 3):
+        st.attend_block(None, None, 5, queries)
+    need = T.tempo_attn_block_workspace_bytes(st.kv, 2, 6, 42, 1000)
+    assert sum(held(calls)) < 4 * need
