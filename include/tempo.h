@@ -526,8 +526,9 @@ int tempo_rope_prefill_window(const tempo_kv* kv, const tempo_rope* rope, const 
  * only; 0 on unsupported arguments): 2 when the prompt's query blocks fill the part
  * (bf16, linear store: one block-store write, then one launch in which every workgroup
  * walks the whole key range of its (step, head) columns through LDS and writes `out`
- * directly), 3 on fp32 linear stores, 4 on e4m3 ones (3 for one block, 5 for two), else 3 (e4m3: 4)
- * per block of 128 / (num_q_heads / num_kv_heads) steps. */
+ * directly), 3 on fp32 linear stores, 4 on e4m3 ones (3 for one block, 5 for two), else 3 (e4m3: 5)
+ * per block of 128 / (num_q_heads / num_kv_heads) steps (a single e4m3 block: 3), and on ring stores 2
+ * more for several blocks, which copy the rows where answers lie over rows that are still to be read. */
 int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t count);
 
 /* Workspace bound for tempo_prefill_* calls whose last step is at most max_t (host only). */

@@ -1690,7 +1690,10 @@ int tempo_prefill_launches(const tempo_kv* kv, int32_t batch, int32_t num_q_head
     if (kv->dtype != TEMPO_BF16) return 3;
     if (prompt_fills_part(kv, batch, G, count)) return 2;  // one launch, and no key range is split
   }
-  return (kv->dtype == TEMPO_E4M3 ? 4 : 3) * ((count + block - 1) / block);
+  // A ring store's prompt goes by chunks, of at least a block each but the last; several may read a copy of the rows.  8 bits: a chunk
+  // of one block 3, of two over the codes 5, of more 4.
+  if (kv->dtype == TEMPO_E4M3 && count <= block) return 3;
+  return (kv->dtype == TEMPO_E4M3 ? 5 : 3) * ((count + block - 1) / block) + (kv->ring_blocks && count > block ? 2 : 0);
 }
 
 size_t tempo_prefill_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t) {

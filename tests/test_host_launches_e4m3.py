@@ -258,3 +258,32 @@ def test_launches_of_a_sparse_step(lib):
     # nothing is launched by a step that is refused
     assert lib.tempo_decode_step_selected(ctypes.byref(kv), AT, AT, AT, AT, AT, AT, 32, 1, 2, 2, 24, 65535, None, 0.1, AT, nbytes - 1, None) == T.TEMPO_ERR_WORKSPACE
     assert not taken(lib)
+
+
+def assert_within_the_launches_promised(lib, kv, batch, Hq, t, count, window, out):
+    rows = 1 << 44
+    rc, launches = prefill(lib, kv, batch, Hq, t, count, window, nbytes=1 << 46, rows=rows, out=out)
+    assert rc == T.TEMPO_OK
+    bound = lib.tempo_prefill_launches(ctypes.byref(kv), batch, Hq, count)
+    assert len(launches) <= bound, (kv.dtype, kv.ring_blocks, batch, Hq, t, count, window, [n for n, _ in launches], bound)
+    return [n for n, _ in launches]
+
+
+def test_prompts_keep_to_the_number_of_launches_promised(lib):
+    # chunks of 64 and 20 steps deep in the sequence, two blocks over the codes and one; answers over the rows
+    kv = store(8, 128, 32, 64, ring=64)
+    names = assert_within_the_launches_promised(lib, kv, 1, 24, 32 * 10000, 84, 1950, 1 << 44)
+    assert names.count("stream_copy") == 2 and names.count("partial_e4m3") == 3
+    r = random.Random(5)
+    for _ in range(3000):
+        Hkv, G, D, Z = r.choice([1, 2, 8]), r.choice([1, 3, 4, 17, 100]), r.choice([64, 128]), r.choice([32, 64, 256])
+        dtype = r.choice([E4M3, E4M3, T.TEMPO_BF16, T.TEMPO_F32])
+        batch, count, t = r.choice([1, 2, 16]), int(2 ** r.uniform(0, 9)), r.choice([0, 0, int(2 ** r.uniform(0, 16))])
+        window, block = r.choice([0, int(2 ** r.uniform(0, 12)), int(2 ** r.uniform(0, 12))]), 128 // G
+        ring = T.tempo_ring_blocks(window, Z, min(block, count)) * r.choice([1, 2]) if window and r.random() < 0.8 else 0
+        kv = store(Hkv, D, Z, ring or (t + count - 1) // Z + 1, ring, dtype)
+        assert_within_the_launches_promised(lib, kv, batch, G * Hkv, t, count, window, r.choice([1 << 44, (1 << 44) + 64, 1 << 45]))
+    # beyond the index range of one launch: chunks of little more than a block
+    for count in (129, 240, 2000):
+        kv = store(64, 64, 256, 100)
+        assert_within_the_launches_promised(lib, kv, 4000, 64, 0, count, 0, 1 << 45)
