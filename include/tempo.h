@@ -623,7 +623,8 @@ size_t tempo_attn_plan_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_
  *             products of bf16 values are exact, so the choice does not hang on rounding.
  *   choice    the first `first` blocks, the `last` newest ones (last >= 1: the newest block is being filled
  *             and has no bounds) and, of the others, those with the largest scores; of equal scores the
- *             earlier block.  A score of NaN counts as the largest, so what is NaN shows in the answer.
+ *             earlier block.  A score of NaN counts as the largest, so what is NaN shows in the answer
+ *             (either product NaN makes it NaN, as 0 times an infinite bound does).
  *
  * bf16 and e4m3 stores (TEMPO_ERR_DTYPE otherwise), linear ones (TEMPO_ERR_SHAPE on rings); query
  * groups as for the attention.  t and t_per_seq as for tempo_attn_decode_causal.

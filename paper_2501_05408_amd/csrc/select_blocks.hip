@@ -408,12 +408,14 @@ __device__ inline uint64_t exact_key(const ChooseParams& p, const uint16_t* ahea
     float x[8];
     unpack8(g < kHeads ? *reinterpret_cast<const u32x4*>(ahead + g * D + (live ? d : 0)) : *reinterpret_cast<const u32x4*>(q + (int64_t)g * D), x);
     double sum = 0.0;
+    bool nan = false;  // a product that is NaN is not the smaller one: 0 times an infinite bound
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float m = x[e] < 0.f ? l[e] : h[e];  // the larger product's (NaN where a bound is)
+      const float m = x[e] < 0.f ? l[e] : h[e];  // the larger product's
       sum = fma((double)x[e], (double)m, sum);
+      nan |= __builtin_isunordered(x[e] * l[e], x[e] * h[e]);
     }
-    sum = live ? sum : 0.0;
+    sum = live ? (nan ? (double)NAN : sum) : 0.0;
     sum += lane_move<kPairs>(sum);
     sum += lane_move<kFours>(sum);
     sum += lane_move<kEights>(sum);

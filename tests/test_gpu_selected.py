@@ -199,6 +199,28 @@ def test_choice_of_nan_infinite_and_extreme_bounds():
         assert {0, 10, 90, blocks - 1} <= set(got[b, 0].tolist()) and (np.diff(got[b, 0]) > 0).all()
 
 
+@pytest.mark.parametrize("D,Hq,blocks,Z", [(64, 2, 100, 32), (128, 20, 300, 32), (128, 6, 5000, 32)])
+def test_zero_times_an_infinite_bound_is_nan_on_either_side(D, Hq, blocks, Z):
+    """max(q lo, q hi) with q = 0, or with an infinite q and a bound of 0: a NaN product is taken, whichever it is."""
+    st = make_store(37, T.TEMPO_BF16, 2, Hq, 1, D, Z, blocks * Z - 1)
+    bounds = random_bounds(st, 37)
+    table = st.block_table.cpu().numpy()
+    q = normal(37, 7, (2, Hq, D))
+    q[0, 1, 3], q[1, 0, D - 1] = 0.0, -0.0
+    for b, d in ((0, 3), (1, D - 1)):
+        bounds[table[b, 11], 0, 0, d] = -np.inf                              # the smaller bound: the larger product is 0, the other NaN
+        bounds[table[b, 40], 0, 1, d] = np.inf
+        bounds[table[b, 77], 0, 0, d], bounds[table[b, 77], 0, 1, d] = -np.inf, np.inf
+    got = assert_choice(st, bounds, q, blocks * Z - 1, None, 6, 1, 1)
+    assert all({11, 40, 77} <= set(got[b, 0].tolist()) for b in range(2))
+    clean = random_bounds(st, 38)
+    q[0, 0, 5] = np.inf
+    clean[table[0], 0, 0, 5], clean[table[0], 0, 1, 5] = 1.0, 2.0            # scores of +inf but where a bound is 0
+    clean[table[0, 23], 0, 0, 5] = 0.0
+    got = st.select_blocks(clean, bf16(q), blocks * Z - 1, 3, 1, 1).cpu().numpy()
+    assert got[0, 0].tolist() == [0, 23, blocks - 1]
+
+
 @pytest.mark.parametrize("bound,query", [(2.0 ** -130, 1.0), (2.0 ** -130, 2.0 ** 100), (2.0 ** -70, 2.0 ** -75), (2.0 ** 60, 2.0 ** 60), (1.0, 2.0 ** -20)])
 def test_choice_at_the_ends_of_the_range(bound, query):
     """Bounds that bf16 holds as subnormals, products that fp32 does, and large ones."""
