@@ -14,8 +14,8 @@
 //     step's are passed over.
 // Bound by HBM: 16 sequences of 4096 keys in 8 heads of 128, 135 MB, in 22 us (6.1 TB/s; a streaming read reaches 7.1; the vector
 // units are busy 7 of the 22), 8 x 64 listed blocks of 64 bf16 keys, 134 MB, in 22; each byte is fetched once.
-// More than 16 (step, head) columns: a wavefront takes 32 (8-bit stores), further workgroups along grid.x the next ones over
-// the same keys, next to each other in dispatch order, so that all but one of them read from a die's L2.
+// More than 16 (step, head) columns: a wavefront takes 32 (8-bit stores), further workgroups the next ones over the same keys, on
+// the same die (units_work()), so that all but one of them read from its L2.
 #include "attn_bf16_common.h"
 #include "attn_units.h"
 #include "store_e4m3.h"
@@ -295,20 +295,21 @@ __global__ __launch_bounds__(512, D == 64 && CT == 2 ? 4 : 1) void attn_units(Se
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nwaves = blockDim.x >> 6;
-  const int hkv = (int)(blockIdx.x % (unsigned)p.Hkv), first_col = 16 * CT * (int)(blockIdx.x / (unsigned)p.Hkv);
-  const int b = blockIdx.y;
+  UnitsWork item = {(int)blockIdx.x, 0, (int)blockIdx.y, (int)blockIdx.z};
+  if constexpr (!k8 || CT > 1) item = units_work(blockIdx.x, blockIdx.y, blockIdx.z, gridDim.x, gridDim.y, gridDim.z, p.Hkv);  // (else one tile)
+  const int hkv = item.hkv, first_col = 16 * CT * item.tile, b = item.b;
   int t_b = p.t_per_seq ? ((const_i32_ptr)p.t_per_seq)[b] : p.t;
   t_b = t_b > p.t ? p.t : (t_b < 0 ? 0 : t_b);
   int split, start, end;  // positions: keys, or places in the list's blocks
   if constexpr (kSelect) {
-    split = blockIdx.z;
+    split = item.split;
     start = split << p.tps_log2;
     const int last = (p.pick << p.z_log2) - 1, ce = split_end(split, p.tps_log2);
     end = last < ce ? last : ce;
   } else {
     const SeqRange rg = seq_range(t_b, p.window, p.tps_log2, p.queries);
-    if ((int)blockIdx.z >= rg.nchunks) return;  // uniform over the workgroup
-    split = rg.nchunks - 1 - (int)blockIdx.z;   // newest first, as in attn_partial_bf16.hip
+    if (item.split >= rg.nchunks) return;  // uniform over the workgroup
+    split = rg.nchunks - 1 - item.split;   // newest first, as in attn_partial_bf16.hip
     const int chunk = rg.chunk0 + split, cs = chunk << p.tps_log2, ce = split_end(chunk, p.tps_log2);
     start = rg.lo > cs ? rg.lo : cs;
     end = rg.hi < ce ? rg.hi : ce;
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(512, D == 64 && CT == 2 ? 4 : 1) void attn_units(Se
   uint8_t* const stage = reinterpret_cast<uint8_t*>(smem + nwaves * (32 + (all_cols < 16 ? all_cols : 16) * D));
   if constexpr (k8 && !kSelect) {
     const int grp_new = t_b >> 5;
-    if (p.k_new && blockIdx.z == 0 && grp_new >= grp && (grp_new - grp) % nwaves == 0) {
+    if (p.k_new && item.split == 0 && grp_new >= grp && (grp_new - grp) % nwaves == 0) {
       key_new = grp_new << 5;
       const u32x4 rows = fetch_new_rows<D>(p, b, hkv, lane);
       write_new_rows<D, kRope>(p, rows, t_b, slot_of(key_new), slots, first_col == 0, lane, stage);

@@ -193,7 +193,7 @@ double plan_cost_ns(int64_t pairs, int64_t splits, int64_t keys_per_split, int b
 // step, in as long ones as fit (48 sequences of 32/8 heads of 64 at steps up to 8191, window 1000: 2 splits 15.3 us, 1 11.1).
 // In a ragged batch of up to 8 sequences a third of the workgroups are taken to exist (3.5% from the fastest plan on the mean for
 // 2 and 3 sequences, all of them 5.2%); of more sequences the longest ones decide.
-// More than 16 columns: a workgroup for every 32, which read a key from one die's cache up to 4 times; what a wavefront computes
+// More than 16 columns: a workgroup for every 32, on one die (units_work()), which read a key from its cache up to 4 times; what a wavefront computes
 // may take longer than its stream, and the combine reads a partial per column.  Fitted to 500 shapes of 17 to 128 columns: 2.9%
 // from the fastest plan on the mean, 28% at most (without tiles, work and partials 16%, 150%).
 void make_plan_e4m3(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int32_t window, bool ragged, int32_t queries,
