@@ -464,3 +464,39 @@ def test_a_captured_step_at_every_sequences_own_position(dtype, t0):
         assert (err <= 2 * 1.03 * 2.0 ** -8 * (np.abs(np64(eager)) * 2 + 4)).all()
     for x, y in ((st.k_pool, other.k_pool), (st.v_pool, other.v_pool)):
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", STORES)
+@pytest.mark.parametrize("Hq,Hkv,t0,count", [(6, 2, 32 * 192 - 4, 4), (6, 2, 90, 4), (40, 2, 700, 3), (6, 2, 4000, 60)])
+def test_answers_of_a_captured_step_are_the_definitions(dtype, Hq, Hkv, t0, count):
+    """Replays at every sequence's own position, each against the 64-bit answer over the chosen blocks: a key left out, taken
+    twice or taken from another position shows."""
+    D, Z, B, steps, G = 64, 32, 3, 8, Hq // Hkv
+    most = t0 + steps
+    K, V, q = normal(39, 2, (B, most, Hkv, D)), normal(39, 3, (B, most, Hkv, D)), normal(39, 1, (steps, B, Hq, D))
+    Kh, Vh = kept(dtype, K), kept(dtype, V)
+    st = make_store(39, dtype, B, Hq, Hkv, D, Z, most + 40)
+    bounds, lengths = st.new_bounds(), np.array([t0, t0 // 2, 3])
+    st.append_block(bf16(K[:, :t0]), bf16(V[:, :t0]), 0, t0)
+    st.update_bounds(bounds, 0, t0, count_per_seq=ints(lengths))
+    at, qd, k, v = ints(lengths), bf16(q[0]), bf16(K[:, 0]), bf16(V[:, 0])
+    out, chosen, graph = st.new_out(), torch.empty((B, Hkv, count), dtype=torch.int32, device=DEV), torch.cuda.CUDAGraph()
+    need = T.tempo_step_selected_workspace_bytes(st.kv, B, Hq, most + 40, count)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        T.tempo_decode_step_selected(st.kv, bounds, qd, k, v, out, chosen, count, 1, 1, B, Hq, most + 40, at, st.scale, ws, need)
+    for i in range(steps):
+        now = lengths + i
+        at.copy_(ints(now)), qd.copy_(bf16(q[i]))
+        k.copy_(bf16(K[np.arange(B), now])), v.copy_(bf16(V[np.arange(B), now]))
+        graph.replay()
+        torch.cuda.synchronize()
+        lists = chosen.cpu().numpy()
+        for b in range(B):
+            whole = Kh[b, :(now[b] + 1) // Z * Z].reshape(-1, Z, Hkv, D)
+            for h in range(Hkv):
+                edges = np.zeros((2, now[b] // Z + 1, D))
+                edges[0, :len(whole)], edges[1, :len(whole)] = whole[:, :, h].min(1), whole[:, :, h].max(1)
+                np.testing.assert_array_equal(lists[b, h], choose(q[i, b, h * G:(h + 1) * G], *edges, now[b] // Z, count, 1, 1))
+        assert_attend(out, q[i], Kh, Vh, lists, Z, now, st.scale, f"replay {i}")
