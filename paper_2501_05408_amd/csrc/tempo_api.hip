@@ -186,16 +186,16 @@ double plan_cost_ns(int64_t pairs, int64_t splits, int64_t keys_per_split, int b
 }
 
 // The same for 8-bit stores, whose kernel has 4 wavefronts' registers on a SIMD: more workgroups share a unit, so a further
-// round costs less, and a workgroup's own stream, half the bytes a key, is slower.  Fitted to 1020 measured shapes (1 to 64
-// sequences, 150 to 65536 keys, half of them ragged, a third with windows): 1.4% from the fastest plan on the mean for uniform
-// steps, 3.0% for ragged ones, 35% at most; bf16's constants 2.1% and 6.5%, 69%.
+// round costs less, and a workgroup's own stream, half the bytes a key, is slower.  Fitted to 1020 measured shapes; on 500
+// others (1 to 64 sequences, 150 to 65536 keys, half of them ragged, a fifth with windows; profiles/attn_units_plan_sweep.txt) 1.4%
+// from the fastest plan on the mean for uniform steps, 14% at most, 4.5% and 48% for ragged ones; bf16's constants 1.8%, 21%, 9.3%, 87%.
 // Ragged: splits of at most 2048 keys, the bytes of bf16's 1024; windows of up to 4096 keys, all of which end near their own
 // step, in as long ones as fit (48 sequences of 32/8 heads of 64 at steps up to 8191, window 1000: 2 splits 15.3 us, 1 11.1).
-// In a ragged batch of up to 8 sequences a third of the workgroups are taken to exist (3.5% from the fastest plan on the mean for
-// 2 and 3 sequences, all of them 5.2%); of more sequences the longest ones decide.
+// In a ragged batch of up to 8 sequences a third of the workgroups are taken to exist (7 of 20; 5.5% from the fastest plan on the
+// mean for 2 and 3 sequences, all of them 6.1%); of more sequences the longest ones decide (2.9%, a third of them 3.1%).
 // More than 16 columns: a workgroup for every 32, on one die (units_work()), which read a key from its cache up to 4 times; what a wavefront computes
-// may take longer than its stream, and the combine reads a partial per column.  Fitted to 500 shapes of 17 to 128 columns: 2.9%
-// from the fastest plan on the mean, 28% at most (without tiles, work and partials 16%, 150%).
+// may take longer than its stream, and the combine reads a partial per column.  Fitted to 500 shapes of 17 to 128 columns; on 400
+// others 2.6% from the fastest plan on the mean, 55% at most (with the constants for up to 16 columns 3.6%).
 void make_plan_e4m3(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t t_max, int32_t window, bool ragged, int32_t queries,
                     int64_t max_splits, tempo_plan* plan) {
   const int columns = queries * (Hq / kv->num_kv_heads), D = kv->head_dim;
