@@ -348,7 +348,7 @@ def _own(state):
             return [out] + _stored(state)
         T.tempo_kv_gather(kv, h["k_back"], h["v_back"], B, t, C)
         return [out, h["k_back"], h["v_back"]]
-    T.tempo_kv_keep(h["kvs"], c["layers"], B, t, steps, state["path"], state["path"].shape[1])
+    T.tempo_kv_keep(h["kvs"], c["layers"], B, t, steps, C, state["path"], state["path"].shape[1])
     return _stored(state)
 
 
