@@ -685,6 +685,122 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
                                size_t workspace_bytes, void* stream);
 
 /*
+ * Windows with sinks: a step attends over a backward window and over the first `sinks` keys of its sequence, which stay visible
+ * (a softmax needs somewhere to put weight that no key in the window asks for; without the first keys long answers fall apart
+ * once they leave the window).  Step p sees
+ *     keys j < sinks, and keys max(0, p-window+1) .. p               (window >= 1, sinks >= 0; keys are counted once)
+ * with positions as they were written.  bf16 and e4m3 stores (TEMPO_ERR_DTYPE otherwise), linear ones (TEMPO_ERR_SHAPE on rings).
+ *
+ * Constant memory: the table of a linear store may name a block more than once.  Blocks 0 .. sink_blocks-1 of a sequence are kept and
+ * window_blocks further ones (tempo_sink_blocks) take the tiles behind them in turn,
+ *     table[n] = n < sink_blocks ? own[n] : own[sink_blocks + (n - sink_blocks) mod window_blocks],
+ * so that a conversation of any length lives in sink_blocks + window_blocks blocks.  What one call writes and what it reads must lie
+ * in blocks of their own then: the sizes that tempo_sink_blocks gives for its `queries` steps do that.  (Longer prompts by several calls.)
+ *
+ * tempo_sink_blocks         *sink_blocks = ceil(sinks / Z); *window_blocks = the most tiles that the windows of `queries` consecutive
+ *                           steps touch.  Host only; TEMPO_ERR_RANGE for window, Z or queries < 1 or sinks < 0, TEMPO_ERR_NULL.
+ * tempo_attn_sinks          `queries` consecutive steps t .. t+queries-1 (t_per_seq[b] ..; t their upper bound), which the store
+ *                           holds: q, out device, [batch][queries][Hq][D].  Any number of steps.
+ * tempo_decode_step_sinks   one step whose row k_new, v_new (device, [batch][Hkv][D]) is written first; q, out [batch][Hq][D].
+ * tempo_rope_decode_step_sinks  the same with q_raw and k_raw turned to position t (t_per_seq[b]), as tempo_rope_decode_step_*.
+ * tempo_prefill_sinks, tempo_rope_prefill_sinks  steps t .. t+count-1: rows written, all steps answered, count_per_seq as for
+ *                           tempo_prefill_* (rows behind a sequence's count are neither written nor answered: the store and `out` stay
+ *                           as they are there).  Answers are those of single steps.  `out` must not alias k_new or v_new.
+ * Workspaces: device, 256-byte aligned (TEMPO_ERR_WORKSPACE).  The size for max_t serves every step up to it; a loop over steps of an
+ * endless conversation asks for it once, with the largest step: it does not grow beyond the window.  0 on bad arguments.
+ * queries * num_q_heads <= 2^30, rows written batch * count * Hkv * D < 2^31 (TEMPO_ERR_SHAPE).
+ */
+int tempo_sink_blocks(int32_t window, int32_t sinks, int32_t Z, int32_t queries, int32_t* sink_blocks, int32_t* window_blocks);
+
+size_t tempo_attn_sinks_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t queries, int32_t max_t,
+                                        int32_t window, int32_t sinks);
+
+int tempo_attn_sinks(const tempo_kv* kv, const void* q, void* out, int32_t batch, int32_t num_q_heads, int32_t queries, int32_t t,
+                     const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
+int tempo_decode_step_sinks(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch,
+                            int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+int tempo_rope_decode_step_sinks(const tempo_kv* kv, const tempo_rope* rope, const void* q_raw, const void* k_raw, const void* v_new,
+                                 void* out, int32_t batch, int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, int32_t window,
+                                 int32_t sinks, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/* For any prompt whose last step is at most max_t. */
+size_t tempo_prefill_sinks_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t);
+
+int tempo_prefill_sinks(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch,
+                        int32_t num_q_heads, int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window, int32_t sinks,
+                        float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+int tempo_rope_prefill_sinks(const tempo_kv* kv, const tempo_rope* rope, const void* q_raw, const void* k_raw, const void* v_new,
+                             void* out, int32_t batch, int32_t num_q_heads, int32_t t, int32_t count, const int32_t* count_per_seq,
+                             int32_t window, int32_t sinks, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Trees of drafted tokens (speculative decoding): several continuations of a sequence, which share beginnings, are answered by one
+ * call and the one that the model agrees with is kept.  A step of a decoder, with t tokens cached:
+ *   tempo_tree_positions, once; then for every layer tempo_rope_kv_append_at (rows of all nodes to steps t .. t+nodes-1, turned to
+ *   the nodes' positions) and tempo_attn_tree; and when the path is known, tempo_kv_keep, once for all layers.
+ *
+ * parents   device, int32 [batch][nodes]: node i's parent, a node before it (0 .. i-1); anything else: none, the node follows step
+ *           t-1.  A node's depth is the number of its ancestors, its position t + depth; its row lies at step t + i.
+ * nodes     of the largest tree, at most 256 (TEMPO_ERR_SHAPE); nodes_per_seq (device, int32 [batch], may be NULL): sequence b has
+ *           only its first nodes_per_seq[b] (0 .. nodes) ones, the other rows of `out` are left as they are.
+ *
+ * tempo_tree_positions  positions (device, int32 [batch][nodes]) = t + depth (t_per_seq[b] + depth if given, t their upper bound).
+ * tempo_attn_tree       q, out device, [batch][nodes][Hq][D].  Node i sees steps 0 .. t-1, its ancestors and itself.  t = 0: no
+ *                       step is cached.  With window >= 1 of these only those at a position above t + depth - window or below
+ *                       `sinks` (window = 0: all, and sinks must be 0).  Stores, workspace and limits as for tempo_attn_sinks.
+ *                       A bf16 or e4m3 value of a node that is not finite may show in nodes that do not see it, as in blocks of steps.
+ * tempo_kv_keep         the row at step t + i becomes what step t + kept[b][i] held before the call, keys and values, for
+ *                       i = 0, 1, .. up to the first entry of kept (device, int32 [batch][count]) outside 0 .. nodes-1; other
+ *                       rows stay as they are.  With the accepted path's node numbers, root first, the sequence goes on at step
+ *                       t + their number (positions are right: the path's node i has depth i).  layers: host, [num_layers], stores
+ *                       that differ in their pools alone (TEMPO_ERR_SHAPE otherwise); all of them are one launch (64 at a time).
+ *                       Any store; count <= 128 (TEMPO_ERR_SHAPE).  Rows of t .. t + max(nodes, count) - 1 must fit.
+ */
+int tempo_tree_positions(const int32_t* parents, int32_t* positions, int32_t batch, int32_t nodes, int32_t t, const int32_t* t_per_seq,
+                         void* stream);
+
+size_t tempo_attn_tree_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t nodes, int32_t max_t,
+                                       int32_t window, int32_t sinks);
+
+int tempo_attn_tree(const tempo_kv* kv, const void* q, void* out, const int32_t* parents, const int32_t* nodes_per_seq, int32_t batch,
+                    int32_t num_q_heads, int32_t nodes, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+int tempo_kv_keep(const tempo_kv* layers, int32_t num_layers, int32_t batch, int32_t t, const int32_t* t_per_seq, int32_t nodes,
+                  const int32_t* kept, int32_t count, void* stream);
+
+/*
+ * Rows at positions of their own: a row's position is not its step (nodes of a tree, tokens of images and video, which have one
+ * in time, in height and in width).  Pair i (dims i and i + D/2) belongs to an axis and is turned by the tables' entry (the row's
+ * position on that axis, i), as in tempo_rope_rotate.
+ *   axes       NULL: one axis.  axes 1 .. 4 (TEMPO_ERR_SHAPE); axis_of_pair[0 .. D/2-1] below axes (TEMPO_ERR_RANGE).
+ *   positions  device, int32 [batch][count][axes]; clamped into the tables' 0 .. rope->positions-1.
+ * tempo_rope_rotate_at      y = x turned; x, y device, [batch][count][heads][D] of bf16 or fp32; y may be x.
+ * tempo_rope_kv_append_at   k_raw (turned) and v_new (device, [batch][count][Hkv][D]) to steps t .. t+count-1 (t_per_seq[b] ..; t
+ *                           their upper bound; only the first count_per_seq[b] rows, if given), and q_out = q_raw turned (device,
+ *                           [batch][count][Hq][D]; both NULL: keys and values alone; q_out may be q_raw) in the same launch.  Any
+ *                           store; of a ring at most its own number of steps.  The bits of tempo_rope_kv_append_block where
+ *                           positions are the steps.  batch * count * (Hq + 2 Hkv) * D/8 < 2^31 (TEMPO_ERR_SHAPE).
+ * Arrays and pools are 16-byte aligned.
+ */
+typedef struct tempo_rope_axes {
+  int32_t axes;
+  uint8_t axis_of_pair[64];
+} tempo_rope_axes;
+
+int tempo_rope_rotate_at(const tempo_rope* rope, const tempo_rope_axes* axes, const int32_t* positions, const void* x, void* y,
+                         int32_t dtype, int32_t batch, int32_t count, int32_t heads, void* stream);
+
+int tempo_rope_kv_append_at(const tempo_kv* kv, const tempo_rope* rope, const tempo_rope_axes* axes, const int32_t* positions,
+                            const void* k_raw, const void* v_new, const void* q_raw, void* q_out, int32_t batch, int32_t num_q_heads,
+                            int32_t t, const int32_t* t_per_seq, int32_t count, const int32_t* count_per_seq, void* stream);
+
+/*
  * Anti-causal window reduction (Section 3, Algorithm 1: the returns of the paper's
  * reinforcement-learning example, `r[t : min(t+n, T)].discounted_sum(gamma)` and
  * `r[t : T].discounted_sum(gamma)`): for every sequence b and step t

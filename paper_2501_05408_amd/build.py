@@ -22,10 +22,13 @@ OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["tempo_api.hip", "kv_store.hip", "attn_partial_bf16.hip", "attn_partial_f32.hip", "attn_step_f32.hip",
            "attn_combine.hip", "stream_read.hip", "rope.hip", "attn_prefill_bf16.hip", "attn_block_bf16.hip",
            "attn_stream_bf16.hip",
-           "worklist.hip", "discounted_sum.hip", "kv_store_e4m3.hip", "attn_units.hip", "select_blocks.hip"]
+           "worklist.hip", "discounted_sum.hip", "kv_store_e4m3.hip", "attn_units.hip", "select_blocks.hip",
+           "attn_spans.hip", "kv_place.hip"]
 HEADERS = [os.path.join(CSRC, "tempo_internal.h"), os.path.join(CSRC, "attn_bf16_common.h"),
            os.path.join(CSRC, "attn_bf16_columns32.h"), os.path.join(CSRC, "attn_combine.h"),
-           os.path.join(CSRC, "store_e4m3.h"), os.path.join(CSRC, "attn_units.h"), os.path.join(ROOT, "include", "tempo.h")]
+           os.path.join(CSRC, "store_e4m3.h"), os.path.join(CSRC, "attn_units.h"), os.path.join(CSRC, "attn_image.h"),
+           os.path.join(CSRC, "attn_spans.h"), os.path.join(CSRC, "attn_tree.h"), os.path.join(CSRC, "tempo_api_spans.h"),
+           os.path.join(ROOT, "include", "tempo.h")]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Rpass-analysis=kernel-resource-usage",

@@ -1993,3 +1993,5 @@ int tempo_stream_copy(const void* src, void* dst, size_t bytes, int32_t workgrou
 }
 
 }  // extern "C"
+
+#include "tempo_api_spans.h"

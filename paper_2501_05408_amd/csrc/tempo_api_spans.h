@@ -1,0 +1,344 @@
+// Entry points of drafted trees, windows with sinks, rows at positions of their own and kept rows; the end of tempo_api.hip, whose
+// checks they use.
+#pragma once
+
+#include "attn_spans.h"
+
+namespace {
+
+// A call of the attention over spans: how its (row, head) columns and its keys are cut.
+struct SpanPlan {
+  int32_t tile_columns, tiles, split_groups, splits, waves;
+};
+
+// Attention over spans is of bf16 and 8-bit linear stores.
+int check_span_store(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows) {
+  int rc = check_layout(kv);
+  if (rc != TEMPO_OK) return rc;
+  if (kv->dtype == TEMPO_F32) return TEMPO_ERR_DTYPE;
+  if (kv->ring_blocks != 0) return TEMPO_ERR_SHAPE;
+  if ((rc = check_heads(kv, batch, Hq)) != TEMPO_OK) return rc;
+  if (rows < 1 || rows > (1 << 24) || (int64_t)rows * Hq > (1 << 30)) return TEMPO_ERR_SHAPE;
+  return TEMPO_OK;
+}
+
+// Steps t .. t + rows - 1 (of a tree the slots of its nodes), the window (0: none, and no sinks then) and the sinks.
+int check_span(const tempo_kv* kv, int32_t t, int32_t rows, int32_t window, int32_t sinks) {
+  if (t < 0 || window < 0 || sinks < 0 || t > INT32_MAX - 128 - rows) return TEMPO_ERR_RANGE;
+  if (window == 0 && sinks > 0) return TEMPO_ERR_RANGE;
+  return check_step(kv, t + rows - 1);
+}
+
+// Most 32-key groups that a tile of columns sees, whatever its steps up to t + rows - 1.
+int32_t span_groups_bound(int32_t t, int32_t rows, int32_t tile_rows, int32_t window, int32_t sinks) {
+  const int64_t all = ((int64_t)t + rows - 1) / 32 + 1;
+  if (window == 0) return (int32_t)all;
+  const int64_t keys = (int64_t)window + tile_rows - 1;  // a run of so many keys touches ...
+  const int64_t some = (keys + 30) / 32 + 1 + ((int64_t)sinks + 31) / 32;
+  return (int32_t)(some < all ? some : all);
+}
+
+constexpr int64_t kSpanWorkgroups = 512;
+
+SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, int32_t window, int32_t sinks, bool tree) {
+  SpanPlan s;
+  const int32_t G = Hq / kv->num_kv_heads;
+  const int64_t columns = (int64_t)rows * G;
+  s.tile_columns = columns <= 16 ? 16 : 32;
+  s.tiles = (int32_t)((columns + s.tile_columns - 1) / s.tile_columns);
+  int32_t tile_rows = (s.tile_columns + G - 2) / G + 1;
+  tile_rows = tree || tile_rows > rows ? rows : tile_rows;
+  const int32_t groups = span_groups_bound(t, rows, tile_rows, window, sinks);
+  const int64_t units = (int64_t)batch * kv->num_kv_heads * s.tiles;
+  int64_t splits = kSpanWorkgroups / units, most = (groups + 7) / 8;
+  splits = splits < most ? splits : most;
+  splits = splits < 1 ? 1 : splits;
+  s.split_groups = (int32_t)((groups + splits - 1) / splits);
+  s.splits = (groups + s.split_groups - 1) / s.split_groups;
+  s.waves = s.split_groups >= 16 ? 8 : s.split_groups >= 4 ? 4 : s.split_groups >= 2 ? 2 : 1;
+  while (s.waves > 1 && units_lds_bytes(s.waves, (int)(columns < 16 ? columns : 16), kv->head_dim) > kMaxUnitsLds) s.waves /= 2;
+  return s;
+}
+
+size_t span_bytes(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, const SpanPlan& s) {
+  return s.splits == 1 ? 256 : plan_bytes(kv, (int64_t)batch * rows * Hq, s.splits);
+}
+
+// Rows of the partials of any call with at most `rows` rows a sequence whose last step is at most max_t.
+size_t span_bytes_bound(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t max_t) {
+  // splits only where there are fewer than kSpanWorkgroups tiles of up to 32 columns: rows * splits is at most 32 times as many
+  const int64_t all = (int64_t)batch * rows * Hq, groups = max_t / 32 + 1, most = 2 * 32 * kSpanWorkgroups;
+  const int64_t partials = all > most / groups ? most : all * groups;
+  return plan_bytes(kv, partials, 1);
+}
+
+// Everything but the arguments that only one of the entry points has has been checked.
+int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* parents, const int32_t* rows_per_seq, int32_t batch, int32_t Hq,
+                 int32_t rows, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale, void* workspace,
+                 hipStream_t stream, const tempo_rope* rope = nullptr) {
+  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, window, sinks, parents != nullptr);
+  tempo_plan plan = {32, s.splits, s.waves};
+  SpanParams p;
+  static_cast<AttnParams&>(p) = attn_params(kv, q, out, Hq, t, t_per_seq, window, scale, &plan, workspace, batch, rows);
+  p.direct = s.splits == 1;
+  p.count_per_seq = rows_per_seq;
+  p.parents = parents;
+  p.sinks = sinks;
+  p.tile_columns = s.tile_columns;
+  p.split_groups = s.split_groups;
+  if (rope) {
+    p.rope_cos = rope->cos;
+    p.rope_sin = rope->sin;
+  }
+  const int rc = launch_status(launch_spans(p, batch, kv->head_dim, kv->dtype, s.waves, stream), "attn_spans");
+  if (rc != TEMPO_OK || p.direct) return rc;
+  return launch_status(launch_combine_spans(p, batch, kv->head_dim, stream), "attn_spans_combine");
+}
+
+int check_span_workspace(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, int32_t window, int32_t sinks, bool tree,
+                         const void* workspace, size_t workspace_bytes) {
+  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, window, sinks, tree);
+  // workgroups: along the grid's first axis, and all of them (numbered in 32 bits)
+  const int64_t first = (int64_t)kv->num_kv_heads * s.tiles;
+  if (first * 512 > INT32_MAX || first * batch * s.splits > INT32_MAX || s.splits > 65535) return TEMPO_ERR_SHAPE;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
+  return workspace_bytes < span_bytes(kv, batch, Hq, rows, s) ? TEMPO_ERR_WORKSPACE : TEMPO_OK;
+}
+
+// Positions of a call's rows: tables, axes.
+int check_axes(const tempo_rope* rope, const tempo_rope_axes* axes, int32_t head_dim) {
+  const int rc = check_rope(rope, head_dim, 0);
+  if (rc != TEMPO_OK || !axes) return rc;
+  if (axes->axes < 1 || axes->axes > 4) return TEMPO_ERR_SHAPE;
+  for (int i = 0; i < head_dim / 2; ++i) {
+    if (axes->axis_of_pair[i] >= axes->axes) return TEMPO_ERR_RANGE;
+  }
+  return TEMPO_OK;
+}
+
+PlaceParams place_params(const StoreParams& store, const tempo_rope* rope, const tempo_rope_axes* axes, const int32_t* positions) {
+  PlaceParams p;
+  static_cast<StoreParams&>(p) = store;
+  p.rope_cos = rope->cos;
+  p.rope_sin = rope->sin;
+  p.positions = positions;
+  p.q = nullptr;
+  p.q_out = nullptr;
+  p.Hq = p.Hrows = 0;
+  p.axes = axes ? axes->axes : 1;
+  p.table_rows = rope->positions;
+  p.axis_bits[0] = p.axis_bits[1] = 0;
+  for (int i = 0; axes && i < rope->head_dim / 2; ++i) p.axis_bits[i >> 5] |= (uint64_t)(axes->axis_of_pair[i] & 3u) << (2 * (i & 31));
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tempo_sink_blocks(int32_t window, int32_t sinks, int32_t Z, int32_t queries, int32_t* sink_blocks, int32_t* window_blocks) {
+  if (!sink_blocks || !window_blocks) return TEMPO_ERR_NULL;
+  if (window < 1 || sinks < 0 || Z < 1 || queries < 1) return TEMPO_ERR_RANGE;
+  const int64_t keys = (int64_t)window + queries - 1;
+  *sink_blocks = (int32_t)(((int64_t)sinks + Z - 1) / Z);
+  *window_blocks = (int32_t)((keys + Z - 2) / Z + 1);
+  return TEMPO_OK;
+}
+
+size_t tempo_attn_sinks_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t queries, int32_t max_t,
+                                        int32_t window, int32_t sinks) {
+  if (check_span_store(kv, batch, num_q_heads, queries) != TEMPO_OK) return 0;
+  if (window < 1 || sinks < 0 || max_t < 0 || max_t > INT32_MAX - 128 - queries) return 0;
+  const int32_t tile_rows = queries;  // (no tile sees more)
+  const int32_t groups = span_groups_bound(max_t, queries, tile_rows, window, sinks);
+  return span_bytes_bound(kv, batch, num_q_heads, queries, (groups - 1) * 32);
+}
+
+size_t tempo_attn_tree_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t nodes, int32_t max_t,
+                                       int32_t window, int32_t sinks) {
+  if (check_span_store(kv, batch, num_q_heads, nodes) != TEMPO_OK || nodes > kMaxNodes) return 0;
+  if (window < 0 || sinks < 0 || max_t < 0 || max_t > INT32_MAX - 128 - nodes) return 0;
+  const int32_t groups = span_groups_bound(max_t, nodes, nodes, window, sinks);
+  return span_bytes_bound(kv, batch, num_q_heads, nodes, (groups - 1) * 32);
+}
+
+size_t tempo_prefill_sinks_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t) {
+  if (check_span_store(kv, batch, num_q_heads, 1) != TEMPO_OK) return 0;
+  if (max_t < 0 || max_t > INT32_MAX - 128) return 0;
+  const int32_t rows = max_t < (1 << 24) ? max_t + 1 : 1 << 24;
+  return span_bytes_bound(kv, batch, num_q_heads, rows, max_t);
+}
+
+int tempo_attn_tree(const tempo_kv* kv, const void* q, void* out, const int32_t* parents, const int32_t* nodes_per_seq, int32_t batch,
+                    int32_t num_q_heads, int32_t nodes, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = check_span_store(kv, batch, num_q_heads, nodes);
+  if (rc != TEMPO_OK) return rc;
+  if (!q || !out || !parents || (rc = check_store(kv)) != TEMPO_OK) return TEMPO_ERR_NULL;
+  if (nodes > kMaxNodes) return TEMPO_ERR_SHAPE;
+  if ((rc = check_span(kv, t, nodes, window, sinks)) != TEMPO_OK) return rc;
+  if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
+  if ((rc = check_span_workspace(kv, batch, num_q_heads, nodes, t, window, sinks, true, workspace, workspace_bytes)) != TEMPO_OK) return rc;
+  return attend_spans(kv, q, out, parents, nodes_per_seq, batch, num_q_heads, nodes, t, t_per_seq, window, sinks, scale, workspace,
+                      static_cast<hipStream_t>(stream));
+}
+
+// A call of consecutive steps; k_new set: their rows are written first.  prompt: count_per_seq and many rows.
+static int sinks_call(const tempo_kv* kv, const tempo_rope* rope, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch,
+                      int32_t Hq, int32_t rows, int32_t t, const int32_t* t_per_seq, const int32_t* count_per_seq, int32_t window, int32_t sinks,
+                      float scale, void* workspace, size_t workspace_bytes, void* stream, bool write) {
+  int rc = check_span_store(kv, batch, Hq, rows);
+  if (rc != TEMPO_OK) return rc;
+  if (!q || !out || (write && (!k_new || !v_new)) || (rc = check_store(kv)) != TEMPO_OK) return TEMPO_ERR_NULL;
+  if (window < 1) return TEMPO_ERR_RANGE;
+  if ((rc = check_span(kv, t, rows, window, sinks)) != TEMPO_OK) return rc;
+  if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
+  if (rope && (rc = check_rope(rope, kv->head_dim, t + rows - 1)) != TEMPO_OK) return rc;
+  if (write && (int64_t)batch * rows * kv->num_kv_heads * kv->head_dim > INT32_MAX) return TEMPO_ERR_SHAPE;
+  if ((rc = check_span_workspace(kv, batch, Hq, rows, t, window, sinks, false, workspace, workspace_bytes)) != TEMPO_OK) return rc;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (write) {
+    StoreParams p = store_params(kv, batch, t, t_per_seq, rows);
+    p.count_per_seq = count_per_seq;
+    if (rope) {
+      p.rope_cos = rope->cos;
+      p.rope_sin = rope->sin;
+    }
+    if ((rc = launch_status(launch_append(p, k_new, v_new, kv->head_dim, kv->dtype, s), "kv_append")) != TEMPO_OK) return rc;
+  }
+  return attend_spans(kv, q, out, nullptr, count_per_seq, batch, Hq, rows, t, t_per_seq, window, sinks, scale, workspace, s, rope);
+}
+
+int tempo_attn_sinks(const tempo_kv* kv, const void* q, void* out, int32_t batch, int32_t num_q_heads, int32_t queries, int32_t t,
+                     const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale, void* workspace, size_t workspace_bytes,
+                     void* stream) {
+  return sinks_call(kv, nullptr, q, nullptr, nullptr, out, batch, num_q_heads, queries, t, t_per_seq, nullptr, window, sinks, scale, workspace,
+                    workspace_bytes, stream, false);
+}
+
+int tempo_decode_step_sinks(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch,
+                            int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  return sinks_call(kv, nullptr, q, k_new, v_new, out, batch, num_q_heads, 1, t, t_per_seq, nullptr, window, sinks, scale, workspace,
+                    workspace_bytes, stream, true);
+}
+
+int tempo_rope_decode_step_sinks(const tempo_kv* kv, const tempo_rope* rope, const void* q_raw, const void* k_raw, const void* v_new, void* out,
+                                 int32_t batch, int32_t num_q_heads, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks,
+                                 float scale, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!rope) return TEMPO_ERR_NULL;
+  return sinks_call(kv, rope, q_raw, k_raw, v_new, out, batch, num_q_heads, 1, t, t_per_seq, nullptr, window, sinks, scale, workspace,
+                    workspace_bytes, stream, true);
+}
+
+int tempo_prefill_sinks(const tempo_kv* kv, const void* q, const void* k_new, const void* v_new, void* out, int32_t batch, int32_t num_q_heads,
+                        int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window, int32_t sinks, float scale, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  return sinks_call(kv, nullptr, q, k_new, v_new, out, batch, num_q_heads, count, t, nullptr, count_per_seq, window, sinks, scale, workspace,
+                    workspace_bytes, stream, true);
+}
+
+int tempo_rope_prefill_sinks(const tempo_kv* kv, const tempo_rope* rope, const void* q_raw, const void* k_raw, const void* v_new, void* out,
+                             int32_t batch, int32_t num_q_heads, int32_t t, int32_t count, const int32_t* count_per_seq, int32_t window,
+                             int32_t sinks, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!rope) return TEMPO_ERR_NULL;
+  return sinks_call(kv, rope, q_raw, k_raw, v_new, out, batch, num_q_heads, count, t, nullptr, count_per_seq, window, sinks, scale, workspace,
+                    workspace_bytes, stream, true);
+}
+
+int tempo_rope_rotate_at(const tempo_rope* rope, const tempo_rope_axes* axes, const int32_t* positions, const void* x, void* y, int32_t dtype,
+                         int32_t batch, int32_t count, int32_t heads, void* stream) {
+  if (!rope || !positions || !x || !y) return TEMPO_ERR_NULL;
+  if (dtype != TEMPO_BF16 && dtype != TEMPO_F32) return TEMPO_ERR_DTYPE;
+  if (rope->head_dim != 64 && rope->head_dim != 128) return TEMPO_ERR_SHAPE;
+  if (batch < 1 || batch > 65535 || count < 1 || heads < 1 || heads > 65535) return TEMPO_ERR_SHAPE;
+  if ((int64_t)count * heads > INT32_MAX || (int64_t)batch * count * heads * rope->head_dim / 8 > INT32_MAX) return TEMPO_ERR_SHAPE;
+  const int rc = check_axes(rope, axes, rope->head_dim);
+  if (rc != TEMPO_OK) return rc;
+  StoreParams none = {};
+  none.batch = batch;
+  none.count = count;
+  PlaceParams p = place_params(none, rope, axes, positions);
+  p.q = x;
+  p.q_out = y;
+  p.Hq = heads;
+  return launch_status(launch_place(p, nullptr, nullptr, rope->head_dim, dtype, static_cast<hipStream_t>(stream)), "rope_rotate_at");
+}
+
+int tempo_rope_kv_append_at(const tempo_kv* kv, const tempo_rope* rope, const tempo_rope_axes* axes, const int32_t* positions, const void* k_raw,
+                            const void* v_new, const void* q_raw, void* q_out, int32_t batch, int32_t num_q_heads, int32_t t,
+                            const int32_t* t_per_seq, int32_t count, const int32_t* count_per_seq, void* stream) {
+  int rc = check_store(kv);
+  if (rc != TEMPO_OK) return rc;
+  if (!positions || !k_raw || !v_new || ((q_raw == nullptr) != (q_out == nullptr))) return TEMPO_ERR_NULL;
+  if (batch < 1 || batch > 65535 || count < 1 || count > (1 << 24)) return TEMPO_ERR_SHAPE;
+  if (q_raw && (rc = check_heads(kv, batch, num_q_heads)) != TEMPO_OK) return rc;
+  if (t < 0 || t > INT32_MAX - 64 - count) return TEMPO_ERR_RANGE;
+  if ((rc = check_step(kv, t + count - 1)) != TEMPO_OK) return rc;
+  if (kv->ring_blocks && (int64_t)count > (int64_t)kv->ring_blocks * kv->block_size) return TEMPO_ERR_RANGE;
+  if ((rc = check_axes(rope, axes, kv->head_dim)) != TEMPO_OK) return rc;
+  const int64_t heads = (q_raw ? num_q_heads : 0) + 2 * (int64_t)kv->num_kv_heads;
+  if (batch * (int64_t)count * heads * kv->head_dim / 8 > INT32_MAX) return TEMPO_ERR_SHAPE;
+  StoreParams store = store_params(kv, batch, t, t_per_seq, count);
+  store.count_per_seq = count_per_seq;
+  PlaceParams p = place_params(store, rope, axes, positions);
+  p.Hrows = kv->num_kv_heads;
+  p.q = q_raw;
+  p.q_out = q_out;
+  p.Hq = q_raw ? num_q_heads : 0;
+  return launch_status(launch_place(p, k_raw, v_new, kv->head_dim, kv->dtype, static_cast<hipStream_t>(stream)), "rope_kv_append_at");
+}
+
+int tempo_tree_positions(const int32_t* parents, int32_t* positions, int32_t batch, int32_t nodes, int32_t t, const int32_t* t_per_seq,
+                         void* stream) {
+  if (!parents || !positions) return TEMPO_ERR_NULL;
+  if (batch < 1 || batch > 65535 || nodes < 1 || nodes > kMaxNodes) return TEMPO_ERR_SHAPE;
+  if (t < 0 || t > INT32_MAX - nodes) return TEMPO_ERR_RANGE;
+  return launch_status(launch_tree_positions(parents, positions, batch, nodes, t, t_per_seq, static_cast<hipStream_t>(stream)),
+                       "tree_positions");
+}
+
+int tempo_kv_keep(const tempo_kv* layers, int32_t num_layers, int32_t batch, int32_t t, const int32_t* t_per_seq, int32_t nodes,
+                  const int32_t* kept, int32_t count, void* stream) {
+  if (!layers || !kept) return TEMPO_ERR_NULL;
+  if (num_layers < 1 || batch < 1 || batch > 65535) return TEMPO_ERR_SHAPE;
+  if (count < 1 || count > kKeepRows || nodes < 1 || nodes > (1 << 24)) return TEMPO_ERR_SHAPE;
+  int rc = TEMPO_OK;
+  for (int32_t i = 0; i < num_layers; ++i) {
+    const tempo_kv &a = layers[i], &first = layers[0];
+    if ((rc = check_store(&a)) != TEMPO_OK) return rc;
+    if (a.block_table != first.block_table || a.num_blocks != first.num_blocks || a.max_blocks_per_seq != first.max_blocks_per_seq ||
+        a.block_size != first.block_size || a.num_kv_heads != first.num_kv_heads || a.head_dim != first.head_dim || a.dtype != first.dtype ||
+        a.ring_blocks != first.ring_blocks)
+      return TEMPO_ERR_SHAPE;
+  }
+  if (layers->num_kv_heads > 32767) return TEMPO_ERR_SHAPE;
+  const int32_t rows = count > nodes ? count : nodes;
+  if (t < 0 || t > INT32_MAX - 64 - rows) return TEMPO_ERR_RANGE;
+  if ((rc = check_step(layers, t + rows - 1)) != TEMPO_OK) return rc;
+  if (layers->ring_blocks && (int64_t)rows > (int64_t)layers->ring_blocks * layers->block_size) return TEMPO_ERR_RANGE;
+  KeepParams p;
+  p.block_table = layers->block_table;
+  p.t_per_seq = t_per_seq;
+  p.kept = kept;
+  p.t = t;
+  p.z_log2 = ilog2_exact(layers->block_size);
+  p.max_blocks_per_seq = layers->max_blocks_per_seq;
+  p.tile_mask = tile_mask_of(layers);
+  p.num_blocks = layers->num_blocks;
+  p.Hkv = layers->num_kv_heads;
+  p.nodes = nodes;
+  p.count = count;
+  for (int32_t at = 0; at < num_layers; at += kKeepLayers) {
+    const int32_t n = num_layers - at < kKeepLayers ? num_layers - at : kKeepLayers;
+    for (int32_t i = 0; i < kKeepLayers; ++i) {
+      p.k_pool[i] = layers[at + (i < n ? i : 0)].k_pool;
+      p.v_pool[i] = layers[at + (i < n ? i : 0)].v_pool;
+    }
+    rc = launch_status(launch_keep(p, batch, n, layers->head_dim, layers->dtype, static_cast<hipStream_t>(stream)), "kv_keep");
+    if (rc != TEMPO_OK) return rc;
+  }
+  return TEMPO_OK;
+}
+
+}  // extern "C"

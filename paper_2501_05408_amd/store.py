@@ -267,6 +267,85 @@ class BlockStore:
                                      self.Hq, t, t_per_seq, self.scale if scale is None else scale, ws, nbytes)
         return out
 
+    # -- windows with sinks, trees of drafted tokens, rows at positions of their own -----------
+    @staticmethod
+    def sinks_table(batch, max_t, block_size, window, sinks, queries=1):
+        """(block table, number of blocks) for BlockStore(block_table=, num_blocks=): sequences of up to max_t steps, in calls of up to
+        `queries`, that keep their first `sinks` keys and a window in blocks that are used in turn."""
+        first, turn = T.tempo_sink_blocks(window, sinks, block_size, queries)
+        columns = max_t // block_size + 1
+        own = min(columns, first + turn)
+        n = torch.arange(columns)
+        n = torch.where(n < first, n, first + (n - first) % turn) if own < columns else n
+        return (n[None] + own * torch.arange(batch)[:, None]).to(torch.int32), batch * own
+
+    def _spans_ws(self, nbytes):
+        if nbytes == 0:
+            raise T.TempoError(T.TEMPO_ERR_SHAPE, "workspace of the attention over spans")
+        ws = self._kept_ws("_span_ws", nbytes)
+        return ws, ws.numel()
+
+    def _last_first_step(self, rows):
+        return max(0, min(self.max_t, 2 ** 31 - 256) - rows + 1)
+
+    def attend_sinks(self, q, out, t, queries, window, sinks, t_per_seq=None, scale=None):
+        """Steps t .. t+queries-1 over their window and the first `sinks` keys; q, out [batch][queries][Hq][D]."""
+        ws, nbytes = self._spans_ws(T.tempo_attn_sinks_workspace_bytes(self.kv, self.batch, self.Hq, queries, self._last_first_step(queries),
+                                                                       window, sinks))
+        T.tempo_attn_sinks(self.kv, q, out, self.batch, self.Hq, queries, t, t_per_seq, window, sinks,
+                           self.scale if scale is None else scale, ws, nbytes)
+        return out
+
+    def step_sinks(self, q, k_new, v_new, out, t, window, sinks, t_per_seq=None, scale=None, rope=False):
+        """Append step t and attend over its window and the first `sinks` keys.  rope=True: q and k_new arrive unrotated."""
+        ws, nbytes = self._spans_ws(T.tempo_attn_sinks_workspace_bytes(self.kv, self.batch, self.Hq, 1, self._last_first_step(1), window, sinks))
+        s = self.scale if scale is None else scale
+        if rope:
+            T.tempo_rope_decode_step_sinks(self.kv, self.rope, q, k_new, v_new, out, self.batch, self.Hq, t, t_per_seq, window, sinks, s,
+                                           ws, nbytes)
+        else:
+            T.tempo_decode_step_sinks(self.kv, q, k_new, v_new, out, self.batch, self.Hq, t, t_per_seq, window, sinks, s, ws, nbytes)
+        return out
+
+    def prefill_sinks(self, q, k_new, v_new, out, t, count, window, sinks, count_per_seq=None, scale=None, rope=False):
+        """Write steps t .. t+count-1 and answer them over their windows and the first `sinks` keys."""
+        ws, nbytes = self._spans_ws(T.tempo_prefill_sinks_workspace_bytes(self.kv, self.batch, self.Hq, min(self.max_t, 2 ** 31 - 256)))
+        s = self.scale if scale is None else scale
+        if rope:
+            T.tempo_rope_prefill_sinks(self.kv, self.rope, q, k_new, v_new, out, self.batch, self.Hq, t, count, count_per_seq, window, sinks,
+                                       s, ws, nbytes)
+        else:
+            T.tempo_prefill_sinks(self.kv, q, k_new, v_new, out, self.batch, self.Hq, t, count, count_per_seq, window, sinks, s, ws, nbytes)
+        return out
+
+    def tree_positions(self, parents, t, t_per_seq=None):
+        """Positions (t + depth) of the nodes of `parents` [batch][nodes], int32."""
+        positions = torch.empty_like(parents)
+        T.tempo_tree_positions(parents, positions, parents.shape[0], parents.shape[1], t, t_per_seq)
+        return positions
+
+    def attend_tree(self, q, out, parents, t, nodes_per_seq=None, window=0, sinks=0, t_per_seq=None, scale=None):
+        """The nodes of a tree, whose rows lie at steps t .. t+nodes-1; q, out [batch][nodes][Hq][D]."""
+        nodes = parents.shape[1]
+        ws, nbytes = self._spans_ws(T.tempo_attn_tree_workspace_bytes(self.kv, self.batch, self.Hq, nodes, self._last_first_step(nodes),
+                                                                      window, sinks))
+        T.tempo_attn_tree(self.kv, q, out, parents, nodes_per_seq, self.batch, self.Hq, nodes, t, t_per_seq, window, sinks,
+                          self.scale if scale is None else scale, ws, nbytes)
+        return out
+
+    def keep(self, kept, t, nodes, t_per_seq=None, layers=None):
+        """The rows t + kept[b][i] (int32 [batch][count]; up to the first negative one) become rows t + i; layers: the stores of all
+        layers (this one among them), which share the block table."""
+        kvs = T.make_kv_layers([s.kv for s in layers] if layers else [self.kv])
+        T.tempo_kv_keep(kvs, len(kvs), self.batch, t, t_per_seq, nodes, kept, kept.shape[1])
+
+    def rope_append_at(self, positions, k_raw, v_new, t, q_raw=None, q_out=None, t_per_seq=None, count_per_seq=None, axes=None):
+        """Rows [batch][count][Hkv][D] to steps t .., keys turned to positions [batch][count][axes] (set_rope tables); queries
+        [batch][count][Hq][D] turned into q_out."""
+        T.tempo_rope_kv_append_at(self.kv, self.rope, axes, positions, k_raw, v_new, q_raw, q_out, self.batch, self.Hq, t, t_per_seq,
+                                  k_raw.shape[1], count_per_seq)
+        return q_out
+
     def attend_with_plan(self, q, out, t, plan, window=0, t_per_seq=None, scale=None):
         """Partial + combine with an explicit plan (its own workspace)."""
         nbytes = T.tempo_attn_plan_workspace_bytes(self.kv, self.batch, self.Hq, plan)

@@ -65,6 +65,13 @@ class tempo_rope(ctypes.Structure):
     ]
 
 
+class tempo_rope_axes(ctypes.Structure):
+    _fields_ = [
+        ("axes", ctypes.c_int32),
+        ("axis_of_pair", ctypes.c_uint8 * 64),
+    ]
+
+
 class TempoError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -78,6 +85,7 @@ _vp = ctypes.c_void_p
 _kvp = ctypes.POINTER(tempo_kv)
 _planp = ctypes.POINTER(tempo_plan)
 _ropep = ctypes.POINTER(tempo_rope)
+_axesp = ctypes.POINTER(tempo_rope_axes)
 _i32p = ctypes.POINTER(ctypes.c_int32)
 
 # name -> (restype, argtypes); kept in the order of include/tempo.h
@@ -156,6 +164,25 @@ SIGNATURES = {
     "tempo_step_selected_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32, _i32]),
     "tempo_decode_step_selected": (ctypes.c_int, [_kvp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _i32,
                                                   _vp, ctypes.c_float, _vp, ctypes.c_size_t, _vp]),
+    "tempo_sink_blocks": (ctypes.c_int, [_i32, _i32, _i32, _i32, _i32p, _i32p]),
+    "tempo_attn_sinks_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32, _i32, _i32, _i32]),
+    "tempo_attn_sinks": (ctypes.c_int, [_kvp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32, _i32, ctypes.c_float, _vp, ctypes.c_size_t, _vp]),
+    "tempo_decode_step_sinks": (ctypes.c_int, [_kvp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _i32, ctypes.c_float, _vp,
+                                               ctypes.c_size_t, _vp]),
+    "tempo_rope_decode_step_sinks": (ctypes.c_int, [_kvp, _ropep, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _i32, ctypes.c_float,
+                                                    _vp, ctypes.c_size_t, _vp]),
+    "tempo_prefill_sinks_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32]),
+    "tempo_prefill_sinks": (ctypes.c_int, [_kvp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32, _i32, ctypes.c_float, _vp,
+                                           ctypes.c_size_t, _vp]),
+    "tempo_rope_prefill_sinks": (ctypes.c_int, [_kvp, _ropep, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32, _i32, ctypes.c_float,
+                                                _vp, ctypes.c_size_t, _vp]),
+    "tempo_tree_positions": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, _vp, _vp]),
+    "tempo_attn_tree_workspace_bytes": (ctypes.c_size_t, [_kvp, _i32, _i32, _i32, _i32, _i32, _i32]),
+    "tempo_attn_tree": (ctypes.c_int, [_kvp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32, _i32, ctypes.c_float, _vp,
+                                       ctypes.c_size_t, _vp]),
+    "tempo_kv_keep": (ctypes.c_int, [_kvp, _i32, _i32, _i32, _vp, _i32, _vp, _i32, _vp]),
+    "tempo_rope_rotate_at": (ctypes.c_int, [_ropep, _axesp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp]),
+    "tempo_rope_kv_append_at": (ctypes.c_int, [_kvp, _ropep, _axesp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _i32, _vp, _vp]),
     "tempo_discounted_sum": (ctypes.c_int, [_vp, _vp, _i32, _i32, _i32, ctypes.c_float, _vp]),
     "tempo_stream_read": (ctypes.c_int, [_vp, ctypes.c_size_t, _vp, _i32, _vp]),
     "tempo_stream_copy": (ctypes.c_int, [_vp, _vp, ctypes.c_size_t, _i32, _vp]),
@@ -251,6 +278,20 @@ def make_kv(k_pool, v_pool, block_table, num_blocks, max_blocks_per_seq, block_s
 def make_rope(cos_table, sin_table, head_dim) -> tempo_rope:
     """Fill a tempo_rope descriptor from two [positions][head_dim/2] fp32 device tensors."""
     return tempo_rope(_ptr(cos_table), _ptr(sin_table), int(cos_table.shape[0]), head_dim)
+
+
+def make_rope_axes(axis_of_pair) -> tempo_rope_axes:
+    """The axis (0 .. 3) of each of the head_dim/2 rotated pairs."""
+    axis_of_pair = [int(a) for a in axis_of_pair]
+    if not 1 <= len(axis_of_pair) <= 64 or not all(0 <= a <= 255 for a in axis_of_pair):
+        raise TempoError(TEMPO_ERR_SHAPE, "make_rope_axes")
+    return tempo_rope_axes(max(axis_of_pair) + 1, (ctypes.c_uint8 * 64)(*axis_of_pair))
+
+
+def make_kv_layers(stores):
+    """An array of the layers' tempo_kv descriptors, as tempo_kv_keep takes it (a copy; the caller keeps the tensors alive)."""
+    stores = list(stores)
+    return (tempo_kv * len(stores))(*stores)
 
 
 # ---- pure host functions -------------------------------------------------------
@@ -572,6 +613,89 @@ def tempo_decode_step_selected(kv, bounds, q, k_new, v_new, out, selected, count
                                              _ptr(selected), count, first, last, batch, num_q_heads, t, _ptr(t_per_seq),
                                              scale, _ptr(workspace), workspace_bytes, _stream(stream)),
            "tempo_decode_step_selected")
+
+
+def tempo_sink_blocks(window: int, sinks: int, Z: int, queries: int = 1):
+    """(sink_blocks, window_blocks): blocks a sequence needs for windows with sinks."""
+    first, turn = ctypes.c_int32(0), ctypes.c_int32(0)
+    _check(load().tempo_sink_blocks(window, sinks, Z, queries, ctypes.byref(first), ctypes.byref(turn)), "tempo_sink_blocks")
+    return first.value, turn.value
+
+
+def tempo_attn_sinks_workspace_bytes(kv: tempo_kv, batch: int, num_q_heads: int, queries: int, max_t: int, window: int, sinks: int) -> int:
+    return load().tempo_attn_sinks_workspace_bytes(ctypes.byref(kv), batch, num_q_heads, queries, max_t, window, sinks)
+
+
+def tempo_attn_sinks(kv, q, out, batch, num_q_heads, queries, t, t_per_seq, window, sinks, scale, workspace, workspace_bytes,
+                     stream=None):
+    _check(load().tempo_attn_sinks(ctypes.byref(kv), _ptr(q), _ptr(out), batch, num_q_heads, queries, t, _ptr(t_per_seq), window, sinks,
+                                   scale, _ptr(workspace), workspace_bytes, _stream(stream)), "tempo_attn_sinks")
+
+
+def tempo_decode_step_sinks(kv, q, k_new, v_new, out, batch, num_q_heads, t, t_per_seq, window, sinks, scale, workspace,
+                            workspace_bytes, stream=None):
+    _check(load().tempo_decode_step_sinks(ctypes.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), batch, num_q_heads, t,
+                                          _ptr(t_per_seq), window, sinks, scale, _ptr(workspace), workspace_bytes, _stream(stream)),
+           "tempo_decode_step_sinks")
+
+
+def tempo_rope_decode_step_sinks(kv, rope, q_raw, k_raw, v_new, out, batch, num_q_heads, t, t_per_seq, window, sinks, scale,
+                                 workspace, workspace_bytes, stream=None):
+    _check(load().tempo_rope_decode_step_sinks(ctypes.byref(kv), ctypes.byref(rope), _ptr(q_raw), _ptr(k_raw), _ptr(v_new), _ptr(out),
+                                               batch, num_q_heads, t, _ptr(t_per_seq), window, sinks, scale, _ptr(workspace),
+                                               workspace_bytes, _stream(stream)), "tempo_rope_decode_step_sinks")
+
+
+def tempo_prefill_sinks_workspace_bytes(kv: tempo_kv, batch: int, num_q_heads: int, max_t: int) -> int:
+    return load().tempo_prefill_sinks_workspace_bytes(ctypes.byref(kv), batch, num_q_heads, max_t)
+
+
+def tempo_prefill_sinks(kv, q, k_new, v_new, out, batch, num_q_heads, t, count, count_per_seq, window, sinks, scale, workspace,
+                        workspace_bytes, stream=None):
+    _check(load().tempo_prefill_sinks(ctypes.byref(kv), _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(out), batch, num_q_heads, t, count,
+                                      _ptr(count_per_seq), window, sinks, scale, _ptr(workspace), workspace_bytes, _stream(stream)),
+           "tempo_prefill_sinks")
+
+
+def tempo_rope_prefill_sinks(kv, rope, q_raw, k_raw, v_new, out, batch, num_q_heads, t, count, count_per_seq, window, sinks, scale,
+                             workspace, workspace_bytes, stream=None):
+    _check(load().tempo_rope_prefill_sinks(ctypes.byref(kv), ctypes.byref(rope), _ptr(q_raw), _ptr(k_raw), _ptr(v_new), _ptr(out), batch,
+                                           num_q_heads, t, count, _ptr(count_per_seq), window, sinks, scale, _ptr(workspace),
+                                           workspace_bytes, _stream(stream)), "tempo_rope_prefill_sinks")
+
+
+def tempo_tree_positions(parents, positions, batch, nodes, t, t_per_seq=None, stream=None):
+    _check(load().tempo_tree_positions(_ptr(parents), _ptr(positions), batch, nodes, t, _ptr(t_per_seq), _stream(stream)),
+           "tempo_tree_positions")
+
+
+def tempo_attn_tree_workspace_bytes(kv: tempo_kv, batch: int, num_q_heads: int, nodes: int, max_t: int, window: int = 0, sinks: int = 0) -> int:
+    return load().tempo_attn_tree_workspace_bytes(ctypes.byref(kv), batch, num_q_heads, nodes, max_t, window, sinks)
+
+
+def tempo_attn_tree(kv, q, out, parents, nodes_per_seq, batch, num_q_heads, nodes, t, t_per_seq, window, sinks, scale, workspace,
+                    workspace_bytes, stream=None):
+    _check(load().tempo_attn_tree(ctypes.byref(kv), _ptr(q), _ptr(out), _ptr(parents), _ptr(nodes_per_seq), batch, num_q_heads, nodes, t,
+                                  _ptr(t_per_seq), window, sinks, scale, _ptr(workspace), workspace_bytes, _stream(stream)),
+           "tempo_attn_tree")
+
+
+def tempo_kv_keep(layers, num_layers, batch, t, t_per_seq, nodes, kept, count, stream=None):
+    """layers: a tempo_kv, or an array of them (make_kv_layers)."""
+    at = layers if isinstance(layers, ctypes.Array) else ctypes.byref(layers)
+    _check(load().tempo_kv_keep(at, num_layers, batch, t, _ptr(t_per_seq), nodes, _ptr(kept), count, _stream(stream)), "tempo_kv_keep")
+
+
+def tempo_rope_rotate_at(rope, axes, positions, x, y, dtype, batch, count, heads, stream=None):
+    _check(load().tempo_rope_rotate_at(ctypes.byref(rope), None if axes is None else ctypes.byref(axes), _ptr(positions), _ptr(x), _ptr(y),
+                                       dtype, batch, count, heads, _stream(stream)), "tempo_rope_rotate_at")
+
+
+def tempo_rope_kv_append_at(kv, rope, axes, positions, k_raw, v_new, q_raw, q_out, batch, num_q_heads, t, t_per_seq, count,
+                            count_per_seq=None, stream=None):
+    _check(load().tempo_rope_kv_append_at(ctypes.byref(kv), ctypes.byref(rope), None if axes is None else ctypes.byref(axes),
+                                          _ptr(positions), _ptr(k_raw), _ptr(v_new), _ptr(q_raw), _ptr(q_out), batch, num_q_heads, t,
+                                          _ptr(t_per_seq), count, _ptr(count_per_seq), _stream(stream)), "tempo_rope_kv_append_at")
 
 
 def tempo_discounted_sum(r, g, batch, T, n, gamma, stream=None):

@@ -1,0 +1,243 @@
+"""Rows at positions of their own, and the keeping of accepted rows, on the GPU against their definitions in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from e4m3_reference import held
+from paper_2501_05408_amd import synth
+from paper_2501_05408_amd import tempo as T
+from paper_2501_05408_amd.store import BlockStore
+from spans_reference import turned
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+STORES = [T.TEMPO_BF16, T.TEMPO_E4M3, T.TEMPO_F32]
+
+
+def dtype_of(dtype):
+    return torch.float32 if dtype == T.TEMPO_F32 else torch.bfloat16
+
+
+def on_gpu(x, dtype):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(DEV).to(dtype_of(dtype))
+
+
+def np64(x):
+    return x.detach().float().cpu().numpy().astype(np.float64)
+
+
+def ints(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(DEV)
+
+
+def normal(seed, which, shape):
+    return synth.normal_as(seed, which, shape, "bf16").astype(np.float64)
+
+
+def make_store(seed, dtype, B, Hq, Hkv, D, Z, max_t, ring=0):
+    columns = ring if ring else max_t // Z + 1
+    n = B * columns + 2
+    table = torch.from_numpy(synth.permutation(seed, 77, n)[:B * columns].reshape(B, columns).copy())
+    st = BlockStore(B, Hq, Hkv, D, Z, max_t, dtype, device=DEV, num_blocks=n, block_table=table, ring_blocks=ring)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    for pool in (st.k_pool, st.v_pool):  # something recognisable everywhere
+        if dtype == T.TEMPO_E4M3:
+            pool.copy_(torch.randint(0, 120, pool.shape, generator=g, device=DEV, dtype=torch.uint8))
+        else:
+            pool.normal_(generator=g)
+    return st
+
+
+def tables(positions, D, seed=0):
+    a = (np.arange(positions)[:, None] + 0.3 * seed) * 10000.0 ** (-np.arange(D // 2) * 2 / D)
+    c, s = np.cos(a).astype(np.float32), np.sin(a).astype(np.float32)
+    return torch.from_numpy(c).to(DEV), torch.from_numpy(s).to(DEV), c.astype(np.float64), s.astype(np.float64)
+
+
+def near_turned(got, x, cos, sin, dtype):
+    """One product and one fused multiply-add in fp32 (2^-24 of the product, 2^-24 of the result), then one rounding."""
+    ref = turned(x, cos, sin)
+    both = np.concatenate([np.abs(x[..., :x.shape[-1] // 2]) * np.abs(cos) + np.abs(x[..., x.shape[-1] // 2:]) * np.abs(sin),
+                           np.abs(x[..., x.shape[-1] // 2:]) * np.abs(cos) + np.abs(x[..., :x.shape[-1] // 2]) * np.abs(sin)], axis=-1)
+    fp32 = 2.0 ** -23 * 1.01 * both
+    bound = fp32 if dtype == T.TEMPO_F32 else 2.0 ** -8 * (np.abs(ref) + fp32) + fp32
+    assert (np.abs(got - ref) <= bound + 1e-37).all()
+
+
+AXES = [  # axis of each pair, by head_dim / 2
+    lambda h: None,
+    lambda h: [0] * h,
+    lambda h: [0] * (h // 4) + [1] * (3 * h // 8) + [2] * (h - h // 4 - 3 * h // 8),
+    lambda h: [i % 3 for i in range(h)],
+    lambda h: [(i * 5 // 7) % 4 for i in range(h)],
+    lambda h: [1] * 5 + [0] * (h - 5),
+]
+
+
+@pytest.mark.parametrize("dtype", STORES)
+@pytest.mark.parametrize("Hq,Hkv,D,Z,B,t,count,ragged,counts,axes", [
+    (6, 2, 128, 32, 2, 0, 1, False, False, 0), (6, 2, 128, 64, 3, 45, 33, True, True, 2), (4, 4, 64, 32, 3, 31, 40, False, True, 3),
+    (24, 8, 128, 64, 1, 7, 200, False, False, 2), (3, 1, 64, 64, 2, 100, 5, True, False, 4), (0, 2, 128, 32, 2, 60, 100, False, False, 5),
+    (100, 1, 64, 32, 1, 64, 64, False, False, 1), (8, 8, 64, 256, 2, 200, 130, True, True, 0)])
+def test_rows_at_their_positions(dtype, Hq, Hkv, D, Z, B, t, count, ragged, counts, axes):
+    rng = np.random.default_rng(t + count)
+    axis = AXES[axes](D // 2)
+    n_axes = 1 if axis is None else max(axis) + 1
+    rows = 500
+    c_dev, s_dev, c, s = tables(rows, D)
+    rope, ax = T.make_rope(c_dev, s_dev, D), None if axis is None else T.make_rope_axes(axis)
+    positions = rng.integers(-3, rows + 3, (B, count, n_axes))
+    steps = np.array([t] + [int(rng.integers(0, t + 1)) for _ in range(B - 1)]) if ragged else np.full(B, t)
+    n = np.array([count, 0, count // 2])[:B] if counts else np.full(B, count)
+    q, k, v = normal(1, 1, (B, count, max(Hq, 1), D)), normal(1, 2, (B, count, Hkv, D)), normal(1, 3, (B, count, Hkv, D))
+    st = make_store(2, dtype, B, Hq or Hkv, Hkv, D, Z, t + count + 40)
+    old = [np64(x) for x in st.gather(0, t + count + 41)]
+    qd = on_gpu(q, dtype)
+    out = torch.full_like(qd, 7.0)
+    T.tempo_rope_kv_append_at(st.kv, rope, ax, ints(positions), on_gpu(k, dtype), on_gpu(v, dtype), qd if Hq else None, out if Hq else None, B,
+                              Hq, t, ints(steps) if ragged else None, count, ints(n) if counts else None)
+    new = [np64(x) for x in st.gather(0, t + count + 41)]
+    at = np.clip(positions, 0, rows - 1)[:, :, [0] * (D // 2) if axis is None else axis]          # [B][count][D/2]
+    cos, sin = (x[at, np.arange(D // 2)][:, :, None] for x in (c, s))
+    for b in range(B):
+        lo, hi = steps[b], steps[b] + n[b]
+        for which in (0, 1):
+            np.testing.assert_array_equal(new[which][b, :lo], old[which][b, :lo])
+            np.testing.assert_array_equal(new[which][b, hi:], old[which][b, hi:])
+        np.testing.assert_array_equal(new[1][b, lo:hi], held(v[b, :n[b]]) if dtype == T.TEMPO_E4M3 else v[b, :n[b]])
+        if dtype != T.TEMPO_E4M3:
+            near_turned(new[0][b, lo:hi], k[b, :n[b]], cos[b, :n[b]], sin[b, :n[b]], dtype)
+        if Hq:
+            near_turned(np64(out)[b, :n[b]], q[b, :n[b]], cos[b, :n[b]], sin[b, :n[b]], dtype)
+            assert (np64(out)[b, n[b]:] == 7.0).all()
+    if dtype == T.TEMPO_E4M3:  # the codes of the rotated rows as bf16 rows have them
+        kr = on_gpu(k, dtype)
+        T.tempo_rope_rotate_at(rope, ax, ints(positions), kr, kr, T.TEMPO_BF16, B, count, Hkv)
+        for b in range(B):
+            near_turned(np64(kr)[b], k[b], cos[b], sin[b], dtype)
+            np.testing.assert_array_equal(new[0][b, steps[b]:steps[b] + n[b]], held(np64(kr)[b, :n[b]]))
+
+
+@pytest.mark.parametrize("dtype", [T.TEMPO_BF16, T.TEMPO_E4M3])
+@pytest.mark.parametrize("D,t,count,ragged", [(128, 45, 70, False), (64, 0, 33, False), (128, 100, 3, True), (64, 95, 64, True)])
+def test_positions_that_are_the_steps(dtype, D, t, count, ragged):
+    """The bits of tempo_rope_kv_append_block and tempo_rope_rotate."""
+    B, Hq, Hkv, Z = 2, 6, 2, 32
+    steps = np.array([t, t // 2]) if ragged else np.full(B, t)
+    c_dev, s_dev, _, _ = tables(t + count, D)
+    k, v, q = (on_gpu(normal(3, w, (B, count, h, D)), dtype) for w, h in ((1, Hkv), (2, Hkv), (3, Hq)))
+    a, b = (make_store(4, dtype, B, Hq, Hkv, D, Z, t + count - 1) for _ in range(2))
+    a.set_rope(c_dev, s_dev), b.set_rope(c_dev, s_dev)
+    given = ints(steps) if ragged else None
+    a.rope_append_block(k, v, t, count, given)
+    positions = ints(steps[:, None] + np.arange(count))
+    out = torch.empty_like(q)
+    b.rope_append_at(positions, k, v, t, q, out, given)
+    for x, y in ((a.k_pool, b.k_pool), (a.v_pool, b.v_pool)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    for i in range(count):
+        one = torch.empty_like(q[:, i])
+        a.rope_rotate(q[:, i].contiguous(), one, t + i, ints(steps + i))
+        assert torch.equal(one, out[:, i])
+
+
+@pytest.mark.parametrize("dtype", [T.TEMPO_BF16, T.TEMPO_F32])
+@pytest.mark.parametrize("D,B,count,heads,axes", [(128, 1, 1, 1, 0), (64, 3, 50, 7, 3), (128, 2, 301, 5, 2)])
+def test_rotation_in_place(dtype, D, B, count, heads, axes):
+    axis = AXES[axes](D // 2)
+    rng = np.random.default_rng(9)
+    c_dev, s_dev, c, s = tables(300, D)
+    positions = rng.integers(0, 300, (B, count, 1 if axis is None else max(axis) + 1))
+    x = normal(5, 1, (B, count, heads, D))
+    rope, ax = T.make_rope(c_dev, s_dev, D), None if axis is None else T.make_rope_axes(axis)
+    same = on_gpu(x, dtype)
+    other = torch.empty_like(same)
+    T.tempo_rope_rotate_at(rope, ax, ints(positions), same, other, dtype, B, count, heads)
+    T.tempo_rope_rotate_at(rope, ax, ints(positions), same, same, dtype, B, count, heads)
+    assert torch.equal(same, other)
+    at = positions[:, :, [0] * (D // 2) if axis is None else axis]
+    near_turned(np64(same), x, c[at, np.arange(D // 2)][:, :, None], s[at, np.arange(D // 2)][:, :, None], dtype)
+
+
+@pytest.mark.parametrize("dtype", STORES)
+def test_rows_on_a_ring_and_with_values_that_are_not_finite(dtype):
+    B, Hq, Hkv, D, Z, ring, t, count = 2, 4, 2, 64, 32, 4, 1000, 128
+    c_dev, s_dev, c, s = tables(50, D)
+    st = make_store(6, dtype, B, Hq, Hkv, D, Z, t + count, ring)
+    st.set_rope(c_dev, s_dev)
+    k, v = normal(7, 1, (B, count, Hkv, D)), normal(7, 2, (B, count, Hkv, D))
+    v[0, 3, 1, 7], v[1, 100, 0, 60] = np.inf, np.nan
+    positions = np.random.default_rng(1).integers(0, 50, (B, count, 1))
+    st.rope_append_at(ints(positions), on_gpu(k, dtype), on_gpu(v, dtype), t)
+    k_back, v_back = (np64(x) for x in st.gather(t, count))
+    np.testing.assert_array_equal(v_back, held(v) if dtype == T.TEMPO_E4M3 else v)
+    if dtype != T.TEMPO_E4M3:
+        at = positions[..., [0] * (D // 2)]
+        near_turned(k_back, k, c[at, np.arange(D // 2)][:, :, None], s[at, np.arange(D // 2)][:, :, None], dtype)
+
+
+# ---- kept rows ------------------------------------------------------------------------------------------
+
+def rows_of(st, upto):
+    return [x.clone() for x in st.gather(0, upto)]
+
+
+def same(a, b):
+    return torch.equal(torch.nan_to_num(a.float(), nan=12345.0), torch.nan_to_num(b.float(), nan=12345.0))
+
+
+@pytest.mark.parametrize("dtype", STORES)
+@pytest.mark.parametrize("Hkv,D,Z,B,t,nodes,ragged,layers,kept", [
+    (2, 128, 32, 3, 20, 30, False, 1, [[0, 2, 5, 17, -1], [0, 1, 2, 3, 4], [-1, 4, 5, 6, 7]]),
+    (2, 64, 64, 2, 100, 64, True, 3, [[0, 9, 40, 63], [3, 7, 30, -1]]),
+    (1, 128, 32, 2, 0, 9, False, 70, [[8, -1, 0], [5, 5, 4]]),          # any order, the same row twice
+    (3, 64, 32, 2, 31, 6, True, 2, [[0, 5, 6, 1], [2 ** 31 - 1, 1, 2, 3]]),  # an entry behind the nodes ends the list
+    (2, 64, 32, 1, 5, 1, False, 1, [[0]]),
+    (1, 64, 32, 1, 77, 256, False, 1, [[255 - 2 * i for i in range(128)]]),
+])
+def test_kept_rows(dtype, Hkv, D, Z, B, t, nodes, ragged, layers, kept):
+    steps = np.array([t, t // 2, t // 3])[:B] if ragged else np.full(B, t)
+    upto = t + max(nodes, len(kept[0]))
+    stores = [make_store(10 + i, dtype, B, Hkv, Hkv, D, Z, upto - 1) for i in range(layers)]
+    for st in stores:
+        st.block_table = stores[0].block_table
+        st.kv.block_table = stores[0].block_table.data_ptr()
+    old = [rows_of(st, upto) for st in stores]
+    stores[0].keep(ints(kept), t, nodes, ints(steps) if ragged else None, layers=stores)
+    for st, was in zip(stores, old):
+        for x, y in zip(rows_of(st, upto), was):
+            ref = y.clone()
+            for b in range(B):
+                for i, n in enumerate(kept[b]):
+                    if not 0 <= n < nodes:
+                        break
+                    ref[b, steps[b] + i] = y[b, steps[b] + n]
+            assert same(x, ref)
+
+
+def test_keeping_on_a_ring_and_captured():
+    B, Hkv, D, Z, t, nodes = 2, 2, 128, 32, 1000, 40
+    st = make_store(20, T.TEMPO_BF16, B, Hkv, Hkv, D, Z, 2000, 4)
+    kept, steps = ints([[0, 3, 20, 39], [1, 2, -1, -1]]), ints([t, t - 7])
+    graph = torch.cuda.CUDAGraph()
+    start = [st.k_pool.clone(), st.v_pool.clone()]
+    with torch.cuda.graph(graph):
+        st.keep(kept, t, nodes, steps)
+    for turn in range(3):
+        st.k_pool.copy_(start[0]), st.v_pool.copy_(start[1])
+        lists = np.array([[0, 3 + turn, 20, 39 - turn], [1, 2 + turn, -1, -1]])
+        at = np.array([t + turn - 5, t - 7])
+        kept.copy_(ints(lists)), steps.copy_(ints(at))
+        was = [x.clone() for x in st.gather(t - 30, 100)]
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(st.gather(t - 30, 100), was):
+            ref = y.clone()
+            for b in range(B):
+                for i, n in enumerate(lists[b]):
+                    if n < 0:
+                        break
+                    ref[b, at[b] - t + 30 + i] = y[b, at[b] - t + 30 + n]
+            assert torch.equal(x, ref)
