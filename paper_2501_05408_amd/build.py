@@ -23,7 +23,7 @@ SOURCES = ["tempo_api.hip", "kv_store.hip", "attn_partial_bf16.hip", "attn_parti
            "attn_combine.hip", "stream_read.hip", "rope.hip", "attn_prefill_bf16.hip", "attn_block_bf16.hip",
            "attn_stream_bf16.hip",
            "worklist.hip", "discounted_sum.hip", "kv_store_e4m3.hip", "attn_units.hip", "select_blocks.hip",
-           "attn_spans.hip", "kv_place.hip"]
+           "attn_spans.hip", "attn_spans_wide.hip", "kv_place.hip"]
 HEADERS = [os.path.join(CSRC, "tempo_internal.h"), os.path.join(CSRC, "attn_bf16_common.h"),
            os.path.join(CSRC, "attn_bf16_columns32.h"), os.path.join(CSRC, "attn_combine.h"),
            os.path.join(CSRC, "store_e4m3.h"), os.path.join(CSRC, "attn_units.h"), os.path.join(CSRC, "attn_image.h"),

@@ -44,7 +44,7 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
   SpanPlan s;
   const int32_t G = Hq / kv->num_kv_heads;
   const int64_t columns = (int64_t)rows * G;
-  s.tile_columns = columns <= 16 ? 16 : 32;
+  s.tile_columns = columns <= 16 ? 16 : columns <= 32 ? 32 : 128;
   s.tiles = (int32_t)((columns + s.tile_columns - 1) / s.tile_columns);
   int32_t tile_rows = (s.tile_columns + G - 2) / G + 1;
   tile_rows = tree || tile_rows > rows ? rows : tile_rows;
@@ -66,8 +66,8 @@ size_t span_bytes(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, c
 
 // Rows of the partials of any call with at most `rows` rows a sequence whose last step is at most max_t.
 size_t span_bytes_bound(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t max_t) {
-  // splits only where there are fewer than kSpanWorkgroups tiles of up to 32 columns: rows * splits is at most 32 times as many
-  const int64_t all = (int64_t)batch * rows * Hq, groups = max_t / 32 + 1, most = 2 * 32 * kSpanWorkgroups;
+  // splits only where there are fewer than kSpanWorkgroups tiles of up to 128 columns: rows * splits is at most 128 times as many
+  const int64_t all = (int64_t)batch * rows * Hq, groups = max_t / 32 + 1, most = 128 * kSpanWorkgroups;
   const int64_t partials = all > most / groups ? most : all * groups;
   return plan_bytes(kv, partials, 1);
 }
@@ -90,7 +90,9 @@ int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* pa
     p.rope_cos = rope->cos;
     p.rope_sin = rope->sin;
   }
-  const int rc = launch_status(launch_spans(p, batch, kv->head_dim, kv->dtype, s.waves, stream), "attn_spans");
+  const int rc = launch_status(s.tile_columns > 32 ? launch_spans_wide(p, batch, kv->head_dim, kv->dtype, stream)
+                                                   : launch_spans(p, batch, kv->head_dim, kv->dtype, s.waves, stream),
+                               "attn_spans");
   if (rc != TEMPO_OK || p.direct) return rc;
   return launch_status(launch_combine_spans(p, batch, kv->head_dim, stream), "attn_spans_combine");
 }
