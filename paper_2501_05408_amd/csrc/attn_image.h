@@ -164,9 +164,9 @@ __device__ __forceinline__ u32x4 fetch_new_rows(const AttnParams& p, int b, int 
   return *reinterpret_cast<const u32x4*>(src);
 }
 
-// slot: the number of the group's first slot among the store's `slots`.
+// The rows of fetch_new_rows(), the key turned to its position.
 template <int D, bool kRope>
-__device__ __forceinline__ void write_new_rows(const AttnParams& p, u32x4 x, int t_b, int64_t slot, int64_t slots, bool store, int lane, uint8_t* stage) {
+__device__ __forceinline__ u32x4 turn_new_row(const AttnParams& p, u32x4 x, int t_b, int lane) {
   constexpr int LANES = D / 8;
   if (kRope) {  // the partner dims, D/2 away, lie in lane ^ (LANES / 2)
     u32x4 other;
@@ -177,6 +177,14 @@ __device__ __forceinline__ void write_new_rows(const AttnParams& p, u32x4 x, int
     rotate_pieces(p.rope_cos, p.rope_sin, t_b, D / 2, d % (D / 2), lo, hi);
     if (lane < LANES) x = d < D / 2 ? lo : hi;
   }
+  return x;
+}
+
+// slot: the number of the group's first slot among the store's `slots`.
+template <int D, bool kRope>
+__device__ __forceinline__ void write_new_rows(const AttnParams& p, u32x4 x, int t_b, int64_t slot, int64_t slots, bool store, int lane, uint8_t* stage) {
+  constexpr int LANES = D / 8;
+  x = turn_new_row<D, kRope>(p, x, t_b, lane);
   const RowPiece r = quantise_piece<D>(x);
   if (lane >= 2 * LANES) return;
   const bool value = lane >= LANES;
@@ -217,6 +225,50 @@ __device__ __forceinline__ void patch_values(int t_b, int lane, const uint8_t* s
   const uint32_t E = (uint32_t)stage[2 * D + 1] << shift;
   g.v_scales.x = tile == 0 ? (g.v_scales.x & others) | E : g.v_scales.x;
   g.v_scales.y = tile == 1 ? (g.v_scales.y & others) | E : g.v_scales.y;
+}
+
+// The same for a bf16 row: [key D][value D] in LDS.  (Only the row's own pieces are written: 16 bytes of a key, single values.)
+template <int D, bool kRope>
+__device__ __forceinline__ void write_new_rows_bf16(const AttnParams& p, u32x4 x, int t_b, int64_t slot, bool store, int lane, uint16_t* stage) {
+  constexpr int LANES = D / 8;
+  x = turn_new_row<D, kRope>(p, x, t_b, lane);
+  if (lane >= 2 * LANES) return;
+  *reinterpret_cast<u32x4*>(stage + lane * 8) = x;
+  if (!store) return;
+  const int part = lane % LANES;
+  if (lane < LANES) {
+    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(p.k_pool) + slot * D + tile_off_k_bf16(D, t_b & 31, 8 * part)) = x;
+  } else {
+    uint16_t* const to = static_cast<uint16_t*>(p.v_pool) + slot * D + tile_off_v_bf16(D, t_b & 31, 8 * part);  // dims 8 elements apart
+#pragma unroll
+    for (int e = 0; e < 8; ++e) to[8 * e] = (uint16_t)(x[e >> 1] >> (16 * (e & 1)));
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void patch_keys_bf16(int t_b, int lane, const uint16_t* stage, Image<D, false>& g) {
+  const int u = t_b & 31, row = u & 15, tile = u >> 4, c = lane >> 4;
+  if ((lane & 15) != row) return;
+#pragma unroll
+  for (int s = 0; s < D / 32; ++s) {
+    const u32x4 val = *reinterpret_cast<const u32x4*>(stage + 32 * s + 8 * c);
+    g.k[s] = tile == 0 ? val : g.k[s];
+    g.k[D / 32 + s] = tile == 1 ? val : g.k[D / 32 + s];
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void patch_values_bf16(int t_b, int lane, const uint16_t* stage, Image<D, false>& g) {
+  const int u = t_b & 31, row = u & 15, tile = u >> 4, n = lane & 15;
+  if ((lane >> 4) != (row >> 2)) return;
+  const int e = (row & 3) + 4 * tile;  // place of the slot among the lane's 8
+  const uint32_t shift = (e & 1) ? 16u : 0u, others = (e & 1) ? 0x0000FFFFu : 0xFFFF0000u;
+#pragma unroll
+  for (int dt = 0; dt < D / 16; ++dt) {
+    const uint32_t val = (uint32_t)stage[D + 16 * dt + n] << shift;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) g.v[dt][w] = w == (e >> 1) ? (g.v[dt][w] & others) | val : g.v[dt][w];
+  }
 }
 
 // Merge of the workgroup's wavefronts, as in attn_partial_bf16.hip; column j is column first_col + j of the call.

@@ -121,6 +121,20 @@ __global__ __launch_bounds__(512, D == 64 && CT == 2 ? 3 : 1) void attn_spans(Sp
     if (kRope) rotate_query<D>(p, position, lane, qreg[ct]);
   }
 
+  // A step's own row lies in the last group; the wavefront that comes to it writes the row (attn_image.h), unless another tile
+  // of columns does, and puts it among what it read.
+  int key_new = -1;
+  void* const stage = smem + nwaves * (32 + (all_cols < 16 ? all_cols : 16) * D);
+  if constexpr (!kTree) {
+    const int newest = rg.groups - 1;
+    if (p.k_new && newest < past && newest >= at && (newest - at) % nwaves == 0) {
+      key_new = span_group(rg, newest) << 5;
+      const u32x4 x = fetch_new_rows<D>(p, b, hkv, lane);
+      if constexpr (k8) write_new_rows<D, kRope>(p, x, t_b, slot_of(key_new), slots, first_col == 0, lane, static_cast<uint8_t*>(stage));
+      else write_new_rows_bf16<D, kRope>(p, x, t_b, slot_of(key_new), first_col == 0, lane, static_cast<uint16_t*>(stage));
+    }
+  }
+
   WaveState<D> st[CT];
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
@@ -133,6 +147,12 @@ __global__ __launch_bounds__(512, D == 64 && CT == 2 ? 3 : 1) void attn_spans(Sp
   // The group in the registers; `more`: and request the one whose first key is key_nxt.
   auto group = [&](int key_nxt, bool more) __attribute__((always_inline)) {
     const int64_t slot_nxt = more ? slot_of(key_nxt) : 0;
+    if constexpr (!kTree) {
+      if (key == key_new) {
+        if constexpr (k8) patch_keys<D>(t_b, lane, static_cast<const uint8_t*>(stage), g);
+        else patch_keys_bf16<D>(t_b, lane, static_cast<const uint16_t*>(stage), g);
+      }
+    }
     float x[CT][8];
     image_logits<D, k8, CT>(qreg, g, x);
     if (more) load_image_keys<D, k8>(p, slot_nxt, slots, lane, g);
@@ -150,6 +170,12 @@ __global__ __launch_bounds__(512, D == 64 && CT == 2 ? 3 : 1) void attn_spans(Sp
     u32x4 w[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) w[ct] = softmax_weights<D, (CT > 1)>(x[ct], p.scale_log2e, lane, st[ct]);
+    if constexpr (!kTree) {
+      if (key == key_new) {
+        if constexpr (k8) patch_values<D>(t_b, lane, static_cast<const uint8_t*>(stage), g);
+        else patch_values_bf16<D>(t_b, lane, static_cast<const uint16_t*>(stage), g);
+      }
+    }
     if (cut) {  // slots that no row sees may be unwritten: values of 0 under the weight of 0
       uint32_t keep[4];
       keep_span<k8>(key, rg.lo, last, p.sinks, lane, keep);
@@ -306,7 +332,7 @@ template <int D, bool k8, bool kTree, bool kRope, int CT>
 hipError_t launch_tiles(const SpanParams& p, int batch, int waves, hipStream_t stream) {
   const int columns = p.queries * p.G, tiles = (columns + 16 * CT - 1) / (16 * CT);
   const dim3 grid((unsigned)(p.Hkv * tiles), (unsigned)batch, (unsigned)p.num_splits), block(64 * waves);
-  const size_t merge = units_lds_bytes(waves, columns, D), tree = kTree ? tree_lds_bytes(p.queries) : 0;
+  const size_t merge = units_lds_bytes(waves, columns, D) + 2 * D, tree = kTree ? tree_lds_bytes(p.queries) : 0;
   return launch((attn_spans<D, k8, kTree, kRope, CT>), grid, block, merge > tree ? merge : tree, stream, p);
 }
 

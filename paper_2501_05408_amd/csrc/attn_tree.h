@@ -32,9 +32,47 @@ struct Tree {
   }
 };
 
+// Up to 64 rows: every wavefront does it in its registers, a lane a row, and writes the same words as the others, so that nobody
+// waits for anybody (8 nodes of one sequence behind 300 keys: 13.9 us a call with barriers between eight wavefronts, 10.6 without).
+__device__ inline Tree small_tree_of(const int32_t* parents, int rows, int window, int sinks, int t, uint32_t* lds) {
+  const int words = tree_words(rows), stride = tree_stride(rows), lane = threadIdx.x & 63;
+  int32_t* const depths = reinterpret_cast<int32_t*>(lds + rows * stride) + rows;
+  const int parent = parents[lane < rows ? lane : 0];
+  int up = lane < rows && parent >= 0 && parent < lane ? parent : -1;
+  uint32_t low = lane < 32 ? 1u << lane : 0u, high = lane < 32 ? 0u : 1u << (lane - 32);
+  while (__any(up >= 0)) {
+    const int above = up >= 0 ? up : lane;
+    const uint32_t a = (uint32_t)__shfl((int)low, above), z = (uint32_t)__shfl((int)high, above);
+    const int next = __shfl(up, above);
+    low |= a;
+    high |= z;
+    up = up >= 0 ? next : -1;
+  }
+  const int depth = __builtin_popcount(low) + __builtin_popcount(high) - 1;
+  if (window > 0 && __any(depth >= window)) {
+    uint64_t left = ((uint64_t)high << 32) | low;
+    while (__any(left != 0)) {  // (uniform: the lanes' depths are asked for)
+      const int bit = left ? __builtin_ctzll(left) : lane;
+      const int other = __shfl(depth, bit);
+      if (left && depth - other >= window && t + other >= sinks) {
+        if (bit < 32) low &= ~(1u << bit);
+        else high &= ~(1u << (bit - 32));
+      }
+      left &= left - 1;
+    }
+  }
+  if (lane < rows) {
+    lds[lane * stride] = low;
+    if (words > 1) lds[lane * stride + 1] = high;
+    depths[lane] = depth;
+  }
+  return Tree{lds, depths, words, stride};
+}
+
 // All threads of the workgroup call this, rows <= 256; lds: tree_lds_bytes().
 // A window of `window` positions hides the ancestors that lie further back, but for those among the first `sinks` positions.
 __device__ inline Tree tree_of(const int32_t* parents, int rows, int window, int sinks, int t, uint32_t* lds) {
+  if (rows <= 64) return small_tree_of(parents, rows, window, sinks, t, lds);
   const int words = tree_words(rows), stride = tree_stride(rows);
   int32_t* const up = reinterpret_cast<int32_t*>(lds + rows * stride);
   int32_t* const depths = up + rows;

@@ -39,24 +39,37 @@ int32_t span_groups_bound(int32_t t, int32_t rows, int32_t tile_rows, int32_t wi
 }
 
 constexpr int64_t kSpanWorkgroups = 512;
+constexpr int64_t kSpanPartials = 65536;  // partials (of a (row, head) and split) of a call at most, if its rows are fewer
 
-SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, int32_t window, int32_t sinks, bool tree) {
+// Up to 32 columns a split is planned as a step's or block's of as many keys (make_plan()): the kernel streams keys as theirs do.
+SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, int32_t window, int32_t sinks, bool tree) {
   SpanPlan s;
   const int32_t G = Hq / kv->num_kv_heads;
-  const int64_t columns = (int64_t)rows * G;
+  const int64_t columns = (int64_t)rows * G, all = (int64_t)batch * rows * Hq;
   s.tile_columns = columns <= 16 ? 16 : columns <= 32 ? 32 : 128;
   s.tiles = (int32_t)((columns + s.tile_columns - 1) / s.tile_columns);
   int32_t tile_rows = (s.tile_columns + G - 2) / G + 1;
   tile_rows = tree || tile_rows > rows ? rows : tile_rows;
   const int32_t groups = span_groups_bound(t, rows, tile_rows, window, sinks);
-  const int64_t units = (int64_t)batch * kv->num_kv_heads * s.tiles;
-  int64_t splits = kSpanWorkgroups / units, most = (groups + 7) / 8;
-  splits = splits < most ? splits : most;
-  splits = splits < 1 ? 1 : splits;
-  s.split_groups = (int32_t)((groups + splits - 1) / splits);
+  const int64_t most = all < kSpanPartials ? kSpanPartials / all : 1;  // splits that the workspace has room for
+  if (s.tile_columns <= 32) {
+    const int64_t keys = 32 * (int64_t)groups;  // a multiple of the unit of splits, so that windows have no worst alignment
+    tempo_plan plan;
+    make_plan(kv, batch, Hq, (int32_t)(keys - 1 < INT32_MAX - 64 ? keys - 1 : INT32_MAX - 64), 0, ragged && window == 0, rows, most < kMaxSplits ? most : kMaxSplits, &plan);
+    s.split_groups = plan.tokens_per_split / 32;
+    s.waves = plan.waves;
+  } else {
+    const int64_t units = (int64_t)batch * kv->num_kv_heads * s.tiles, even = (groups + 7) / 8;
+    int64_t splits = kSpanWorkgroups / units;
+    splits = splits < even ? splits : even;
+    splits = splits < most ? splits : most;
+    splits = splits < 1 ? 1 : splits;
+    s.split_groups = (int32_t)((groups + splits - 1) / splits);
+    s.waves = 4;
+  }
+  while ((groups + s.split_groups - 1) / s.split_groups > most) s.split_groups *= 2;
   s.splits = (groups + s.split_groups - 1) / s.split_groups;
-  s.waves = s.split_groups >= 16 ? 8 : s.split_groups >= 4 ? 4 : s.split_groups >= 2 ? 2 : 1;
-  while (s.waves > 1 && units_lds_bytes(s.waves, (int)(columns < 16 ? columns : 16), kv->head_dim) > kMaxUnitsLds) s.waves /= 2;
+  while (s.tile_columns <= 32 && s.waves > 1 && units_lds_bytes(s.waves, (int)(columns < 16 ? columns : 16), kv->head_dim) > kMaxUnitsLds) s.waves /= 2;
   return s;
 }
 
@@ -64,25 +77,26 @@ size_t span_bytes(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, c
   return s.splits == 1 ? 256 : plan_bytes(kv, (int64_t)batch * rows * Hq, s.splits);
 }
 
-// Rows of the partials of any call with at most `rows` rows a sequence whose last step is at most max_t.
-size_t span_bytes_bound(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t max_t) {
-  // splits only where there are fewer than kSpanWorkgroups tiles of up to 128 columns: rows * splits is at most 128 times as many
-  const int64_t all = (int64_t)batch * rows * Hq, groups = max_t / 32 + 1, most = 128 * kSpanWorkgroups;
-  const int64_t partials = all > most / groups ? most : all * groups;
+// Of any call with at most `rows` rows a sequence whose tiles of columns see at most `groups` groups.
+size_t span_bytes_bound(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t groups) {
+  const int64_t all = (int64_t)batch * rows * Hq;
+  const int64_t partials = all > kSpanPartials / groups ? kSpanPartials : all * groups;
   return plan_bytes(kv, partials, 1);
 }
 
 // Everything but the arguments that only one of the entry points has has been checked.
 int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* parents, const int32_t* rows_per_seq, int32_t batch, int32_t Hq,
                  int32_t rows, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale, void* workspace,
-                 hipStream_t stream, const tempo_rope* rope = nullptr) {
-  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, window, sinks, parents != nullptr);
+                 hipStream_t stream, const tempo_rope* rope = nullptr, const void* k_new = nullptr, const void* v_new = nullptr) {
+  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, t_per_seq != nullptr, window, sinks, parents != nullptr);
   tempo_plan plan = {32, s.splits, s.waves};
   SpanParams p;
   static_cast<AttnParams&>(p) = attn_params(kv, q, out, Hq, t, t_per_seq, window, scale, &plan, workspace, batch, rows);
   p.direct = s.splits == 1;
   p.count_per_seq = rows_per_seq;
   p.parents = parents;
+  p.k_new = k_new;
+  p.v_new = v_new;
   p.sinks = sinks;
   p.tile_columns = s.tile_columns;
   p.split_groups = s.split_groups;
@@ -97,9 +111,9 @@ int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* pa
   return launch_status(launch_combine_spans(p, batch, kv->head_dim, stream), "attn_spans_combine");
 }
 
-int check_span_workspace(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, int32_t window, int32_t sinks, bool tree,
-                         const void* workspace, size_t workspace_bytes) {
-  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, window, sinks, tree);
+int check_span_workspace(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, int32_t window, int32_t sinks,
+                         bool tree, const void* workspace, size_t workspace_bytes) {
+  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, ragged, window, sinks, tree);
   // workgroups: along the grid's first axis, and all of them (numbered in 32 bits)
   const int64_t first = (int64_t)kv->num_kv_heads * s.tiles;
   if (first * 512 > INT32_MAX || first * batch * s.splits > INT32_MAX || s.splits > 65535) return TEMPO_ERR_SHAPE;
@@ -151,24 +165,21 @@ size_t tempo_attn_sinks_workspace_bytes(const tempo_kv* kv, int32_t batch, int32
                                         int32_t window, int32_t sinks) {
   if (check_span_store(kv, batch, num_q_heads, queries) != TEMPO_OK) return 0;
   if (window < 1 || sinks < 0 || max_t < 0 || max_t > INT32_MAX - 128 - queries) return 0;
-  const int32_t tile_rows = queries;  // (no tile sees more)
-  const int32_t groups = span_groups_bound(max_t, queries, tile_rows, window, sinks);
-  return span_bytes_bound(kv, batch, num_q_heads, queries, (groups - 1) * 32);
+  return span_bytes_bound(kv, batch, num_q_heads, queries, span_groups_bound(max_t, queries, queries, window, sinks));
 }
 
 size_t tempo_attn_tree_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t nodes, int32_t max_t,
                                        int32_t window, int32_t sinks) {
   if (check_span_store(kv, batch, num_q_heads, nodes) != TEMPO_OK || nodes > kMaxNodes) return 0;
   if (window < 0 || sinks < 0 || max_t < 0 || max_t > INT32_MAX - 128 - nodes) return 0;
-  const int32_t groups = span_groups_bound(max_t, nodes, nodes, window, sinks);
-  return span_bytes_bound(kv, batch, num_q_heads, nodes, (groups - 1) * 32);
+  return span_bytes_bound(kv, batch, num_q_heads, nodes, span_groups_bound(max_t, nodes, nodes, window, sinks));
 }
 
 size_t tempo_prefill_sinks_workspace_bytes(const tempo_kv* kv, int32_t batch, int32_t num_q_heads, int32_t max_t) {
   if (check_span_store(kv, batch, num_q_heads, 1) != TEMPO_OK) return 0;
   if (max_t < 0 || max_t > INT32_MAX - 128) return 0;
   const int32_t rows = max_t < (1 << 24) ? max_t + 1 : 1 << 24;
-  return span_bytes_bound(kv, batch, num_q_heads, rows, max_t);
+  return span_bytes_bound(kv, batch, num_q_heads, rows, max_t / 32 + 1);
 }
 
 int tempo_attn_tree(const tempo_kv* kv, const void* q, void* out, const int32_t* parents, const int32_t* nodes_per_seq, int32_t batch,
@@ -180,7 +191,7 @@ int tempo_attn_tree(const tempo_kv* kv, const void* q, void* out, const int32_t*
   if (nodes > kMaxNodes) return TEMPO_ERR_SHAPE;
   if ((rc = check_span(kv, t, nodes, window, sinks)) != TEMPO_OK) return rc;
   if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
-  if ((rc = check_span_workspace(kv, batch, num_q_heads, nodes, t, window, sinks, true, workspace, workspace_bytes)) != TEMPO_OK) return rc;
+  if ((rc = check_span_workspace(kv, batch, num_q_heads, nodes, t, t_per_seq != nullptr, window, sinks, true, workspace, workspace_bytes)) != TEMPO_OK) return rc;
   return attend_spans(kv, q, out, parents, nodes_per_seq, batch, num_q_heads, nodes, t, t_per_seq, window, sinks, scale, workspace,
                       static_cast<hipStream_t>(stream));
 }
@@ -197,9 +208,10 @@ static int sinks_call(const tempo_kv* kv, const tempo_rope* rope, const void* q,
   if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
   if (rope && (rc = check_rope(rope, kv->head_dim, t + rows - 1)) != TEMPO_OK) return rc;
   if (write && (int64_t)batch * rows * kv->num_kv_heads * kv->head_dim > INT32_MAX) return TEMPO_ERR_SHAPE;
-  if ((rc = check_span_workspace(kv, batch, Hq, rows, t, window, sinks, false, workspace, workspace_bytes)) != TEMPO_OK) return rc;
+  if ((rc = check_span_workspace(kv, batch, Hq, rows, t, t_per_seq != nullptr, window, sinks, false, workspace, workspace_bytes)) != TEMPO_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (write) {
+  const bool fused = write && rows == 1 && Hq / kv->num_kv_heads <= 32;  // the attention of a step writes its row itself
+  if (write && !fused) {
     StoreParams p = store_params(kv, batch, t, t_per_seq, rows);
     p.count_per_seq = count_per_seq;
     if (rope) {
@@ -208,7 +220,8 @@ static int sinks_call(const tempo_kv* kv, const tempo_rope* rope, const void* q,
     }
     if ((rc = launch_status(launch_append(p, k_new, v_new, kv->head_dim, kv->dtype, s), "kv_append")) != TEMPO_OK) return rc;
   }
-  return attend_spans(kv, q, out, nullptr, count_per_seq, batch, Hq, rows, t, t_per_seq, window, sinks, scale, workspace, s, rope);
+  return attend_spans(kv, q, out, nullptr, count_per_seq, batch, Hq, rows, t, t_per_seq, window, sinks, scale, workspace, s, rope,
+                      fused ? k_new : nullptr, fused ? v_new : nullptr);
 }
 
 int tempo_attn_sinks(const tempo_kv* kv, const void* q, void* out, int32_t batch, int32_t num_q_heads, int32_t queries, int32_t t,
