@@ -9,6 +9,7 @@
 #include "attn_bf16_columns32.h"
 #include "attn_spans.h"
 #include "attn_tree.h"
+#include "attn_units.h"
 #include "store_e4m3.h"
 
 namespace tempo {
@@ -17,6 +18,7 @@ namespace {
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kWaveColumns = 32;
+constexpr unsigned kRunBlocks = 8;
 
 template <bool kTree>
 __device__ __forceinline__ void mask_span_tile(int key, int lo, int hi, int sinks, uint32_t bits, int lane, f32x16& x) {
@@ -42,23 +44,27 @@ __device__ __forceinline__ void keep_values(int key, int lo, int last, int sinks
   }
 }
 
-// Eight codes as bf16, under one scale, or under one each.
+// Eight codes as bf16, under one scale.
 __device__ __forceinline__ u32x4 bf16_of(uint32_t a, uint32_t b, float scale) {
   const bf16x2 r[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true),
                        __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true)};
   return __builtin_bit_cast(u32x4, r);
 }
-__device__ __forceinline__ u32x4 bf16_of_each(uint32_t a, uint32_t b, const float* scale) {
-  typedef float f32x2 __attribute__((ext_vector_type(2)));
-  const f32x2 v[4] = {__builtin_amdgcn_cvt_pk_f32_fp8(a, false), __builtin_amdgcn_cvt_pk_f32_fp8(a, true),
-                      __builtin_amdgcn_cvt_pk_f32_fp8(b, false), __builtin_amdgcn_cvt_pk_f32_fp8(b, true)};
-  u32x4 w;
+// Codes of 8 slots for each of two dims, under a scale for each slot: a pair of one slot's is turned by one instruction.
+__device__ __forceinline__ void bf16_of_slots(u32x4 codes, uint2 scales, u32x4& a, u32x4& z) {
+  uint32_t shift = 23;  // (unknown to the compiler, so that a byte is taken and shifted by one instruction)
+  asm("" : "+v"(shift));
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {  // (exact: a code has 4 bits)
-    const bf16x2 pair = {(__bf16)(v[i][0] * scale[2 * i]), (__bf16)(v[i][1] * scale[2 * i + 1])};
-    w[i] = __builtin_bit_cast(uint32_t, pair);
+  for (int i = 0; i < 4; ++i) {               // slots 2i, 2i + 1
+    const uint32_t both = __builtin_amdgcn_perm(i < 2 ? codes.z : codes.w, i < 2 ? codes.x : codes.y, i & 1 ? 0x07030602u : 0x05010400u);
+    const uint32_t four = i < 2 ? scales.x : scales.y;
+    const float s = __builtin_bit_cast(float, ((four >> (16 * (i & 1))) & 0xFFu) << shift);
+    const float t = __builtin_bit_cast(float, ((four >> (16 * (i & 1) + 8)) & 0xFFu) << shift);
+    const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(both, s, false));
+    const uint32_t v = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(both, t, true));
+    a[i] = __builtin_amdgcn_perm(v, u, 0x05040100u);
+    z[i] = __builtin_amdgcn_perm(v, u, 0x07060302u);
   }
-  return w;
 }
 
 template <int D, int NW, bool k8, bool kTree, bool kRope>
@@ -68,23 +74,33 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   constexpr int KU = D / 16;                  // 1 KiB units of one group's keys
   constexpr int UNITS = 2 * KU;               // ... and of its keys and values together
   constexpr int PER_WAVE = UNITS / NW;        // units each wavefront copies per group
-  constexpr int NBUF = 4, kBuf = UNITS * 64;
+  constexpr int NBUF = k8 ? 3 : 4, kBuf = UNITS * 64;
+  constexpr int kRaw = KU * 64 + 4 * NW, kRaws = 3;  // 8 bits: a group's codes as they lie in the pools, and the scale bytes for each wavefront
   constexpr int CODES = KU / NW;              // 1 KiB units of codes, of keys or values, that each wavefront turns into bf16
   static_assert(KU % NW == 0, "copy split");
-  extern __shared__ u32x4 lds[];              // [NBUF][UNITS][64] x 16 bytes: a group's keys, then its values; then the tree
+  extern __shared__ u32x4 lds[];              // [NBUF][UNITS][64] x 16 bytes: a group's keys, then its values; 8 bits: [kRaws][kRaw];
+                                              // then the tree
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // Workgroups go to the 8 dies round-robin by linear index; each die gets a contiguous run of the list, in which the blocks of
-  // one (sequence, kv head, split), which read the same keys, are neighbours.
-  const unsigned nx = gridDim.x, ny = gridDim.y, total = nx * ny * gridDim.z;
-  const unsigned linear = blockIdx.x + nx * (blockIdx.y + ny * blockIdx.z);
-  const unsigned die = linear & 7u, share = total >> 3, extra = total & 7u;
-  const unsigned item = die * share + (die < extra ? die : extra) + (linear >> 3);
-  const unsigned ix = item % nx, iyz = item / nx;
-  const int hkv = (int)(iyz % ny), b = (int)(iyz / ny);
-  const unsigned nblocks = nx / (unsigned)p.num_splits;
-  const int split = (int)(ix / nblocks), block = (int)(nblocks - 1 - ix % nblocks);
+  // The blocks of columns of one (sequence, kv head, split) read the same keys, so they run on one die.  Few blocks: units of work lie
+  // on the dies in turn (units_work()).  The many of a prompt, whose neighbours read nearly the same windows: each die gets a
+  // contiguous run of the list of blocks.
+  const unsigned blocks = gridDim.x / (unsigned)p.Hkv;
+  int hkv, b, split, block;
+  if (blocks <= kRunBlocks) {
+    const UnitsWork item = units_work(blockIdx.x, blockIdx.y, blockIdx.z, gridDim.x, gridDim.y, gridDim.z, p.Hkv);
+    hkv = item.hkv, b = item.b, split = item.split, block = item.tile;
+  } else {
+    const unsigned total = gridDim.x * gridDim.y * gridDim.z, linear = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
+    const unsigned die = linear & 7u, share = total >> 3, extra = total & 7u;
+    const unsigned item = die * share + (die < extra ? die : extra) + (linear >> 3);
+    block = (int)(blocks - 1 - item % blocks);
+    const unsigned unit = item / blocks;
+    split = (int)(unit % gridDim.z);
+    hkv = (int)(unit / gridDim.z % (unsigned)p.Hkv);
+    b = (int)(unit / gridDim.z / (unsigned)p.Hkv);
+  }
 
   int t_b = p.t_per_seq ? ((const_i32_ptr)p.t_per_seq)[b] : p.t;
   t_b = t_b > p.t ? p.t : (t_b < 0 ? 0 : t_b);
@@ -108,13 +124,14 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   const int32_t* table = p.block_table + (int64_t)b * p.max_blocks_per_seq;
   const int tile_last = key_of(past - 1) >> p.z_log2;
   int tile_base = key_of(from) >> p.z_log2;
-  uint32_t tile_lo, tile_hi;                  // slot number of the tile's first slot
+  constexpr int kSlotBytes = k8 ? D : 2 * D;
+  uint32_t tile_lo, tile_hi;                  // byte offset, in either pool, of the tile's first slot
   auto fetch_entry = [&]() {
     const int tile = tile_base + lane < tile_last ? tile_base + lane : tile_last;
     return table[tile & p.tile_mask];
   };
   auto place_tiles = [&](int found) {
-    const uint64_t at = (uint64_t)((int64_t)clamp_block(found, p.num_blocks) * p.Hkv + hkv) << p.z_log2;
+    const uint64_t at = ((uint64_t)((int64_t)clamp_block(found, p.num_blocks) * p.Hkv + hkv) << p.z_log2) * kSlotBytes;
     tile_lo = (uint32_t)at;
     tile_hi = (uint32_t)(at >> 32);
     asm volatile("" : "+v"(tile_lo), "+v"(tile_hi));  // waited for here, not among the copies in flight
@@ -144,31 +161,46 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   }
 
   place_tiles(entry);
-  auto slot_of = [&](int key) {               // of a group's first slot, among the store's slots
-    const int tile = key >> p.z_log2;
+  // Groups are copied in their order: the next one, at last again and again the split's last, into buffers that nobody reads any
+  // more (every iteration then issues the same number of copies, and "all but the newest have landed" is one counted wait).
+  // Scalar instructions take the loop's issue slots as others do (94 an iteration and wavefront in its first form, KEPT now).
+  int next_group = from, next_key = key_of(from);
+  auto next_offset = [&]() {                  // byte offset of the group in either pool
+    const int tile = next_key >> p.z_log2;
     if (tile - tile_base >= 64) {
       tile_base = tile;
       place_tiles(fetch_entry());
     }
     const uint32_t lo = __builtin_amdgcn_readlane(tile_lo, tile - tile_base), hi = __builtin_amdgcn_readlane(tile_hi, tile - tile_base);
-    return (((uint64_t)hi << 32) | lo) + (uint32_t)(key & ((1 << p.z_log2) - 1));
-  };
-  // A group that holds slots no row sees, which may be unwritten: its values there become 0.
-  auto masked = [&](int key) { return key + 31 > t_last || (key < rg.lo && key + 31 >= p.sinks); };
-
-  // bf16: wavefront w copies units w, w + NW, ... straight into LDS.  Beyond the last group that one is copied again, into a
-  // buffer that nobody reads any more: every iteration then issues the same number of copies, and "all but the newest group has
-  // landed" is one counted wait.
-  const uint32_t lane_bytes = 16u * (uint32_t)lane;
-  auto issue = [&](int at, int g) {
-    const uint64_t slot = slot_of(key_of(g < past ? g : past - 1));
-#pragma unroll
-    for (int i = 0; i < PER_WAVE; ++i) {
-      const int u = wave + NW * i;            // wave-uniform
-      char* const pool = static_cast<char*>(u < KU ? p.k_pool : p.v_pool) + slot * (2 * D) + (u < KU ? u : u - KU) * 1024;
-      const auto unit = __builtin_amdgcn_make_buffer_rsrc(pool, 0, 1024, 0x00020000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(unit, (lds_ptr)(lds + at + u * 64), 16, lane_bytes, 0, 0, 0);
+    const uint64_t at = (((uint64_t)hi << 32) | lo) + (uint32_t)(next_key & ((1 << p.z_log2) - 1)) * kSlotBytes;
+    if (next_group < past - 1) {
+      ++next_group;
+      next_key = next_group == rg.sink_groups ? rg.g_lo << 5 : next_key + 32;
     }
+    return at;
+  };
+  // Groups that hold slots no row sees, which may be unwritten: values there become 0.  The last of the sinks, the window's first,
+  // the rows' last.
+  const int edge_sinks = rg.sink_groups > 0 && 32 * rg.sink_groups > p.sinks ? rg.sink_groups - 1 : -1;
+  const int edge_window = 32 * rg.g_lo < rg.lo ? rg.sink_groups : -1;
+  const int edge_rows = ((t_last + 1) & 31) != 0 ? rg.groups - 1 : -1;
+  auto masked = [&](int g) { return g == edge_sinks || g == edge_window || g == edge_rows; };
+
+  // bf16: wavefront w copies units w, w + NW, ... straight into LDS.
+  const uint32_t lane_bytes = 16u * (uint32_t)lane;
+  char* const k_units = static_cast<char*>(p.k_pool) + 1024 * wave;
+  char* const v_units = static_cast<char*>(p.v_pool) + 1024 * wave;
+  auto issue = [&](int at) {
+    const uint64_t from_byte = next_offset();
+    const auto k = __builtin_amdgcn_make_buffer_rsrc(k_units + from_byte, 0, 1024 * KU, 0x00020000);
+    const auto v = __builtin_amdgcn_make_buffer_rsrc(v_units + from_byte, 0, 1024 * KU, 0x00020000);
+    u32x4* const to = lds + at + wave * 64;
+#pragma unroll
+    for (int i = 0; i < PER_WAVE / 2; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(k, (lds_ptr)(to + NW * i * 64), 16, lane_bytes, 1024 * NW * i, 0, 0);
+#pragma unroll
+    for (int i = 0; i < PER_WAVE / 2; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(v, (lds_ptr)(to + (KU + NW * i) * 64), 16, lane_bytes, 1024 * NW * i, 0, 0);
   };
   auto mask_values = [&](int g, int at) {
     uint32_t keep[4];
@@ -179,52 +211,69 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
       if (u >= KU) mask_piece(lds + at + u * 64 + lane, keep);
     }
   };
-  // 8 bits: the wavefront's codes of a group wait in registers for an iteration, and are turned into the same image.
+  // 8 bits: codes and scale bytes are copied into LDS as they are, three groups ahead of where a wavefront turns the pieces that it
+  // copied itself into the same image: at D = 128 a unit of keys and one of values, at D = 64 one of either.
+  constexpr int kCopies = CODES + 2;          // of a wavefront, a group
+  const bool key_unit = CODES > 1 || wave < NW / 2;
+  const int code_unit = CODES > 1 ? wave : wave % (NW / 2);
+  const uint64_t scales_at = (((uint64_t)p.num_blocks * (uint64_t)p.Hkv) << p.z_log2) * D;
+  auto fetch = [&](int raw) {
+    const uint64_t from_byte = next_offset(), slot = from_byte / D;
+    char *const k = static_cast<char*>(p.k_pool), *const v = static_cast<char*>(p.v_pool);
+    const auto first = __builtin_amdgcn_make_buffer_rsrc((key_unit ? k : v) + from_byte + 1024 * code_unit, 0, 1024, 0x00020000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(first, (lds_ptr)(lds + raw + wave * 64), 16, lane_bytes, 0, 0, 0);
+    if constexpr (CODES > 1) {
+      const auto second = __builtin_amdgcn_make_buffer_rsrc(v + from_byte + 1024 * code_unit, 0, 1024, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(second, (lds_ptr)(lds + raw + (wave + NW) * 64), 16, lane_bytes, 0, 0, 0);
+    }
+    // (each wavefront its own copy of the 32 bytes of keys and of values: another may be a group ahead)
+    if (lane < 8) {
+      const auto ks = __builtin_amdgcn_make_buffer_rsrc(k + scales_at + slot, 0, 32, 0x00020000);
+      const auto vs = __builtin_amdgcn_make_buffer_rsrc(v + scales_at + slot, 0, 32, 0x00020000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ks, (lds_ptr)(lds + raw + KU * 64 + 4 * wave), 4, 4 * lane, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vs, (lds_ptr)(lds + raw + KU * 64 + 4 * wave + 2), 4, 4 * lane, 0, 0, 0);
+    }
+  };
   struct Codes {
     u32x4 unit[CODES];
     uint32_t k_scales;
     uint2 v_scales;
   };
-  auto fetch = [&](int g) {
-    const uint64_t slot = slot_of(key_of(g < past ? g : past - 1)), slots = ((uint64_t)p.num_blocks * (uint64_t)p.Hkv) << p.z_log2;
-    const char *const k = static_cast<const char*>(p.k_pool), *const v = static_cast<const char*>(p.v_pool);
+  // The oldest of three groups in flight.
+  auto take = [&](int raw) {
+    asm volatile("" ::: "memory");
+    constexpr int kLeft = 2 * kCopies;
+    __builtin_amdgcn_s_waitcnt((kLeft & 15) | 0x0F70 | ((kLeft >> 4) << 14));  // vmcnt only
+    asm volatile("" ::: "memory");
     Codes c;
 #pragma unroll
-    for (int i = 0; i < CODES; ++i) {
-      const int u = wave + NW * i;            // wave-uniform: keys, then values
-      c.unit[i] = *reinterpret_cast<const u32x4*>((u < KU / 2 ? k : v) + slot * D + (u < KU / 2 ? u : u - KU / 2) * 1024 + lane_bytes);
-    }
-    c.k_scales = *reinterpret_cast<const uint16_t*>(k + slots * D + slot + 2 * (lane & 15));
-    c.v_scales = *reinterpret_cast<const uint2*>(v + slots * D + slot + 8 * (lane >> 4));
+    for (int i = 0; i < CODES; ++i) c.unit[i] = lds[raw + (wave + NW * i) * 64 + lane];
+    const char* const scales = reinterpret_cast<const char*>(lds + raw + KU * 64 + 4 * wave);
+    c.k_scales = *reinterpret_cast<const uint16_t*>(scales + 2 * (lane & 15));
+    c.v_scales = *reinterpret_cast<const uint2*>(scales + 32 + 8 * (lane >> 4));
     return c;
   };
   auto settle = [&](const Codes& c, int g, int at) {
-    const int key = key_of(g < past ? g : past - 1);
-#pragma unroll
-    for (int i = 0; i < CODES; ++i) {
-      const int u = wave + NW * i;
-      if (u < KU / 2) {                       // keys: tile u / (D / 64), dims from 64 (u mod (D / 64))
-        const int tile = u / (D / 64), w = u % (D / 64);
-        const float scale = scale_of(tile ? c.k_scales >> 8 : c.k_scales & 0xFFu);
-        u32x4* const to = lds + at + (tile * (D / 32) + 2 * w) * 64 + lane;
-        to[0] = bf16_of(c.unit[i].x, c.unit[i].y, scale);
-        to[64] = bf16_of(c.unit[i].z, c.unit[i].w, scale);
-        continue;
-      }
-      float scale[8];                         // values: dims from 32 (u - KU / 2)
-#pragma unroll
-      for (int r = 0; r < 8; ++r) scale[r] = scale_of((r < 4 ? c.v_scales.x >> (8 * r) : c.v_scales.y >> (8 * (r - 4))) & 0xFFu);
-      u32x4 a = bf16_of_each(c.unit[i].x, c.unit[i].y, scale), z = bf16_of_each(c.unit[i].z, c.unit[i].w, scale);
-      if (masked(key)) {
+    if (key_unit) {                           // tile code_unit / (D / 64), dims from 64 (code_unit mod (D / 64))
+      const int tile = code_unit / (D / 64), w = code_unit % (D / 64);
+      const float scale = scale_of((c.k_scales >> (8 * tile)) & 0xFFu);
+      u32x4* const to = lds + at + (tile * (D / 32) + 2 * w) * 64 + lane;
+      to[0] = bf16_of(c.unit[0].x, c.unit[0].y, scale);
+      to[64] = bf16_of(c.unit[0].z, c.unit[0].w, scale);
+    }
+    if (CODES > 1 || !key_unit) {             // dims from 32 code_unit
+      u32x4 a, z;
+      bf16_of_slots(c.unit[CODES - 1], c.v_scales, a, z);
+      if (masked(g)) {
         uint32_t keep[4];
-        keep_values(key, rg.lo, t_last, p.sinks, lane, keep);
+        keep_values(key_of(g), rg.lo, t_last, p.sinks, lane, keep);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           a[e] &= keep[e];
           z[e] &= keep[e];
         }
       }
-      u32x4* const to = lds + at + 2 * u * 64 + lane;  // (KU units of keys before them)
+      u32x4* const to = lds + at + (KU + 2 * code_unit) * 64 + lane;
       to[0] = a;
       to[64] = z;
     }
@@ -251,26 +300,28 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   auto value_operand = [&](int at, int chunk, int ot) { return as_bf16x8(lds[at + v_lane + ot * 128 + chunk * 32]); };
 
   int grp = from, at0 = 0;                    // LDS offset of the buffer of group grp
-  auto next = [&](int ahead) { return (at0 + ahead * kBuf) & (NBUF * kBuf - 1); };
+  auto next = [&](int ahead) {
+    if constexpr (!k8) return (at0 + ahead * kBuf) & (NBUF * kBuf - 1);
+    const int at = at0 + ahead * kBuf;
+    return at < NBUF * kBuf ? at : at - NBUF * kBuf;
+  };
+  int raw0 = NBUF * kBuf;                     // LDS offset of the codes of group grp + 2
 
   // The first three groups.
-  Codes held;
   if constexpr (k8) {
-    const Codes a = fetch(from), b = fetch(from + 1), c = fetch(from + 2);
-    held = fetch(from + 3);
-    settle(a, from, 0);
-    settle(b, from + 1, kBuf);
-    settle(c, from + 2, 2 * kBuf);
+    fetch(raw0);
+    fetch(raw0 + kRaw);
+    fetch(raw0 + 2 * kRaw);
   } else {
 #pragma unroll
-    for (int i = 0; i < NBUF - 1; ++i) issue(i * kBuf, from + i);
+    for (int i = 0; i < NBUF - 1; ++i) issue(i * kBuf);
   }
   __builtin_amdgcn_sched_barrier(0);
   Tree tree;
   int position = t_b + row;
   if constexpr (kTree) {
     if (p.window > 0 || key_of(past - 1) + 31 >= t_b) {
-      tree = tree_of(p.parents + (int64_t)b * p.queries, rows, p.window, p.sinks, t_b, reinterpret_cast<uint32_t*>(lds + NBUF * kBuf));
+      tree = tree_of(p.parents + (int64_t)b * p.queries, rows, p.window, p.sinks, t_b, reinterpret_cast<uint32_t*>(lds + NBUF * kBuf + (k8 ? kRaws * kRaw : 0)));
       if (p.window > 0) position = t_b + tree.depth(row);
     }
   }
@@ -295,9 +346,12 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   const int own_last = idle ? past - 1 : (hi_at < past - 1 ? hi_at : past - 1);
   float base = 0.f;                           // m_run, or 0 while the column has seen no key
   float limit = -INFINITY;                    // raw dot product from which on m_run has to move
+  // (numbers of groups: those of the sinks below sink_whole, and whole_first .. whole_last; a few that are whole may not count)
+  const int behind = rg.sink_groups - rg.g_lo, sink_whole = (p.sinks >> 5) < rg.sink_groups ? p.sinks >> 5 : rg.sink_groups;
+  const int whole_first = ((lo_last + 31) >> 5) + behind, whole_last = ((whole_hi + 1) >> 5) - 1 + behind;
   auto enter = [&](int g, f32x16& x, float mx) {
-    const int key = key_of(g);
-    if (key + 31 > whole_hi || (key < lo_last && key + 31 >= p.sinks)) {
+    if (g >= sink_whole && (g < whole_first || g > whole_last)) {
+      const int key = key_of(g);
       uint32_t bits = 0;
       if constexpr (kTree) {
         if (key + 31 >= t_b) bits = tree.bits(row, key - t_b);
@@ -307,17 +361,23 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
     }
     softmax_reference<D>(mx, p.scale_log2e, limit, m_run, base, acc, l_run);
   };
+  Codes codes;
+  auto peek = [&]() {
+    if constexpr (k8) codes = take(raw0);
+  };
   auto copies = [&]() {                       // into the buffer of group grp - 1, which everybody finished before the last barrier
     if constexpr (k8) {
-      settle(held, grp + NBUF - 1, next(NBUF - 1));
-      held = fetch(grp + NBUF);
+      settle(codes, grp + 2, next(2));
+      __builtin_amdgcn_s_waitcnt(0xC07F);     // (they are in registers: the copy may go over them)
+      fetch(raw0);
+      raw0 = raw0 + kRaw < NBUF * kBuf + kRaws * kRaw ? raw0 + kRaw : NBUF * kBuf;
     } else {
-      issue(next(NBUF - 1), grp + NBUF - 1);
+      issue(next(NBUF - 1));
     }
   };
   auto mask_landed = [&](int g, int at) {
     if constexpr (!k8) {
-      if (g < past && masked(key_of(g))) mask_values(g, at);
+      if (g < past && masked(g)) mask_values(g, at);
     }
   };
   auto finish = [&]() {
@@ -327,11 +387,22 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
     at0 = next(1);
     ++grp;
   };
+  if constexpr (k8) {                         // the first two
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const Codes c = take(raw0 + i * kRaw);
+      settle(c, from + i, i * kBuf);
+      __builtin_amdgcn_s_waitcnt(0xC07F);
+      fetch(raw0 + i * kRaw);
+    }
+    raw0 += 2 * kRaw;
+  }
   landed();
   mask_landed(from, 0);
   mask_landed(from + 1, kBuf);
   meet();
   while (grp < own_first && grp < past) {
+    peek();
     copies();
     finish();
   }
@@ -367,6 +438,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
         acc[ot] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[s], as_bf16x8(pa[(s - KT) / OT]), acc[ot], 0, 0, 0);
       }
       if (s + kRead < kSlots) read_operand(s + kRead);
+      if (s == KT) peek();
       if (s == KT + OT) copies();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -393,6 +465,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
     iterate(xb, xa);
   }
   while (grp < past) {
+    peek();
     copies();
     finish();
   }
@@ -434,8 +507,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
 template <int D, int NW, bool k8>
 hipError_t launch_wide(const SpanParams& p, int batch, hipStream_t stream) {
   const int blocks = (p.queries * p.G + p.tile_columns - 1) / p.tile_columns;
-  const dim3 grid((unsigned)(blocks * p.num_splits), (unsigned)p.Hkv, (unsigned)batch), block(64 * NW);
-  const size_t lds = 4 * (size_t)(D / 8) * 1024 + (p.parents ? tree_lds_bytes(p.queries) : 0);
+  const dim3 grid((unsigned)(p.Hkv * blocks), (unsigned)batch, (unsigned)p.num_splits), block(64 * NW);
+  const size_t lds = (k8 ? 3 * ((size_t)(D / 8 + D / 16) * 1024 + 64 * NW) : 4 * (size_t)(D / 8) * 1024) + (p.parents ? tree_lds_bytes(p.queries) : 0);
   if (p.parents) return launch((attn_spans_wide<D, NW, k8, true, false>), grid, block, lds, stream, p);
   if (p.rope_cos) return launch((attn_spans_wide<D, NW, k8, false, true>), grid, block, lds, stream, p);
   return launch((attn_spans_wide<D, NW, k8, false, false>), grid, block, lds, stream, p);

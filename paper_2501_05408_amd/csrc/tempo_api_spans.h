@@ -38,8 +38,35 @@ int32_t span_groups_bound(int32_t t, int32_t rows, int32_t tile_rows, int32_t wi
   return (int32_t)(some < all ? some : all);
 }
 
-constexpr int64_t kSpanWorkgroups = 512;
 constexpr int64_t kSpanPartials = 65536;  // partials (of a (row, head) and split) of a call at most, if its rows are fewer
+
+// Groups of a split of the kernel for many columns: a time model as make_plan()'s, in nanoseconds.  A workgroup of 128 columns costs
+// kWideFixedNs before its first group and behind its last one, hidden behind others only in part; a group, with two or three
+// workgroups to a unit (what registers and LDS let in), 560 ns of the unit's time at D = 128 and 420 at 64, with one 720 and 540.
+// The combine reads and writes a partial per (row, head) and split.  Of a ragged batch's workgroups about half exist.
+constexpr double kWideFixedNs = 8000.0, kWideCombineNs = 4000.0, kWidePartialBytesPerNs = 5000.0;
+
+int32_t wide_split_groups(int64_t units, int32_t groups, int D, int64_t rows, bool ragged, int64_t most) {
+  const int64_t resident = D == 128 ? 2 : 3;
+  const double alone = D == 128 ? 720.0 : 540.0, shared = D == 128 ? 560.0 : 420.0;
+  int32_t best = groups;
+  double least = -1.0;
+  for (int64_t splits = 1; splits <= most && splits <= 64 && splits <= (groups + 3) / 4; ++splits) {
+    const int32_t each = (int32_t)((groups + splits - 1) / splits);
+    const int64_t there = (groups + each - 1) / each;  // splits of so many groups
+    const int64_t workgroups = ragged ? (units * there * 11 + 19) / 20 : units * there;
+    const int64_t whole = (workgroups + kComputeUnits - 1) / kComputeUnits, rounds = (whole + resident - 1) / resident;
+    const double at = whole <= 4 ? (double)whole : (double)workgroups / kComputeUnits;  // (many even out)
+    const double group = at * shared > (double)rounds * alone ? at * shared : (double)rounds * alone;
+    double cost = (double)rounds * kWideFixedNs + each * group;
+    if (there > 1) cost += kWideCombineNs + 2.0 * (double)(rows * there) * D * 4 / kWidePartialBytesPerNs * (ragged ? 0.55 : 1.0);
+    if (least < 0.0 || cost < least * 0.99) {
+      least = cost;
+      best = each;
+    }
+  }
+  return best;
+}
 
 // Up to 32 columns a split is planned as a step's or block's of as many keys (make_plan()): the kernel streams keys as theirs do.
 SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, int32_t window, int32_t sinks, bool tree) {
@@ -59,12 +86,7 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
     s.split_groups = plan.tokens_per_split / 32;
     s.waves = plan.waves;
   } else {
-    const int64_t units = (int64_t)batch * kv->num_kv_heads * s.tiles, even = (groups + 7) / 8;
-    int64_t splits = kSpanWorkgroups / units;
-    splits = splits < even ? splits : even;
-    splits = splits < most ? splits : most;
-    splits = splits < 1 ? 1 : splits;
-    s.split_groups = (int32_t)((groups + splits - 1) / splits);
+    s.split_groups = wide_split_groups((int64_t)batch * kv->num_kv_heads * s.tiles, groups, kv->head_dim, all, ragged && window == 0, most);
     s.waves = 4;
   }
   while ((groups + s.split_groups - 1) / s.split_groups > most) s.split_groups *= 2;
