@@ -38,7 +38,7 @@ int32_t span_groups_bound(int32_t t, int32_t rows, int32_t tile_rows, int32_t wi
   return (int32_t)(some < all ? some : all);
 }
 
-constexpr int64_t kSpanPartials = 65536;  // partials (of a (row, head) and split) of a call at most, if its rows are fewer
+constexpr int64_t kSpanPartials = 131072;  // partials (of a (row, head) and split) of a call at most, if its rows are fewer
 
 // Groups of a split of the kernel for many columns: a time model as make_plan()'s, in nanoseconds.  A workgroup of 128 columns costs
 // kWideFixedNs before its first group and behind its last one, hidden behind others only in part; a group, with two or three
@@ -68,21 +68,69 @@ int32_t wide_split_groups(int64_t units, int32_t groups, int D, int64_t rows, bo
   return best;
 }
 
+// Columns of a workgroup: 16 or 32 in the registers of each wavefront, which share the keys out (attn_spans.hip), or 128, 32 to a
+// wavefront, over keys in LDS (attn_spans_wide.hip).  Estimates in us: a launch's fixed part; a workgroup's group, of 256 at work
+// (for 128 columns by its wavefronts that have some); the combine, where fewer workgroups than units call for splits.  A key is
+// fetched from HBM once whatever the tiles.  Fitted to 9 counts of columns of 6 to 190 at 40 shapes of 1 to 48 sequences; us with
+// 16 / 32 / 128: 24/8 heads of 128, bf16, 1 sequence of 1000 keys, 63 columns 11.5 / 13.0 / 13.8; 8 of 1000, 96 columns 21 / 17 / 22;
+// 16 of 4000, 96 columns 127 / 92 / 67; 32/8 heads of 64, 8 bits, 48 of 1000, 60 columns 27 / 22 / 31; 188 columns 66 / 53 / 46.
+// Of a batch whose sequences have steps, or trees, of their own, about half of the longest are taken to be there, though a range
+// that is not split takes as long as the longest (16 trees of up to 32 nodes behind up to 4000 keys, 24/8 heads of 128, 8 bits,
+// 16 / 32 / 128: 35 / 30 / 44; bf16 61 / 44 / 36).
+double span_cost_us(const tempo_kv* kv, int64_t pairs, int64_t columns, int64_t rows_heads, int32_t tile, int32_t groups, bool ragged, bool counts) {
+  const bool k8 = kv->dtype == TEMPO_E4M3, narrow = kv->head_dim == 64;
+  const int at = (k8 ? 2 : 0) + (narrow ? 1 : 0);
+  static const double c16[] = {0.36, 0.15, 0.20, 0.105}, c32[] = {0.40, 0.17, 0.25, 0.155}, c128[] = {0.45, 0.20, 0.40, 0.20};
+  static const double wave[] = {0.08, 0.04, 0.10, 0.06}, hbm[] = {0.6, 0.3, 0.3, 0.15};
+  const double all = (double)((columns + tile - 1) / tile), tiles = counts ? 0.55 * all + 0.25 : all;
+  const double there = counts ? 0.55 * (double)columns : (double)columns, mean = ragged ? 0.55 * groups : groups;
+  const double workgroups = (double)pairs * tiles, units = kComputeUnits;
+  const bool split = workgroups < 192 && groups > 12;
+  double work = workgroups * mean / units;                 // groups one after another on a unit
+  if (!split && work < groups) work = groups;
+  double each = tile == 16 ? c16[at] : tile == 32 ? c32[at] : c128[at] + wave[at] * there / 32.0 / tiles;
+  if (tile == 32 && at == 2 && workgroups > units) each *= 1.3;
+  const double stream = hbm[at] * (double)pairs * mean / units;
+  double cost = (tile == 16 ? 5.0 : tile == 32 ? 7.0 : 9.0) + (each * work > stream ? each * work : stream);
+  if (split) {
+    const double splits = 512.0 / workgroups < groups / 8.0 ? 512.0 / workgroups : groups / 8.0;
+    cost += 5.0 + (double)rows_heads * (counts ? 0.55 : 1.0) * splits * kv->head_dim * 4 / (kWidePartialBytesPerNs * 1000.0);
+  }
+  return cost;
+}
+
 // Up to 32 columns a split is planned as a step's or block's of as many keys (make_plan()): the kernel streams keys as theirs do.
-SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, int32_t window, int32_t sinks, bool tree) {
+// (Ragged steps, which make_plan() gives short splits, only where there are fewer workgroups than units: 40 trees of up to 20 nodes
+// behind up to 2000 keys, 32/4 heads of 128, 8 bits, one split 35 us, two 50.)
+SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, bool counts, int32_t window, int32_t sinks,
+                   bool tree) {
   SpanPlan s;
   const int32_t G = Hq / kv->num_kv_heads;
   const int64_t columns = (int64_t)rows * G, all = (int64_t)batch * rows * Hq;
-  s.tile_columns = columns <= 16 ? 16 : columns <= 32 ? 32 : 128;
+  int32_t groups = 0;
+  double least = -1.0;
+  for (int32_t tile = 16; tile <= 128; tile = tile == 16 ? 32 : 4 * tile) {
+    int32_t tile_rows = (tile + G - 2) / G + 1;
+    tile_rows = tree || tile_rows > rows ? rows : tile_rows;
+    const int32_t here = span_groups_bound(t, rows, tile_rows, window, sinks);
+    const double cost = span_cost_us(kv, (int64_t)batch * kv->num_kv_heads, columns, all, tile, here, ragged && window == 0, counts);
+    if (least < 0.0 || cost < least) {
+      least = cost;
+      groups = here;
+      s.tile_columns = tile;
+    }
+    if (columns <= tile) break;  // a wider one holds no more
+  }
   s.tiles = (int32_t)((columns + s.tile_columns - 1) / s.tile_columns);
-  int32_t tile_rows = (s.tile_columns + G - 2) / G + 1;
-  tile_rows = tree || tile_rows > rows ? rows : tile_rows;
-  const int32_t groups = span_groups_bound(t, rows, tile_rows, window, sinks);
   const int64_t most = all < kSpanPartials ? kSpanPartials / all : 1;  // splits that the workspace has room for
   if (s.tile_columns <= 32) {
     const int64_t keys = 32 * (int64_t)groups;  // a multiple of the unit of splits, so that windows have no worst alignment
+    // tiles of columns are workgroups of their own, as sequences are
+    const int64_t like = (int64_t)batch * s.tiles;
+    const int32_t queries = s.tile_columns / G < 1 ? 1 : s.tile_columns / G < rows ? s.tile_columns / G : rows;
     tempo_plan plan;
-    make_plan(kv, batch, Hq, (int32_t)(keys - 1 < INT32_MAX - 64 ? keys - 1 : INT32_MAX - 64), 0, ragged && window == 0, rows, most < kMaxSplits ? most : kMaxSplits, &plan);
+    make_plan(kv, like < 65535 ? (int32_t)like : 65535, Hq, (int32_t)(keys - 1 < INT32_MAX - 64 ? keys - 1 : INT32_MAX - 64), 0,
+              ragged && window == 0 && like * kv->num_kv_heads < kComputeUnits, queries, most < kMaxSplits ? most : kMaxSplits, &plan);
     s.split_groups = plan.tokens_per_split / 32;
     s.waves = plan.waves;
   } else {
@@ -108,9 +156,8 @@ size_t span_bytes_bound(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t r
 
 // Everything but the arguments that only one of the entry points has has been checked.
 int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* parents, const int32_t* rows_per_seq, int32_t batch, int32_t Hq,
-                 int32_t rows, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale, void* workspace,
+                 int32_t rows, int32_t t, const int32_t* t_per_seq, int32_t window, int32_t sinks, float scale, const SpanPlan& s, void* workspace,
                  hipStream_t stream, const tempo_rope* rope = nullptr, const void* k_new = nullptr, const void* v_new = nullptr) {
-  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, t_per_seq != nullptr, window, sinks, parents != nullptr);
   tempo_plan plan = {32, s.splits, s.waves};
   SpanParams p;
   static_cast<AttnParams&>(p) = attn_params(kv, q, out, Hq, t, t_per_seq, window, scale, &plan, workspace, batch, rows);
@@ -133,9 +180,9 @@ int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* pa
   return launch_status(launch_combine_spans(p, batch, kv->head_dim, stream), "attn_spans_combine");
 }
 
-int check_span_workspace(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, int32_t window, int32_t sinks,
-                         bool tree, const void* workspace, size_t workspace_bytes) {
-  const SpanPlan s = span_plan(kv, batch, Hq, rows, t, ragged, window, sinks, tree);
+int check_span_workspace(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, bool counts, int32_t window,
+                         int32_t sinks, bool tree, const void* workspace, size_t workspace_bytes, SpanPlan* plan) {
+  const SpanPlan s = *plan = span_plan(kv, batch, Hq, rows, t, ragged, counts, window, sinks, tree);
   // workgroups: along the grid's first axis, and all of them (numbered in 32 bits)
   const int64_t first = (int64_t)kv->num_kv_heads * s.tiles;
   if (first * 512 > INT32_MAX || first * batch * s.splits > INT32_MAX || s.splits > 65535) return TEMPO_ERR_SHAPE;
@@ -213,8 +260,9 @@ int tempo_attn_tree(const tempo_kv* kv, const void* q, void* out, const int32_t*
   if (nodes > kMaxNodes) return TEMPO_ERR_SHAPE;
   if ((rc = check_span(kv, t, nodes, window, sinks)) != TEMPO_OK) return rc;
   if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
-  if ((rc = check_span_workspace(kv, batch, num_q_heads, nodes, t, t_per_seq != nullptr, window, sinks, true, workspace, workspace_bytes)) != TEMPO_OK) return rc;
-  return attend_spans(kv, q, out, parents, nodes_per_seq, batch, num_q_heads, nodes, t, t_per_seq, window, sinks, scale, workspace,
+  SpanPlan plan;
+  if ((rc = check_span_workspace(kv, batch, num_q_heads, nodes, t, t_per_seq != nullptr, nodes_per_seq != nullptr, window, sinks, true, workspace, workspace_bytes, &plan)) != TEMPO_OK) return rc;
+  return attend_spans(kv, q, out, parents, nodes_per_seq, batch, num_q_heads, nodes, t, t_per_seq, window, sinks, scale, plan, workspace,
                       static_cast<hipStream_t>(stream));
 }
 
@@ -230,7 +278,8 @@ static int sinks_call(const tempo_kv* kv, const tempo_rope* rope, const void* q,
   if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
   if (rope && (rc = check_rope(rope, kv->head_dim, t + rows - 1)) != TEMPO_OK) return rc;
   if (write && (int64_t)batch * rows * kv->num_kv_heads * kv->head_dim > INT32_MAX) return TEMPO_ERR_SHAPE;
-  if ((rc = check_span_workspace(kv, batch, Hq, rows, t, t_per_seq != nullptr, window, sinks, false, workspace, workspace_bytes)) != TEMPO_OK) return rc;
+  SpanPlan plan;
+  if ((rc = check_span_workspace(kv, batch, Hq, rows, t, t_per_seq != nullptr, count_per_seq != nullptr, window, sinks, false, workspace, workspace_bytes, &plan)) != TEMPO_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
   const bool fused = write && rows == 1 && Hq / kv->num_kv_heads <= 32;  // the attention of a step writes its row itself
   if (write && !fused) {
@@ -242,7 +291,7 @@ static int sinks_call(const tempo_kv* kv, const tempo_rope* rope, const void* q,
     }
     if ((rc = launch_status(launch_append(p, k_new, v_new, kv->head_dim, kv->dtype, s), "kv_append")) != TEMPO_OK) return rc;
   }
-  return attend_spans(kv, q, out, nullptr, count_per_seq, batch, Hq, rows, t, t_per_seq, window, sinks, scale, workspace, s, rope,
+  return attend_spans(kv, q, out, nullptr, count_per_seq, batch, Hq, rows, t, t_per_seq, window, sinks, scale, plan, workspace, s, rope,
                       fused ? k_new : nullptr, fused ? v_new : nullptr);
 }
 
