@@ -1,6 +1,7 @@
 // What the launches of attn_spans*.hip and kv_place.hip take, on top of tempo_internal.h.
 #pragma once
 
+#include "attn_units.h"
 #include "tempo_internal.h"
 
 namespace tempo {
@@ -41,6 +42,19 @@ __host__ __device__ inline int span_group(const SpanRange& r, int i) { return i 
 __host__ __device__ inline SpanRange tile_range(int t, int tile, int tile_columns, int G, int rows, int window, int sinks, bool tree) {
   const int first = (int)((int64_t)tile * tile_columns / G), past = (int)(((int64_t)(tile + 1) * tile_columns - 1) / G);
   return span_range(t, tree ? 0 : first, past < rows - 1 ? past : rows - 1, window, sinks);
+}
+
+// What workgroup (x, y, z) takes of a launch for many columns, whose grid is (kv heads * blocks of columns, sequences, splits).  The
+// blocks of one (sequence, kv head, split) read the same keys, so they run on one die.  Few blocks: units of work lie on the dies in
+// turn (units_work()).  The many of a prompt, whose neighbours read nearly the same windows: each die gets a contiguous run of the
+// list of blocks, a unit's last block first.
+constexpr uint32_t kRunBlocks = 8;
+__host__ __device__ inline UnitsWork wide_work(uint32_t x, uint32_t y, uint32_t z, uint32_t nx, uint32_t ny, uint32_t nz, int Hkv) {
+  const uint32_t blocks = nx / (uint32_t)Hkv;
+  if (blocks <= kRunBlocks) return units_work(x, y, z, nx, ny, nz, Hkv);
+  const uint32_t total = nx * ny * nz, linear = x + nx * (y + ny * z), die = linear & 7u, share = total >> 3, extra = total & 7u;
+  const uint32_t item = die * share + (die < extra ? die : extra) + (linear >> 3), unit = item / blocks, row = unit / nz;
+  return {(int)(row % (uint32_t)Hkv), (int)(blocks - 1 - (item - unit * blocks)), (int)(row / (uint32_t)Hkv), (int)(unit - row * nz)};
 }
 
 // Rows at positions of their own.

@@ -9,7 +9,6 @@
 #include "attn_bf16_columns32.h"
 #include "attn_spans.h"
 #include "attn_tree.h"
-#include "attn_units.h"
 #include "store_e4m3.h"
 
 namespace tempo {
@@ -18,7 +17,6 @@ namespace {
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr int kWaveColumns = 32;
-constexpr unsigned kRunBlocks = 8;
 
 template <bool kTree>
 __device__ __forceinline__ void mask_span_tile(int key, int lo, int hi, int sinks, uint32_t bits, int lane, f32x16& x) {
@@ -83,25 +81,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  // The blocks of columns of one (sequence, kv head, split) read the same keys, so they run on one die.  Few blocks: units of work lie
-  // on the dies in turn (units_work()).  The many of a prompt, whose neighbours read nearly the same windows: each die gets a
-  // contiguous run of the list of blocks.
-  const unsigned blocks = gridDim.x / (unsigned)p.Hkv;
-  int hkv, b, split, block;
-  if (blocks <= kRunBlocks) {
-    const UnitsWork item = units_work(blockIdx.x, blockIdx.y, blockIdx.z, gridDim.x, gridDim.y, gridDim.z, p.Hkv);
-    hkv = item.hkv, b = item.b, split = item.split, block = item.tile;
-  } else {
-    const unsigned total = gridDim.x * gridDim.y * gridDim.z, linear = blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z);
-    const unsigned die = linear & 7u, share = total >> 3, extra = total & 7u;
-    const unsigned item = die * share + (die < extra ? die : extra) + (linear >> 3);
-    block = (int)(blocks - 1 - item % blocks);
-    const unsigned unit = item / blocks;
-    split = (int)(unit % gridDim.z);
-    hkv = (int)(unit / gridDim.z % (unsigned)p.Hkv);
-    b = (int)(unit / gridDim.z / (unsigned)p.Hkv);
-  }
-
+  const UnitsWork item = wide_work(blockIdx.x, blockIdx.y, blockIdx.z, gridDim.x, gridDim.y, gridDim.z, p.Hkv);
+  const int hkv = item.hkv, b = item.b, split = item.split, block = item.tile;
   int t_b = p.t_per_seq ? ((const_i32_ptr)p.t_per_seq)[b] : p.t;
   t_b = t_b > p.t ? p.t : (t_b < 0 ? 0 : t_b);
   int rows = p.queries;

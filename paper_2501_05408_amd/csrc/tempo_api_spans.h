@@ -89,7 +89,7 @@ double span_cost_us(const tempo_kv* kv, int64_t pairs, int64_t columns, int64_t 
   double work = workgroups * mean / units;                 // groups one after another on a unit
   if (!split && work < groups) work = groups;
   double each = tile == 16 ? c16[at] : tile == 32 ? c32[at] : c128[at] + wave[at] * there / 32.0 / tiles;
-  if (tile == 32 && at == 2 && workgroups > units) each *= 1.3;
+  if (tile == 32 && at == 2 && workgroups > units && !ragged) each *= 1.3;
   const double stream = hbm[at] * (double)pairs * mean / units;
   double cost = (tile == 16 ? 5.0 : tile == 32 ? 7.0 : 9.0) + (each * work > stream ? each * work : stream);
   if (split) {
@@ -397,6 +397,10 @@ int tempo_kv_keep(const tempo_kv* layers, int32_t num_layers, int32_t batch, int
         a.block_size != first.block_size || a.num_kv_heads != first.num_kv_heads || a.head_dim != first.head_dim || a.dtype != first.dtype ||
         a.ring_blocks != first.ring_blocks)
       return TEMPO_ERR_SHAPE;
+    for (int32_t j = 0; j <= i; ++j) {  // (a pool twice would be moved twice, one half of the launch over the other)
+      if (layers[j].k_pool == a.v_pool || layers[j].v_pool == a.k_pool || (j < i && (layers[j].k_pool == a.k_pool || layers[j].v_pool == a.v_pool)))
+        return TEMPO_ERR_SHAPE;
+    }
   }
   if (layers->num_kv_heads > 32767) return TEMPO_ERR_SHAPE;
   const int32_t rows = count > nodes ? count : nodes;

@@ -196,9 +196,11 @@ def same(a, b):
     (3, 64, 32, 2, 31, 6, True, 2, [[0, 5, 6, 1], [2 ** 31 - 1, 1, 2, 3]]),  # an entry behind the nodes ends the list
     (2, 64, 32, 1, 5, 1, False, 1, [[0]]),
     (1, 64, 32, 1, 77, 256, False, 1, [[255 - 2 * i for i in range(128)]]),
+    (2, 128, 32, 1, 40, 256, False, 2, [[128 + i for i in range(128)]]),
+    (5, 128, 64, 4, 50, 33, True, 40, [[0, 4, 9, 32, -1]] * 4),
 ])
 def test_kept_rows(dtype, Hkv, D, Z, B, t, nodes, ragged, layers, kept):
-    steps = np.array([t, t // 2, t // 3])[:B] if ragged else np.full(B, t)
+    steps = np.array([t, t // 2, t // 3, 0])[:B] if ragged else np.full(B, t)
     upto = t + max(nodes, len(kept[0]))
     stores = [make_store(10 + i, dtype, B, Hkv, Hkv, D, Z, upto - 1) for i in range(layers)]
     for st in stores:

@@ -93,6 +93,12 @@ TREES = [  # Hq, Hkv, D, Z, B, t, nodes, kind, window, sinks, ragged, counts
     (6, 2, 64, 32, 2, 700, 21, "random", 64, 100, False, False),
     (6, 2, 64, 32, 2, 100, 21, "random", 5000, 500, True, False),
     (2, 1, 128, 64, 1, 9000, 70, "random", 0, 0, False, False),
+    (6, 2, 128, 32, 2, 0, 30, "deep", 3, 2, False, True),
+    (12, 2, 64, 32, 3, 2, 150, "deep", 4, 9, True, True),
+    (24, 8, 64, 32, 20, 300, 33, "random", 0, 0, True, True),
+    (24, 8, 128, 32, 20, 400, 43, "random", 100, 33, True, True),
+    (128, 1, 64, 32, 2, 2500, 40, "random", 2200, 31, True, False),
+    (32, 4, 128, 256, 1, 4100, 16, "chain", 0, 0, False, False),
 ]
 
 
@@ -101,7 +107,7 @@ TREES = [  # Hq, Hkv, D, Z, B, t, nodes, kind, window, sinks, ragged, counts
 def test_tree(dtype, Hq, Hkv, D, Z, B, t, nodes, kind, window, sinks, ragged, counts):
     rng = np.random.default_rng(t * 1000 + nodes + window)
     steps = pick_steps(rng, t, B, ragged)
-    n = np.array([nodes, 0, max(1, nodes // 2)])[:B] if counts else np.full(B, nodes)
+    n = np.resize([nodes, 0, max(1, nodes // 2)], B) if counts else np.full(B, nodes)
     parents = np.stack([tree_of(kind, nodes, rng) for _ in range(B)])
     q, K, V = normal(31, 1, (B, nodes, Hq, D)), normal(31, 2, (B, t + nodes, Hkv, D)), normal(31, 3, (B, t + nodes, Hkv, D))
     st = make_store(31, dtype, B, Hq, Hkv, D, Z, t + nodes - 1)
@@ -175,6 +181,9 @@ SINKS = [  # Hq, Hkv, D, Z, B, t, queries, window, sinks, ragged
     (2, 1, 64, 32, 1, 40000, 1, 20000, 70, False),
     (6, 2, 64, 32, 2, 95, 33, 32, 32, True),
     (8, 8, 128, 32, 40, 200, 1, 70, 3, True),
+    (6, 2, 128, 32, 2, 150, 300, 90, 35, True),
+    (8, 1, 64, 64, 3, 3000, 100, 600, 65, True),
+    (4, 2, 128, 32, 2, 4500, 60, 4000, 2200, False),
 ]
 
 

@@ -12,7 +12,7 @@ FAKE = 1 << 20      # checked for NULL and alignment, never read
 BIG = 1 << 40
 
 
-def kv_desc(dtype=T.TEMPO_BF16, D=128, Z=64, Hkv=2, num_blocks=3, max_blocks=4, pools=(FAKE, FAKE, FAKE), ring=0):
+def kv_desc(dtype=T.TEMPO_BF16, D=128, Z=64, Hkv=2, num_blocks=3, max_blocks=4, pools=(FAKE, 4 * FAKE, FAKE), ring=0):
     return T.make_kv(*pools, num_blocks, max_blocks, Z, Hkv, D, dtype, ring)
 
 
@@ -187,7 +187,7 @@ def test_positions_and_kept_rows_are_refused():
     assert lib.tempo_tree_positions(FAKE, FAKE, 1, 5, 2 ** 31 - 3, None, None) == reach
 
     def keep(layers=None, n=None, batch=2, t=100, nodes=20, kept=FAKE, count=5):
-        layers = [kv_desc(), kv_desc()] if layers is None else layers
+        layers = [kv_desc(), kv_desc(pools=(2 * FAKE, 3 * FAKE, FAKE))] if layers is None else layers
         kvs = T.make_kv_layers(layers) if layers else None
         return lib.tempo_kv_keep(kvs, len(layers) if n is None else n, batch, t, None, nodes, kept, count, None)
     assert keep([], 1) == null and keep(kept=None) == null and keep([kv_desc(), kv_desc(pools=(FAKE, None, FAKE))]) == null
