@@ -68,6 +68,13 @@ int32_t wide_split_groups(int64_t units, int32_t groups, int D, int64_t rows, bo
   return best;
 }
 
+// Groups up to which a workgroup of up to 32 columns takes all of them, eight wavefronts: a combine costs about 3 us (us, one split of
+// eight wavefronts / the best of 2 to 8 splits: bf16, 24/8 heads of 128, one sequence, 10 groups 6.8 / 10.2, 19 groups 7.7 / 10.4, 34 groups
+// 11.4 / 9.7; 32/8 heads of 64, 34 groups 8.0 / 9.2, 65 groups 13.0 / 9.7; 8 bits, heads of 128, 32 groups 9.4 / 9.7).
+int32_t whole_groups(const tempo_kv* kv) {
+  return kv->dtype == TEMPO_E4M3 ? (kv->head_dim == 64 ? 48 : 32) : (kv->head_dim == 64 ? 40 : 24);
+}
+
 // Columns of a workgroup: 16 or 32 in the registers of each wavefront, which share the keys out (attn_spans.hip), or 128, 32 to a
 // wavefront, over keys in LDS (attn_spans_wide.hip).  Estimates in us: a launch's fixed part; a workgroup's group, of 256 at work
 // (for 128 columns by its wavefronts that have some); the combine, where fewer workgroups than units call for splits.  A key is
@@ -85,11 +92,11 @@ double span_cost_us(const tempo_kv* kv, int64_t pairs, int64_t columns, int64_t 
   const double all = (double)((columns + tile - 1) / tile), tiles = counts ? 0.55 * all + 0.25 : all;
   const double there = counts ? 0.55 * (double)columns : (double)columns, mean = ragged ? 0.55 * groups : groups;
   const double workgroups = (double)pairs * tiles, units = kComputeUnits;
-  const bool split = workgroups < 192 && groups > 12;
+  const bool split = workgroups < 192 && groups > (tile == 128 ? 12 : whole_groups(kv));
   double work = workgroups * mean / units;                 // groups one after another on a unit
   if (!split && work < groups) work = groups;
   double each = tile == 16 ? c16[at] : tile == 32 ? c32[at] : c128[at] + wave[at] * there / 32.0 / tiles;
-  if (tile == 32 && at == 2 && workgroups > units && !ragged) each *= 1.3;
+  if (tile == 32 && at == 2 && workgroups > units && !ragged) each *= 1.2;
   const double stream = hbm[at] * (double)pairs * mean / units;
   double cost = (tile == 16 ? 5.0 : tile == 32 ? 7.0 : 9.0) + (each * work > stream ? each * work : stream);
   if (split) {
@@ -133,6 +140,10 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
               ragged && window == 0 && like * kv->num_kv_heads < kComputeUnits, queries, most < kMaxSplits ? most : kMaxSplits, &plan);
     s.split_groups = plan.tokens_per_split / 32;
     s.waves = plan.waves;
+    if (groups <= whole_groups(kv) && like * kv->num_kv_heads <= kComputeUnits) {
+      s.split_groups = groups;
+      s.waves = groups > 4 ? 8 : groups > 2 ? 4 : groups;
+    }
   } else {
     s.split_groups = wide_split_groups((int64_t)batch * kv->num_kv_heads * s.tiles, groups, kv->head_dim, all, ragged && window == 0, most);
     s.waves = 4;

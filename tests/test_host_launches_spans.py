@@ -197,10 +197,10 @@ def test_calls_far_out_do_not_overflow(lib):
 
 def test_a_workspace_too_small_launches_nothing(lib):
     kv = store(8, 128, 64, 1000, T.TEMPO_BF16)
-    nbytes = lib.tempo_attn_tree_workspace_bytes(ctypes.byref(kv), 1, 24, 8, 300, 0, 0)
+    nbytes = lib.tempo_attn_tree_workspace_bytes(ctypes.byref(kv), 1, 24, 8, 9000, 0, 0)
     lib.host_launches_take()
-    for given in (0, 255, 256, nbytes // 8):
-        assert lib.tempo_attn_tree(ctypes.byref(kv), AT, AT, AT, None, 1, 24, 8, 300, None, 0, 0, 0.1, AT, given, None) == T.TEMPO_ERR_WORKSPACE
+    for given in (0, 255, 256, nbytes // 200):
+        assert lib.tempo_attn_tree(ctypes.byref(kv), AT, AT, AT, None, 1, 24, 8, 9000, None, 0, 0, 0.1, AT, given, None) == T.TEMPO_ERR_WORKSPACE
         assert lib.tempo_decode_step_sinks(ctypes.byref(kv), AT, AT, AT, AT, 1, 24, 3000, None, 2000, 4, 0.1, AT, given, None) == T.TEMPO_ERR_WORKSPACE
         assert lib.tempo_prefill_sinks(ctypes.byref(kv), AT, AT, AT, AT, 1, 24, 3000, 20, None, 2000, 4, 0.1, AT, given, None) == T.TEMPO_ERR_WORKSPACE
     assert taken(lib) == []
