@@ -689,7 +689,8 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  * (a softmax needs somewhere to put weight that no key in the window asks for; without the first keys long answers fall apart
  * once they leave the window).  Step p sees
  *     keys j < sinks, and keys max(0, p-window+1) .. p               (window >= 1, sinks >= 0; keys are counted once)
- * with positions as they were written.  bf16 and e4m3 stores (TEMPO_ERR_DTYPE otherwise), linear ones (TEMPO_ERR_SHAPE on rings).
+ * with positions as they were written.  Linear stores (TEMPO_ERR_SHAPE on rings); q, out and rows are of the store's dtype, bf16 for
+ * an 8-bit one.  A value inside the union of the ranges that is not finite may show in steps of the call that do not see it, in fp32 too.
  *
  * Constant memory: the table of a linear store may name a block more than once.  Blocks 0 .. sink_blocks-1 of a sequence are kept and
  * window_blocks further ones (tempo_sink_blocks) take the tiles behind them in turn,
@@ -706,6 +707,8 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  * tempo_prefill_sinks, tempo_rope_prefill_sinks  steps t .. t+count-1: rows written, all steps answered, count_per_seq as for
  *                           tempo_prefill_* (rows behind a sequence's count are neither written nor answered: the store and `out` stay
  *                           as they are there).  Answers are those of single steps.  `out` must not alias k_new or v_new.
+ *                           Rows of an fp32 store are not turned here (tempo_rope_prefill_sinks: TEMPO_ERR_DTYPE, but for one step
+ *                           without counts).
  * Workspaces: device, 256-byte aligned (TEMPO_ERR_WORKSPACE).  The size for max_t serves every step up to it; a loop over steps of an
  * endless conversation asks for it once, with the largest step: it does not grow beyond the window.  0 on bad arguments.
  * queries * num_q_heads <= 2^30, rows written batch * count * Hkv * D < 2^31 (TEMPO_ERR_SHAPE).
@@ -753,12 +756,13 @@ int tempo_rope_prefill_sinks(const tempo_kv* kv, const tempo_rope* rope, const v
  * tempo_attn_tree       q, out device, [batch][nodes][Hq][D].  Node i sees steps 0 .. t-1, its ancestors and itself.  t = 0: no
  *                       step is cached.  With window >= 1 of these only those at a position above t + depth - window or below
  *                       `sinks` (window = 0: all, and sinks must be 0).  Stores, workspace and limits as for tempo_attn_sinks.
- *                       A bf16 or e4m3 value of a node that is not finite may show in nodes that do not see it, as in blocks of steps.
+ *                       A value of a node that is not finite may show in nodes that do not see it.
  * tempo_kv_keep         the row at step t + i becomes what step t + kept[b][i] held before the call, keys and values, for
  *                       i = 0, 1, .. up to the first entry of kept (device, int32 [batch][count]) outside 0 .. nodes-1; other
  *                       rows stay as they are.  With the accepted path's node numbers, root first, the sequence goes on at step
  *                       t + their number (positions are right: the path's node i has depth i).  layers: host, [num_layers], stores
- *                       that differ in their pools alone (TEMPO_ERR_SHAPE otherwise); all of them are one launch (64 at a time).
+ *                       that differ in their pools alone, no pool among them twice (TEMPO_ERR_SHAPE otherwise); all of them are one
+ *                       launch (64 at a time).
  *                       Any store; count <= 128 (TEMPO_ERR_SHAPE).  Rows of t .. t + max(nodes, count) - 1 must fit.
  */
 int tempo_tree_positions(const int32_t* parents, int32_t* positions, int32_t batch, int32_t nodes, int32_t t, const int32_t* t_per_seq,

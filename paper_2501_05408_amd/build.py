@@ -23,7 +23,7 @@ SOURCES = ["tempo_api.hip", "kv_store.hip", "attn_partial_bf16.hip", "attn_parti
            "attn_combine.hip", "stream_read.hip", "rope.hip", "attn_prefill_bf16.hip", "attn_block_bf16.hip",
            "attn_stream_bf16.hip",
            "worklist.hip", "discounted_sum.hip", "kv_store_e4m3.hip", "attn_units.hip", "select_blocks.hip",
-           "attn_spans.hip", "attn_spans_wide.hip", "kv_place.hip"]
+           "attn_spans.hip", "attn_spans_wide.hip", "attn_spans_f32.hip", "kv_place.hip"]
 HEADERS = [os.path.join(CSRC, "tempo_internal.h"), os.path.join(CSRC, "attn_bf16_common.h"),
            os.path.join(CSRC, "attn_bf16_columns32.h"), os.path.join(CSRC, "attn_combine.h"),
            os.path.join(CSRC, "store_e4m3.h"), os.path.join(CSRC, "attn_units.h"), os.path.join(CSRC, "attn_image.h"),
@@ -76,6 +76,9 @@ MIN_OCCUPANCY = [
     ("attn_stream_bf16ILi128E", 2),            # stream kernel, D = 128: one workgroup of 8 wavefronts per compute unit
     ("attn_unitsILi128ELb1ELb0ELb0ELi1E", 3),  # 8-bit decode kernel, D = 128: its plans expect three wavefronts to a SIMD
     ("attn_prefill_bf16ILi128E", 2),           # prompt kernel, D = 128: two wavefronts of 32 columns per SIMD
+    ("attn_spansILi128E", 2),                  # sinks and trees, D = 128: two workgroups of four wavefronts to a unit, or one of eight
+    ("attn_spans_wideILi128E", 2),             # the same, 128 columns: two workgroups to a unit, as its splits are planned
+    ("attn_spans_wideILi64E", 3),              # D = 64: three
 ]
 
 

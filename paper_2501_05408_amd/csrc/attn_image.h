@@ -272,7 +272,7 @@ __device__ __forceinline__ void patch_values_bf16(int t_b, int lane, const uint1
 }
 
 // Merge of the workgroup's wavefronts, as in attn_partial_bf16.hip; column j is column first_col + j of the call.
-template <int D, int NW, bool kSelect>
+template <int D, int NW, bool kSelect, bool kBf16 = true>
 __device__ __forceinline__ void merge_units(const AttnParams& p, const float* smem, int first_col, int ncols, int b, int hkv, int split) {
   const float* sm_m = smem;
   const float* sm_l = smem + NW * 16;
@@ -304,7 +304,10 @@ __device__ __forceinline__ void merge_units(const AttnParams& p, const float* sm
       den += seen ? wgt * lw[w] : 0.f;
     }
     const int jc = (first_col + j) / p.G, jg = first_col + j - jc * p.G;
-    if (p.direct) {
+    if (p.direct && !kBf16) {
+      const int64_t orow = ((int64_t)b * p.io_steps + jc) * p.Hq + (int64_t)hkv * p.G + jg;
+      *reinterpret_cast<f32x4*>(static_cast<float*>(p.out) + orow * D + d) = f32x4{num[0] / den, num[1] / den, num[2] / den, num[3] / den};
+    } else if (p.direct) {
       const int64_t orow = ((int64_t)b * p.io_steps + jc) * p.Hq + (int64_t)hkv * p.G + jg;
       typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
       bf16x4 o;

@@ -92,7 +92,8 @@ struct KeepParams {
 #define TEMPO_LAUNCHER __attribute__((weak)) hipError_t
 TEMPO_LAUNCHER launch_spans(const SpanParams& p, int batch, int D, int dtype, int waves, hipStream_t stream);
 TEMPO_LAUNCHER launch_spans_wide(const SpanParams& p, int batch, int D, int dtype, hipStream_t stream);
-TEMPO_LAUNCHER launch_combine_spans(const SpanParams& p, int batch, int D, hipStream_t stream);
+TEMPO_LAUNCHER launch_spans_f32(const SpanParams& p, int batch, int D, int waves, hipStream_t stream);
+TEMPO_LAUNCHER launch_combine_spans(const SpanParams& p, int batch, int D, int dtype, hipStream_t stream);
 TEMPO_LAUNCHER launch_place(const PlaceParams& p, const void* k_raw, const void* v_new, int D, int dtype, hipStream_t stream);
 TEMPO_LAUNCHER launch_tree_positions(const int32_t* parents, int32_t* positions, int batch, int nodes, int t, const int32_t* t_per_seq, hipStream_t stream);
 TEMPO_LAUNCHER launch_keep(const KeepParams& p, int batch, int layers, int D, int dtype, hipStream_t stream);

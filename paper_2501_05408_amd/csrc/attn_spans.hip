@@ -16,19 +16,6 @@
 namespace tempo {
 namespace {
 
-// Logits that this lane's column does not see become -inf.  bits: of the group's slots, those of the row's ancestors.
-template <bool kTree>
-__device__ __forceinline__ void mask_span(int key, int lo, int hi, int sinks, uint32_t bits, int lane, float* x) {
-  const int c = lane >> 4;
-#pragma unroll
-  for (int r = 0; r < 8; ++r) {
-    const int at = 4 * c + (r & 3) + 16 * (r >> 2), j = key + at;
-    bool seen = j <= hi && (j >= lo || j < sinks);
-    if (kTree) seen = seen || ((bits >> at) & 1u) != 0;
-    x[r] = seen ? x[r] : -INFINITY;
-  }
-}
-
 // Slots of the group that some row may see, as masks of the lane's value bytes or halves.
 template <bool k8>
 __device__ __forceinline__ void keep_span(int key, int lo, int last, int sinks, int lane, uint32_t* keep) {
@@ -275,19 +262,19 @@ __device__ inline int splits_of(const SpanParams& p, int b, int at) {
 }
 
 // One workgroup to a (row, head): any number of splits.
-template <int D>
+template <int D, bool kBf16>
 __global__ __launch_bounds__(256) void combine_spans(SpanParams p) {
   extern __shared__ float smem[];
   const int b = blockIdx.y, at = blockIdx.x;
   const int n = splits_of(p, b, at);
   if (n == 0) return;  // uniform over the workgroup
   const int64_t row = (int64_t)b * gridDim.x + at, orow = (int64_t)b * p.io_steps * p.Hq + at;
-  combine_heads<D, true, true>(p.ws_ml + row * p.num_splits * 2, p.ws_acc + row * p.num_splits * D, p.num_splits, n, 1,
-                               static_cast<uint16_t*>(p.out) + orow * D, smem);
+  combine_heads<D, kBf16, true>(p.ws_ml + row * p.num_splits * 2, p.ws_acc + row * p.num_splits * D, p.num_splits, n, 1,
+                                static_cast<char*>(p.out) + orow * D * (kBf16 ? 2 : 4), smem);
 }
 
 // At most 8 splits: a thread to four dims of a (row, head), all of whose partials it asks for at once.
-template <int D>
+template <int D, bool kBf16>
 __global__ __launch_bounds__(256) void combine_spans_few(SpanParams p, int64_t total) {
   constexpr int C4 = D / 4, U = 8;
   const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x, row = idx / C4;
@@ -322,9 +309,13 @@ __global__ __launch_bounds__(256) void combine_spans_few(SpanParams p, int64_t t
     A.z = fmaf(w, a[u].z, A.z); A.w = fmaf(w, a[u].w, A.w);
   }
   const float inv = 1.0f / L;  // every row sees itself
+  const int64_t orow = (int64_t)b * p.io_steps * p.Hq + at;
+  if constexpr (!kBf16) {
+    *reinterpret_cast<float4*>(static_cast<float*>(p.out) + orow * D + 4 * c4) = float4{A.x * inv, A.y * inv, A.z * inv, A.w * inv};
+    return;
+  }
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
   const bf16x4 o = {(__bf16)(A.x * inv), (__bf16)(A.y * inv), (__bf16)(A.z * inv), (__bf16)(A.w * inv)};
-  const int64_t orow = (int64_t)b * p.io_steps * p.Hq + at;
   *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(p.out) + orow * D + 4 * c4) = o;
 }
 
@@ -361,18 +352,22 @@ hipError_t launch_spans(const SpanParams& p, int batch, int D, int dtype, int wa
   return launch_spans_of<64>(p, batch, dtype, waves, stream);
 }
 
-hipError_t launch_combine_spans(const SpanParams& p, int batch, int D, hipStream_t stream) {
+namespace {
+template <int D, bool kBf16>
+hipError_t launch_combine_of(const SpanParams& p, int batch, hipStream_t stream) {
   const dim3 block(256);
   if (p.num_splits <= 8) {
     const int64_t total = (int64_t)batch * p.queries * p.Hq;
-    const dim3 few((unsigned)((total * (D / 4) + 255) / 256));
-    if (D == 128) return launch(combine_spans_few<128>, few, block, 0, stream, p, total);
-    return launch(combine_spans_few<64>, few, block, 0, stream, p, total);
+    return launch((combine_spans_few<D, kBf16>), dim3((unsigned)((total * (D / 4) + 255) / 256)), block, 0, stream, p, total);
   }
   const dim3 grid((unsigned)(p.Hq * p.queries), (unsigned)batch);
-  const size_t lds = (size_t)combine_lds_floats(256, D) * sizeof(float);
-  if (D == 128) return launch(combine_spans<128>, grid, block, lds, stream, p);
-  return launch(combine_spans<64>, grid, block, lds, stream, p);
+  return launch((combine_spans<D, kBf16>), grid, block, (size_t)combine_lds_floats(256, D) * sizeof(float), stream, p);
+}
+}  // namespace
+
+hipError_t launch_combine_spans(const SpanParams& p, int batch, int D, int dtype, hipStream_t stream) {
+  if (dtype == TEMPO_F32) return D == 128 ? launch_combine_of<128, false>(p, batch, stream) : launch_combine_of<64, false>(p, batch, stream);
+  return D == 128 ? launch_combine_of<128, true>(p, batch, stream) : launch_combine_of<64, true>(p, batch, stream);
 }
 
 }  // namespace tempo

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   place_tiles(entry);
   // Groups are copied in their order: the next one, at last again and again the split's last, into buffers that nobody reads any
   // more (every iteration then issues the same number of copies, and "all but the newest have landed" is one counted wait).
-  // Scalar instructions take the loop's issue slots as others do (94 an iteration and wavefront in its first form, KEPT now).
+  // Scalar instructions take the loop's issue slots as others do (94 an iteration and wavefront in its first form, 70 now).
   int next_group = from, next_key = key_of(from);
   auto next_offset = [&]() {                  // byte offset of the group in either pool
     const int tile = next_key >> p.z_log2;

@@ -18,6 +18,19 @@ inline size_t tree_lds_bytes(int rows) { return (size_t)rows * (tree_stride(rows
 
 namespace {
 
+// Logits that this lane's column does not see become -inf.  bits: of the group's slots, those of the row's ancestors.
+template <bool kTree>
+__device__ __forceinline__ void mask_span(int key, int lo, int hi, int sinks, uint32_t bits, int lane, float* x) {
+  const int c = lane >> 4;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const int at = 4 * c + (r & 3) + 16 * (r >> 2), j = key + at;
+    bool seen = j <= hi && (j >= lo || j < sinks);
+    if (kTree) seen = seen || ((bits >> at) & 1u) != 0;
+    x[r] = seen ? x[r] : -INFINITY;
+  }
+}
+
 struct Tree {
   const uint32_t* seen;   // [rows][stride]: the rows that a row sees
   const int32_t* depths;  // [rows]

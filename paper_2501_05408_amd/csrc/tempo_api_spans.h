@@ -11,11 +11,10 @@ struct SpanPlan {
   int32_t tile_columns, tiles, split_groups, splits, waves;
 };
 
-// Attention over spans is of bf16 and 8-bit linear stores.
+// Attention over spans is of linear stores.
 int check_span_store(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows) {
   int rc = check_layout(kv);
   if (rc != TEMPO_OK) return rc;
-  if (kv->dtype == TEMPO_F32) return TEMPO_ERR_DTYPE;
   if (kv->ring_blocks != 0) return TEMPO_ERR_SHAPE;
   if ((rc = check_heads(kv, batch, Hq)) != TEMPO_OK) return rc;
   if (rows < 1 || rows > (1 << 24) || (int64_t)rows * Hq > (1 << 30)) return TEMPO_ERR_SHAPE;
@@ -126,21 +125,22 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
       groups = here;
       s.tile_columns = tile;
     }
-    if (columns <= tile) break;  // a wider one holds no more
+    if (columns <= tile || kv->dtype == TEMPO_F32) break;  // a wider one holds no more; fp32: 16
   }
   s.tiles = (int32_t)((columns + s.tile_columns - 1) / s.tile_columns);
   const int64_t most = all < kSpanPartials ? kSpanPartials / all : 1;  // splits that the workspace has room for
   if (s.tile_columns <= 32) {
     const int64_t keys = 32 * (int64_t)groups;  // a multiple of the unit of splits, so that windows have no worst alignment
     // tiles of columns are workgroups of their own, as sequences are
-    const int64_t like = (int64_t)batch * s.tiles;
-    const int32_t queries = s.tile_columns / G < 1 ? 1 : s.tile_columns / G < rows ? s.tile_columns / G : rows;
+    const bool f32 = kv->dtype == TEMPO_F32;  // (whose tiles make_plan() counts itself)
+    const int64_t like = f32 ? batch : (int64_t)batch * s.tiles;
+    const int32_t queries = f32 ? rows : s.tile_columns / G < 1 ? 1 : s.tile_columns / G < rows ? s.tile_columns / G : rows;
     tempo_plan plan;
     make_plan(kv, like < 65535 ? (int32_t)like : 65535, Hq, (int32_t)(keys - 1 < INT32_MAX - 64 ? keys - 1 : INT32_MAX - 64), 0,
               ragged && window == 0 && like * kv->num_kv_heads < kComputeUnits, queries, most < kMaxSplits ? most : kMaxSplits, &plan);
     s.split_groups = plan.tokens_per_split / 32;
     s.waves = plan.waves;
-    if (groups <= whole_groups(kv) && like * kv->num_kv_heads <= kComputeUnits) {
+    if (!f32 && groups <= whole_groups(kv) && like * kv->num_kv_heads <= kComputeUnits) {
       s.split_groups = groups;
       s.waves = groups > 4 ? 8 : groups > 2 ? 4 : groups;
     }
@@ -184,11 +184,12 @@ int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* pa
     p.rope_cos = rope->cos;
     p.rope_sin = rope->sin;
   }
-  const int rc = launch_status(s.tile_columns > 32 ? launch_spans_wide(p, batch, kv->head_dim, kv->dtype, stream)
-                                                   : launch_spans(p, batch, kv->head_dim, kv->dtype, s.waves, stream),
+  const int rc = launch_status(kv->dtype == TEMPO_F32 ? launch_spans_f32(p, batch, kv->head_dim, s.waves, stream)
+                               : s.tile_columns > 32 ? launch_spans_wide(p, batch, kv->head_dim, kv->dtype, stream)
+                                                     : launch_spans(p, batch, kv->head_dim, kv->dtype, s.waves, stream),
                                "attn_spans");
   if (rc != TEMPO_OK || p.direct) return rc;
-  return launch_status(launch_combine_spans(p, batch, kv->head_dim, stream), "attn_spans_combine");
+  return launch_status(launch_combine_spans(p, batch, kv->head_dim, kv->dtype, stream), "attn_spans_combine");
 }
 
 int check_span_workspace(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, bool counts, int32_t window,
@@ -288,12 +289,16 @@ static int sinks_call(const tempo_kv* kv, const tempo_rope* rope, const void* q,
   if ((rc = check_span(kv, t, rows, window, sinks)) != TEMPO_OK) return rc;
   if ((rc = check_scale(scale)) != TEMPO_OK) return rc;
   if (rope && (rc = check_rope(rope, kv->head_dim, t + rows - 1)) != TEMPO_OK) return rc;
+  if (rope && kv->dtype == TEMPO_F32 && (rows > 1 || count_per_seq)) return TEMPO_ERR_DTYPE;  // rows of several steps are not turned on their way in
   if (write && (int64_t)batch * rows * kv->num_kv_heads * kv->head_dim > INT32_MAX) return TEMPO_ERR_SHAPE;
   SpanPlan plan;
   if ((rc = check_span_workspace(kv, batch, Hq, rows, t, t_per_seq != nullptr, count_per_seq != nullptr, window, sinks, false, workspace, workspace_bytes, &plan)) != TEMPO_OK) return rc;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const bool fused = write && rows == 1 && Hq / kv->num_kv_heads <= 32;  // the attention of a step writes its row itself
-  if (write && !fused) {
+  const bool f32 = kv->dtype == TEMPO_F32, fused = write && !f32 && rows == 1 && Hq / kv->num_kv_heads <= 32;  // the attention of a step writes its row itself
+  if (write && f32 && rope) {
+    const StoreParams p = store_params(kv, batch, t, t_per_seq);
+    if ((rc = launch_status(launch_rope_append(p, rope->cos, rope->sin, k_new, v_new, kv->head_dim, kv->dtype, s), "kv_append")) != TEMPO_OK) return rc;
+  } else if (write && !fused) {
     StoreParams p = store_params(kv, batch, t, t_per_seq, rows);
     p.count_per_seq = count_per_seq;
     if (rope) {

@@ -10,7 +10,8 @@ static hipError_t spans(const char* what, const SpanParams& p, int batch, int D,
 }
 hipError_t launch_spans(const SpanParams& p, int batch, int D, int, int waves, hipStream_t) { return spans("spans", p, batch, D, waves); }
 hipError_t launch_spans_wide(const SpanParams& p, int batch, int D, int, hipStream_t) { return spans("spans_wide", p, batch, D, 4); }
-hipError_t launch_combine_spans(const SpanParams& p, int batch, int D, hipStream_t) { return spans("combine_spans", p, batch, D, 0); }
+hipError_t launch_spans_f32(const SpanParams& p, int batch, int D, int waves, hipStream_t) { return spans("spans_f32", p, batch, D, waves); }
+hipError_t launch_combine_spans(const SpanParams& p, int batch, int D, int, hipStream_t) { return spans("combine_spans", p, batch, D, 0); }
 hipError_t launch_place(const PlaceParams& p, const void* k, const void*, int, int, hipStream_t) {
   return say("place t=%d count=%d Hq=%d Hrows=%d axes=%d rows=%d low=%zu high=%zu k=%zu", p.t, p.count, p.Hq, p.Hrows, p.axes, p.table_rows,
              (size_t)p.axis_bits[0], (size_t)p.axis_bits[1], (size_t)k);

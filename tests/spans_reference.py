@@ -61,6 +61,18 @@ def within(got, out, size):
     assert not np.isnan(got).any() and worst <= 1.0, f"{worst:.3f} of the bound at {np.unravel_index(np.argmax(np.abs(got - out) / bound), out.shape)}"
 
 
+def within_fp32(got, out, size, q, K, turns=0):
+    """A logit of D products: D + 4 roundings of at most sum |q k| <= |q| |k| each, scale and log2 e among them; its weight is off by as much,
+    and by 4 steps more for the power of two and the running maximum.  Sums over T keys: T/4 + 64 additions of four products, and a product by
+    a power of two for each group of 32 keys.  Rows that were turned in fp32 (turns: of queries 1, of keys too 2): a product and a fused
+    multiply-add of a pair, against one rounding: 3 roundings of at most sqrt(2) of it.  Numerator and sum are each off by that part of themselves; one division."""
+    T, D = K.shape[0], K.shape[-1]
+    norms = np.sqrt((q ** 2).sum(-1)).max() * np.sqrt(np.nanmax((K ** 2).sum(-1))) / math.sqrt(D)
+    part = 2.0 ** -24 * ((D + 4 + 4.3 * turns) * norms + 8 + T / 4 + 64 + T / 8)
+    bound = 1.03 * (part * (size + np.abs(out)) + 2.0 ** -24 * np.abs(out)) + 1e-37
+    assert not np.isnan(got).any() and (np.abs(got - out) <= bound).all(), f"{np.max(np.abs(got - out) / bound):.3f} of the bound"
+
+
 def turned(x, cos, sin):
     """Rows x [..., D], cosines and sines [..., D/2]."""
     half = x.shape[-1] // 2

@@ -14,7 +14,7 @@ from spans_reference import sees_chain, sees_tree
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 AT = 1 << 20                              # pointers that are checked for NULL and alignment, never read
-STORES = [T.TEMPO_BF16, T.TEMPO_E4M3]
+STORES = [T.TEMPO_BF16, T.TEMPO_E4M3, T.TEMPO_F32]
 
 
 @pytest.fixture(scope="module")
@@ -131,7 +131,7 @@ def test_trees_are_launched_whole_and_in_their_workspace(lib):
         assert lib.tempo_attn_tree(ctypes.byref(kv), AT, AT, AT, AT if ragged else None, batch, G * Hkv, nodes, t, AT if ragged else None, window,
                                    sinks, 0.1, AT, nbytes, None) == T.TEMPO_OK
         (name, f), *rest = taken(lib)
-        assert name == ("spans_wide" if f["tile"] == 128 else "spans") and f["tree"] == 1 and f["k"] == 0
+        assert name == ("spans_f32" if dtype == T.TEMPO_F32 else "spans_wide" if f["tile"] == 128 else "spans") and f["tree"] == 1 and f["k"] == 0
         assert [n for n, _ in rest] == ([] if f["splits"] == 1 else ["combine_spans"])
         check(lib, f, batch, G * Hkv, G, D, nodes, t, window, sinks, True, nbytes, ragged)
 
@@ -147,12 +147,13 @@ def test_steps_with_sinks_write_their_row_once(lib):
         assert lib.tempo_decode_step_sinks(ctypes.byref(kv), AT, 3 * AT, AT, AT, batch, G * Hkv, t, AT if ragged else None, window, sinks, 0.1, AT,
                                            nbytes, None) == T.TEMPO_OK
         names = taken(lib)
-        if G > 32:
+        fused = G <= 32 and dtype != T.TEMPO_F32
+        if not fused:
             (name, f), *names = names
             assert name == "append" and f["t"] == t and f["count"] == 1 and f["k"] == 3 * AT
         (name, f), *rest = names
-        assert name in ("spans", "spans_wide") and f["k"] == (0 if G > 32 else 3 * AT) and f["tree"] == 0
-        assert G > 32 or name == "spans"
+        assert name in (("spans_f32",) if dtype == T.TEMPO_F32 else ("spans", "spans_wide")) and f["k"] == (3 * AT if fused else 0) and f["tree"] == 0
+        assert G > 32 or name != "spans_wide"
         assert [n for n, _ in rest] == ([] if f["splits"] == 1 else ["combine_spans"])
         check(lib, f, batch, G * Hkv, G, D, 1, t, window, sinks, False, nbytes, ragged)
 
@@ -169,7 +170,7 @@ def test_prompts_with_sinks_are_written_then_answered(lib):
         lib.host_launches_take()
         assert lib.tempo_prefill_sinks(ctypes.byref(kv), AT, AT, AT, AT, batch, G * Hkv, t, count, None, window, sinks, 0.1, AT, nbytes, None) == T.TEMPO_OK
         names = taken(lib)
-        fused = count == 1 and G <= 32
+        fused = count == 1 and G <= 32 and dtype != T.TEMPO_F32
         if not fused:
             (name, f), *names = names
             assert name == "append" and f["t"] == t and f["count"] == count
