@@ -699,7 +699,7 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  * in blocks of their own then: the sizes that tempo_sink_blocks gives for its `queries` steps do that.  (Longer prompts by several calls.)
  *
  * tempo_sink_blocks         *sink_blocks = ceil(sinks / Z); *window_blocks = the most tiles that the windows of `queries` consecutive
- *                           steps touch.  Host only; TEMPO_ERR_RANGE for window, Z or queries < 1 or sinks < 0, TEMPO_ERR_NULL.
+ *                           steps touch.  Host only; TEMPO_ERR_RANGE for window, Z or queries < 1, sinks < 0 or 2^31 tiles and more, TEMPO_ERR_NULL.
  * tempo_attn_sinks          `queries` consecutive steps t .. t+queries-1 (t_per_seq[b] ..; t their upper bound), which the store
  *                           holds: q, out device, [batch][queries][Hq][D].  Any number of steps.
  * tempo_decode_step_sinks   one step whose row k_new, v_new (device, [batch][Hkv][D]) is written first; q, out [batch][Hq][D].

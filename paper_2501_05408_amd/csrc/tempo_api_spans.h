@@ -236,9 +236,10 @@ extern "C" {
 int tempo_sink_blocks(int32_t window, int32_t sinks, int32_t Z, int32_t queries, int32_t* sink_blocks, int32_t* window_blocks) {
   if (!sink_blocks || !window_blocks) return TEMPO_ERR_NULL;
   if (window < 1 || sinks < 0 || Z < 1 || queries < 1) return TEMPO_ERR_RANGE;
-  const int64_t keys = (int64_t)window + queries - 1;
+  const int64_t keys = (int64_t)window + queries - 1, turn = (keys + Z - 2) / Z + 1;
+  if (turn > INT32_MAX) return TEMPO_ERR_RANGE;
   *sink_blocks = (int32_t)(((int64_t)sinks + Z - 1) / Z);
-  *window_blocks = (int32_t)((keys + Z - 2) / Z + 1);
+  *window_blocks = (int32_t)turn;
   return TEMPO_OK;
 }
 

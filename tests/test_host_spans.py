@@ -39,6 +39,10 @@ def test_blocks_of_windows_with_sinks_refused():
     assert lib.tempo_sink_blocks(1, 1, 32, 1, None, ctypes.byref(b)) == T.TEMPO_ERR_NULL
     assert lib.tempo_sink_blocks(1, 1, 32, 1, ctypes.byref(a), None) == T.TEMPO_ERR_NULL
     assert T.tempo_sink_blocks(2 ** 31 - 1, 2 ** 31 - 1, 1, 1) == (2 ** 31 - 1, 2 ** 31 - 1)
+    # more tiles than an int32 counts
+    for window, queries in ((2 ** 31 - 1, 2), (2 ** 31 - 1, 2 ** 31 - 1), (2, 2 ** 31 - 1)):
+        assert lib.tempo_sink_blocks(window, 0, 1, queries, ctypes.byref(a), ctypes.byref(b)) == T.TEMPO_ERR_RANGE
+    assert T.tempo_sink_blocks(2 ** 31 - 1, 0, 4, 2 ** 31 - 1) == (0, 2 ** 30)
 
 
 GOOD = dict(kv=None, q=FAKE, k=FAKE, v=FAKE, out=FAKE, parents=FAKE, nodes=None, batch=2, Hq=6, rows=5, t=100, steps=None, window=20, sinks=4,
