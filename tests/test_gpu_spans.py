@@ -500,3 +500,43 @@ def test_values_that_nobody_sees_and_large_ones(dtype):
     top = np.abs(np.einsum("nhd,td->nht", np.abs(q[0]), np.abs(kept(dtype, K[0]))[:, 0])).max() / 8.0
     slack = 4 * D * 2.0 ** -24 * top
     assert np.abs(np64(out)[0] - o).max() <= (1.03 * 2.0 ** -8 * 3 + 2 * slack) * np.abs(V).max()
+
+
+@pytest.mark.parametrize("dtype", ALL_STORES)
+@pytest.mark.parametrize("seed", range(24))
+def test_drawn_calls(dtype, seed):
+    """Trees, steps and prompts of any shape."""
+    rng = np.random.default_rng(1000 + seed)
+    pick = lambda *x: x[int(rng.integers(0, len(x)))]  # noqa: E731
+    Hkv, G, D, B = pick(1, 2, 3, 8), pick(1, 2, 3, 4, 5, 8, 16, 17, 33, 128), pick(64, 128), pick(1, 2, 3, 7)
+    Z, t = pick(32, 64, 128), int(2 ** rng.uniform(0, 9.5)) - 1
+    rows = min(int(2 ** rng.uniform(0, 8.1)), max(1, 1200 // (G * Hkv)))
+    window, sinks = pick(1, 2, 33, int(2 ** rng.uniform(0, 10))), pick(0, 1, 4, int(2 ** rng.uniform(0, 8)))
+    ragged, counts, Hq = rng.random() < 0.5, rng.random() < 0.5, G * Hkv
+    n = rng.integers(0, rows + 1, B) if counts else np.full(B, rows)
+    q, K, V = normal(seed, 1, (B, rows, Hq, D), dtype), normal(seed, 2, (B, t + rows, Hkv, D), dtype), normal(seed, 3, (B, t + rows, Hkv, D), dtype)
+
+    def check(got, seen, steps, n):
+        for b in range(B):
+            assert (got[b, n[b]:] == UNTOUCHED).all()
+            if n[b]:
+                end = steps[b] + n[b]
+                near(dtype, got[b, :n[b]], q[b, :n[b]], K[b, :end], V[b, :end], seen(b))
+
+    st = make_store(seed, dtype, B, Hq, Hkv, D, Z, t + rows - 1)
+    steps = pick_steps(rng, t, B, ragged)
+    parents = np.stack([tree_of(pick("random", "chain", "star", "deep"), rows, rng) for _ in range(B)])
+    write_lengths(st, K, V, steps + n)
+    out = rows_of(dtype, np.full(q.shape, UNTOUCHED))
+    for w, s in ((0, 0), (window, sinks)):
+        out.fill_(UNTOUCHED)
+        st.attend_tree(rows_of(dtype, q), out, ints(parents), t, ints(n) if counts else None, w, s, ints(steps) if ragged else None)
+        check(np64(out), lambda b: sees_tree(steps[b], parents[b, :n[b]], w, s), steps, n)
+    write_lengths(st, K, V, steps + rows)
+    st.attend_sinks(rows_of(dtype, q), out, t, rows, window, sinks, ints(steps) if ragged else None)
+    check(np64(out), lambda b: sees_chain(steps[b], rows, window, sinks), steps, np.full(B, rows))
+    st = make_store(seed, dtype, B, Hq, Hkv, D, Z, t + rows - 1)
+    write_lengths(st, K, V, np.full(B, t))
+    out.fill_(UNTOUCHED)
+    st.prefill_sinks(rows_of(dtype, q), rows_of(dtype, K[:, t:]), rows_of(dtype, V[:, t:]), out, t, rows, window, sinks, ints(n) if counts else None)
+    check(np64(out), lambda b: sees_chain(t, n[b], window, sinks), np.full(B, t), n)
