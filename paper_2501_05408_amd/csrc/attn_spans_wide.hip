@@ -90,9 +90,9 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
     const int n = ((const_i32_ptr)p.count_per_seq)[b];
     rows = n < 0 ? 0 : (n < rows ? n : rows);
   }
-  const int first = block * (kWaveColumns * NW), all = rows * p.G;  // columns
+  const int first = block * p.tile_columns, all = rows * p.G;  // columns
   if (first >= all) return;                   // uniform over the workgroup, before any barrier
-  const int ncols = all - first < kWaveColumns * NW ? all - first : kWaveColumns * NW;
+  const int ncols = all - first < p.tile_columns ? all - first : p.tile_columns;
   const int c0 = first / p.G, skip = first - c0 * p.G, row_last = c0 + (skip + ncols - 1) / p.G;
   const SpanRange rg = span_range(t_b, kTree ? 0 : c0, row_last, p.window, p.sinks);
   const int from = split * p.split_groups;
@@ -499,7 +499,7 @@ hipError_t launch_wide(const SpanParams& p, int batch, hipStream_t stream) {
 
 hipError_t launch_spans_wide(const SpanParams& p, int batch, int D, int dtype, hipStream_t stream) {
   const bool k8 = dtype == TEMPO_E4M3;
-  if (p.tile_columns != 128) return hipErrorInvalidConfiguration;
+  if (p.tile_columns < kWaveColumns || p.tile_columns > 128 || p.tile_columns % kWaveColumns != 0) return hipErrorInvalidConfiguration;
   if (D == 128) return k8 ? launch_wide<128, 4, true>(p, batch, stream) : launch_wide<128, 4, false>(p, batch, stream);
   return k8 ? launch_wide<64, 4, true>(p, batch, stream) : launch_wide<64, 4, false>(p, batch, stream);
 }

@@ -105,6 +105,16 @@ double span_cost_us(const tempo_kv* kv, int64_t pairs, int64_t columns, int64_t 
   return cost;
 }
 
+// Wavefronts that share few groups, if four to a workgroup would not fit the part at once: more workgroups side by side hide each other's
+// beginnings and ends better (us with 4 / 2 / 1: 3648 of 3 groups, 32 columns, 8 bits, D = 128 65 / 49 / 41; 720 of 4, bf16 28 / 20 / 23; 2048 of 3,
+// 16 columns, 8 bits 19.5 / 16.2 / 13.5; D = 64, 1944 of 10, 16 columns, 8 bits 33.5 / 24.6 / 25.7; 1008 of 4, bf16 16.1 / 13.6 / 15.6;
+// ragged 768 of 9, 32 columns, D = 128 19.0 / 22.5 / 30.4).
+int32_t few_waves(int64_t workgroups, int32_t groups, int D, int32_t tile, bool ragged) {
+  const int64_t room = kComputeUnits * (D == 128 ? (tile == 16 ? 12 : 8) : (tile == 16 ? 14 : 12));  // (D = 64, 16 columns: registers let in 16)
+  if (groups < 3 || groups > (ragged ? 8 : 12) || 4 * workgroups <= room) return 8;
+  return !ragged && groups <= 6 && 2 * workgroups > room ? 1 : 2;
+}
+
 // Up to 32 columns a split is planned as a step's or block's of as many keys (make_plan()): the kernel streams keys as theirs do.
 // (Ragged steps, which make_plan() gives short splits, only where there are fewer workgroups than units: 40 trees of up to 20 nodes
 // behind up to 2000 keys, 32/4 heads of 128, 8 bits, one split 35 us, two 50.)
@@ -128,6 +138,9 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
     if (columns <= tile || kv->dtype == TEMPO_F32) break;  // a wider one holds no more; fp32: 16
   }
   s.tiles = (int32_t)((columns + s.tile_columns - 1) / s.tile_columns);
+  // As many wavefronts with columns in every tile (us: 8 trees of 18 nodes behind 6007 keys, 32/4 heads, 144 columns as 2 x 96 34.8, as
+  // 128 + 16 37.3; 4 trees of 64 nodes behind 4000 keys, 24/8 heads 25.2 and 26.9).
+  if (s.tile_columns > 32) s.tile_columns = (int32_t)((columns + s.tiles - 1) / s.tiles + 31) / 32 * 32;
   const int64_t most = all < kSpanPartials ? kSpanPartials / all : 1;  // splits that the workspace has room for
   if (s.tile_columns <= 32) {
     const int64_t keys = 32 * (int64_t)groups;  // a multiple of the unit of splits, so that windows have no worst alignment
@@ -150,6 +163,10 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
   }
   while ((groups + s.split_groups - 1) / s.split_groups > most) s.split_groups *= 2;
   s.splits = (groups + s.split_groups - 1) / s.split_groups;
+  if (s.tile_columns <= 32 && s.splits == 1 && kv->dtype != TEMPO_F32) {
+    const int64_t waves = few_waves((int64_t)batch * kv->num_kv_heads * s.tiles, groups, kv->head_dim, s.tile_columns, ragged || counts);
+    s.waves = s.waves < waves ? s.waves : (int32_t)waves;
+  }
   while (s.tile_columns <= 32 && s.waves > 1 && units_lds_bytes(s.waves, (int)(columns < 16 ? columns : 16), kv->head_dim) > kMaxUnitsLds) s.waves /= 2;
   return s;
 }
