@@ -450,15 +450,21 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
     copies();
     finish();
   }
-  // the copies issued last may still be in flight: they must land before the LDS is given up
+  // the copies issued last may still be in flight: they must land before the LDS is used again or given up
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 
   const float l_j = half_sum(l_run);
-  if (col >= ncols) return;
   if (p.direct) {                             // every row saw itself
-    __bf16* orow = static_cast<__bf16*>(p.out) + (((int64_t)b * p.io_steps + row) * p.Hq + (int64_t)hkv * p.G + gq) * D + 4 * half;
+    // Answers leave in whole rows: a wavefront's 32 columns pass through its quarter of the LDS, a column's 16-byte units in an order that
+    // spreads them over the banks (4 x 4096 steps, window 1024, 259 us with 8 bytes a lane straight from the registers, 252; window 128
+    // 130 and 121.  Partials, 16 bytes a lane, do not gain: 16 ragged trees of 32 nodes 35.9, through LDS 37.4).
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    constexpr int kRow = 2 * D, kUnits = kRow / 16, kRows = 64 / kUnits;
+    __syncthreads();                          // all copies have landed, all operands have been read
+    if (first_col >= ncols) return;
+    char* const own = reinterpret_cast<char*>(lds) + wave * (kWaveColumns * kRow);
     const float inv = 1.0f / l_j;
+    const int n = lane & 31, at_row = row * p.Hq + hkv * p.G + gq;
 #pragma unroll
     for (int ot = 0; ot < OT; ++ot) {
 #pragma unroll
@@ -466,22 +472,31 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
         bf16x4 o;
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[r] = (__bf16)(acc[ot][4 * i + r] * inv);
-        *reinterpret_cast<bf16x4*>(orow + 32 * ot + 8 * i) = o;
+        *reinterpret_cast<bf16x4*>(own + n * kRow + 16 * ((4 * ot + i) ^ (n & (kUnits - 1))) + 8 * half) = o;
       }
     }
-  } else {
-    const int64_t part = (((int64_t)b * p.queries + row) * p.Hq + (int64_t)hkv * p.G + gq) * p.num_splits + split;
-    float* arow = p.ws_acc + part * D + 4 * half;
+    char* const to = static_cast<char*>(p.out) + (int64_t)b * p.io_steps * p.Hq * kRow;
 #pragma unroll
-    for (int ot = 0; ot < OT; ++ot) {
+    for (int k = 0; k < kWaveColumns / kRows; ++k) {
+      const int c = kRows * k + lane / kUnits, unit = lane % kUnits;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(own + c * kRow + 16 * (unit ^ (c & (kUnits - 1))));
+      const int at = __shfl(at_row, c);
+      if (first_col + c < ncols) *reinterpret_cast<u32x4*>(to + (int64_t)at * kRow + 16 * unit) = v;
+    }
+    return;
+  }
+  if (col >= ncols) return;
+  const int64_t part = (((int64_t)b * p.queries + row) * p.Hq + (int64_t)hkv * p.G + gq) * p.num_splits + split;
+  float* arow = p.ws_acc + part * D + 4 * half;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(arow + 32 * ot + 8 * i) = f32x4{acc[ot][4 * i], acc[ot][4 * i + 1], acc[ot][4 * i + 2], acc[ot][4 * i + 3]};
-    }
-    if (half == 0) {
-      p.ws_ml[part * 2] = m_run;
-      p.ws_ml[part * 2 + 1] = l_j;
-    }
+  for (int ot = 0; ot < OT; ++ot) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(arow + 32 * ot + 8 * i) = f32x4{acc[ot][4 * i], acc[ot][4 * i + 1], acc[ot][4 * i + 2], acc[ot][4 * i + 3]};
+  }
+  if (half == 0) {
+    p.ws_ml[part * 2] = m_run;
+    p.ws_ml[part * 2 + 1] = l_j;
   }
 }
 
