@@ -30,6 +30,17 @@ __device__ __forceinline__ void mask_span_tile(int key, int lo, int hi, int sink
   }
 }
 
+// The same where only one end matters: slots behind `hi`, or before `lo`, which are numbered from the lane's first of the group on (two
+// instructions a logit for six).
+__device__ __forceinline__ void mask_behind(int hi, f32x16& x) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = 8 * (r >> 2) + (r & 3) <= hi ? x[r] : -INFINITY;
+}
+__device__ __forceinline__ void mask_before(int lo, f32x16& x) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = 8 * (r >> 2) + (r & 3) >= lo ? x[r] : -INFINITY;
+}
+
 // Of the 8 slots of lane (n + 16c)'s pieces of values those that some row may see: two to a word.
 __device__ __forceinline__ void keep_values(int key, int lo, int last, int sinks, int lane, uint32_t* keep) {
   const int c = (lane >> 4) & 3;
@@ -333,11 +344,16 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   auto enter = [&](int g, f32x16& x, float mx) {
     if (g >= sink_whole && (g < whole_first || g > whole_last)) {
       const int key = key_of(g);
-      uint32_t bits = 0;
-      if constexpr (kTree) {
-        if (key + 31 >= t_b) bits = tree.bits(row, key - t_b);
+      if (key < p.sinks || (kTree && key + 31 >= t_b)) {
+        uint32_t bits = 0;
+        if constexpr (kTree) {
+          if (key + 31 >= t_b) bits = tree.bits(row, key - t_b);
+        }
+        mask_span_tile<kTree>(key, lo_col, hi_col, p.sinks, bits, lane, x);
+      } else {
+        if (g > whole_last) mask_behind(hi_col - key - 4 * half, x);
+        if (g < whole_first) mask_before(lo_col - key - 4 * half, x);
       }
-      mask_span_tile<kTree>(key, lo_col, hi_col, p.sinks, bits, lane, x);
       mx = tile_max(x);
     }
     softmax_reference<D>(mx, p.scale_log2e, limit, m_run, base, acc, l_run);
