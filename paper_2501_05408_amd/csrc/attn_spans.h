@@ -47,14 +47,36 @@ __host__ __device__ inline SpanRange tile_range(int t, int tile, int tile_column
 // What workgroup (x, y, z) takes of a launch for many columns, whose grid is (kv heads * blocks of columns, sequences, splits).  The
 // blocks of one (sequence, kv head, split) read the same keys, so they run on one die.  Few blocks: units of work lie on the dies in
 // turn (units_work()).  The many of a prompt, whose neighbours read nearly the same windows: each die gets a contiguous run of the
-// list of blocks, a unit's last block first.
+// list of blocks, a unit's last block first, and at its end, so that the die's workgroups end together, one of the list of the units' first
+// `fewer` blocks, whose windows begin before step 0: those of an eighth of the units at a time, from the longest on.  (us, unit by unit / so: 4 x 4096
+// steps of 24/8 heads of 128, window 1024 249 / 246, 512 176 / 173, 8 bits 275 / 267; 32/8 heads of 64, window 4000 335 / 323; 6000 steps 145 / 145.5.)
 constexpr uint32_t kRunBlocks = 8;
-__host__ __device__ inline UnitsWork wide_work(uint32_t x, uint32_t y, uint32_t z, uint32_t nx, uint32_t ny, uint32_t nz, int Hkv) {
+__host__ __device__ inline UnitsWork wide_work(uint32_t x, uint32_t y, uint32_t z, uint32_t nx, uint32_t ny, uint32_t nz, int Hkv, uint32_t fewer) {
   const uint32_t blocks = nx / (uint32_t)Hkv;
   if (blocks <= kRunBlocks) return units_work(x, y, z, nx, ny, nz, Hkv);
-  const uint32_t total = nx * ny * nz, linear = x + nx * (y + ny * z), die = linear & 7u, share = total >> 3, extra = total & 7u;
-  const uint32_t item = die * share + (die < extra ? die : extra) + (linear >> 3), unit = item / blocks, row = unit / nz;
-  return {(int)(row % (uint32_t)Hkv), (int)(blocks - 1 - (item - unit * blocks)), (int)(row / (uint32_t)Hkv), (int)(unit - row * nz)};
+  const uint32_t total = nx * ny * nz, linear = x + nx * (y + ny * z), die = linear & 7u, at = linear >> 3, units = total / blocks;
+  const uint32_t full = blocks - fewer, first = units * full, share = first >> 3, extra = first & 7u;
+  const uint32_t begin = die * share + (die < extra ? die : extra), mine = share + (die < extra ? 1 : 0);
+  uint32_t unit, block;
+  if (at < mine) {
+    const uint32_t item = begin + at;
+    unit = item / full;
+    block = blocks - 1 - (item - unit * full);
+  } else {
+    const uint32_t item = die * (total >> 3) + (die < (total & 7u) ? die : total & 7u) - begin + at - mine;
+    const uint32_t together = (units + 7) >> 3, set = item / (together * fewer), left = units - set * together, width = left < together ? left : together;
+    const uint32_t in = item - set * together * fewer, row = in / width;
+    unit = set * together + in - row * width;
+    block = fewer - 1 - row;
+  }
+  const uint32_t row = unit / nz;
+  return {(int)(row % (uint32_t)Hkv), (int)block, (int)(row / (uint32_t)Hkv), (int)(unit - row * nz)};
+}
+// Blocks of columns whose first row is nearer to step 0 than its window is long.
+__host__ __device__ inline uint32_t fewer_keys(int t, int window, int G, int tile_columns, uint32_t blocks) {
+  if (window <= 0 || t >= window) return 0;
+  const int64_t n = ((int64_t)(window - t) * G + tile_columns - 1) / tile_columns;
+  return n < (int64_t)blocks ? (uint32_t)n : blocks;
 }
 
 // Rows at positions of their own.

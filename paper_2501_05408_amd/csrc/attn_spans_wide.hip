@@ -92,7 +92,8 @@ __global__ __launch_bounds__(64 * NW, 2) void attn_spans_wide(SpanParams p) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const UnitsWork item = wide_work(blockIdx.x, blockIdx.y, blockIdx.z, gridDim.x, gridDim.y, gridDim.z, p.Hkv);
+  const UnitsWork item = wide_work(blockIdx.x, blockIdx.y, blockIdx.z, gridDim.x, gridDim.y, gridDim.z, p.Hkv,
+                                   kTree ? 0 : fewer_keys(p.t, p.window, p.G, p.tile_columns, gridDim.x / (uint32_t)p.Hkv));
   const int hkv = item.hkv, b = item.b, split = item.split, block = item.tile;
   int t_b = p.t_per_seq ? ((const_i32_ptr)p.t_per_seq)[b] : p.t;
   t_b = t_b > p.t ? p.t : (t_b < 0 ? 0 : t_b);

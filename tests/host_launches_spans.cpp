@@ -33,8 +33,9 @@ void span_range_of(int t, int tile, int tile_columns, int G, int rows, int windo
 int span_group_of(int t, int first, int last, int window, int sinks, int i) {
   return tempo::span_group(tempo::span_range(t, first, last, window, sinks), i);
 }
-void wide_work_of(uint32_t x, uint32_t y, uint32_t z, uint32_t nx, uint32_t ny, uint32_t nz, int Hkv, int32_t* out) {
-  const tempo::UnitsWork w = tempo::wide_work(x, y, z, nx, ny, nz, Hkv);
+uint32_t fewer_keys_of(int t, int window, int G, int tile_columns, uint32_t blocks) { return tempo::fewer_keys(t, window, G, tile_columns, blocks); }
+void wide_work_of(uint32_t x, uint32_t y, uint32_t z, uint32_t nx, uint32_t ny, uint32_t nz, int Hkv, uint32_t fewer, int32_t* out) {
+  const tempo::UnitsWork w = tempo::wide_work(x, y, z, nx, ny, nz, Hkv, fewer);
   out[0] = w.hkv;
   out[1] = w.tile;
   out[2] = w.b;

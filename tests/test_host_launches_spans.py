@@ -89,17 +89,33 @@ def test_ranges_far_out(lib):
 def test_all_wide_work_is_taken_once(lib, Hkv):
     out = (ctypes.c_int32 * 4)()
     for blocks, B, splits in itertools.product((1, 2, 8, 9, 13, 30), (1, 2, 5), (1, 2, 3)):
-        seen, dies = set(), {}
-        for z, y, x in itertools.product(range(splits), range(B), range(Hkv * blocks)):
-            lib.wide_work_of(x, y, z, Hkv * blocks, B, splits, Hkv, out)
-            hkv, block, b, split = got = tuple(out)
-            assert 0 <= hkv < Hkv and 0 <= block < blocks and 0 <= b < B and 0 <= split < splits
-            seen.add(got)
-            dies.setdefault((x + Hkv * blocks * (y + B * z)) % 8, []).append((b, hkv, split, -block))
-        assert len(seen) == Hkv * blocks * B * splits
-        if blocks > 8:                    # a die's blocks follow each other
-            for run in dies.values():
-                assert run == sorted(run)
+        for fewer in sorted({0, 1, blocks // 3, blocks - 1, blocks}):
+            seen, dies = set(), {}
+            for z, y, x in itertools.product(range(splits), range(B), range(Hkv * blocks)):
+                lib.wide_work_of(x, y, z, Hkv * blocks, B, splits, Hkv, fewer, out)
+                hkv, block, b, split = got = tuple(out)
+                assert 0 <= hkv < Hkv and 0 <= block < blocks and 0 <= b < B and 0 <= split < splits
+                seen.add(got)
+                dies.setdefault((x + Hkv * blocks * (y + B * z)) % 8, []).append((b, hkv, split, -block))
+            assert len(seen) == Hkv * blocks * B * splits
+            if blocks > 8:                    # a die's blocks follow each other, those with fewer keys last, from the longest on
+                units = Hkv * B * splits
+                for run in dies.values():
+                    most = [w for w in run if -w[3] >= fewer]
+                    assert run[:len(most)] == most == sorted(most)
+                    rest = run[len(most):]
+                    if units % 8 == 0:
+                        assert rest == sorted(rest, key=lambda w: (w[3], w[:3])) and len({w[:3] for w in rest}) <= units // 8
+
+
+def test_blocks_with_fewer_keys(lib):
+    r = random.Random(9)
+    for _ in range(3000):
+        t, window, G, tile, blocks = r.randrange(0, 300), r.randrange(1, 400), r.choice([1, 3, 8, 20, 128]), r.choice([32, 64, 96, 128]), r.randrange(9, 60)
+        fewer = lib.fewer_keys_of(t, window, G, tile, blocks)
+        assert fewer == sum(t + n * tile // G < window and t + n * tile / G < window for n in range(blocks))
+    assert lib.fewer_keys_of(0, 0, 3, 128, 40) == 0 and lib.fewer_keys_of(2 ** 31 - 200, 2 ** 31 - 1, 128, 32, 2 ** 20) == 796
+    assert lib.fewer_keys_of(0, 2 ** 31 - 1, 128, 32, 1000) == 1000
 
 
 # ---- launches --------------------------------------------------------------------------------------------
