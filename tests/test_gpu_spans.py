@@ -540,3 +540,59 @@ def test_drawn_calls(dtype, seed):
     out.fill_(UNTOUCHED)
     st.prefill_sinks(rows_of(dtype, q), rows_of(dtype, K[:, t:]), rows_of(dtype, V[:, t:]), out, t, rows, window, sinks, ints(n) if counts else None)
     check(np64(out), lambda b: sees_chain(t, n[b], window, sinks), np.full(B, t), n)
+
+
+def framed(n, dtype):
+    """A tensor of n elements between two frames of 4096, and a check that the frames are as they were."""
+    whole = torch.full((n + 8192,), 119, dtype=torch.uint8, device=DEV) if dtype == torch.uint8 else torch.full((n + 8192,), -9.0, dtype=dtype, device=DEV)
+    before = whole.clone()
+
+    def intact():
+        assert torch.equal(whole[:4096], before[:4096]) and torch.equal(whole[-4096:], before[-4096:])
+    return whole[4096:4096 + n], intact
+
+
+@pytest.mark.parametrize("dtype", ALL_STORES)
+@pytest.mark.parametrize("Hq,Hkv,D,B,t,rows,window,sinks", [
+    (24, 8, 128, 2, 700, 1, 300, 4), (24, 8, 128, 3, 333, 8, 100, 5), (32, 8, 64, 1, 2500, 13, 1000, 33), (32, 4, 128, 2, 900, 41, 500, 4),
+    (32, 4, 64, 1, 3000, 23, 2000, 0), (16, 16, 64, 20, 90, 30, 60, 2), (6, 2, 128, 2, 40, 256, 77, 3), (128, 1, 64, 1, 1500, 3, 900, 31),
+])
+def test_nothing_is_written_beside_answers_workspace_and_rows(dtype, Hq, Hkv, D, B, t, rows, window, sinks):
+    """Exact workspaces and answers between frames; blocks of no sequence and slots behind the rows stay."""
+    rng = np.random.default_rng(t)
+    st = make_store(97, dtype, B, Hq, Hkv, D, 64, t + rows - 1)
+    K, V = normal(97, 2, (B, t, Hkv, D), dtype), normal(97, 3, (B, t, Hkv, D), dtype)
+    write_lengths(st, K, V, [t] * B)
+    q, k, v = (rows_of(dtype, normal(98, w, (B, rows, h, D), dtype)) for w, h in ((1, Hq), (2, Hkv), (3, Hkv)))
+    parents = ints(np.stack([tree_of("random", rows, rng) for _ in range(B)]))
+    out, out_intact = framed(q.numel(), q.dtype)
+    out = out.view(q.shape)
+    pools = st.k_pool.clone(), st.v_pool.clone()
+    n = T.tempo_prefill_sinks_workspace_bytes(st.kv, B, Hq, t + rows - 1)
+    n = min(n, T.tempo_attn_sinks_workspace_bytes(st.kv, B, Hq, rows, t, window, sinks))  # (of the same steps: as much is needed)
+    ws, ws_intact = framed(n, torch.uint8)
+    assert ws.data_ptr() % 256 == 0
+    T.tempo_prefill_sinks(st.kv, q, k, v, out, B, Hq, t, rows, None, window, sinks, st.scale, ws, n)
+    out_intact(), ws_intact()
+    first = out.clone()
+    written = st.k_pool.clone(), st.v_pool.clone()
+    T.tempo_attn_sinks(st.kv, q, out, B, Hq, rows, t, None, window, sinks, st.scale, ws, n)
+    out_intact(), ws_intact()
+    if rows > 1:  # (a single step's row is patched in as it is written, with the same bits)
+        assert torch.equal(out, first)
+    n = T.tempo_attn_tree_workspace_bytes(st.kv, B, Hq, rows, t, window, sinks)
+    ws, ws_intact = framed(n, torch.uint8)
+    T.tempo_attn_tree(st.kv, q, out, parents, None, B, Hq, rows, t, None, window, sinks, st.scale, ws, n)
+    out_intact(), ws_intact()
+    for now, then in zip((st.k_pool, st.v_pool), written):  # attention writes no row
+        assert torch.equal(now.view(torch.uint8), then.view(torch.uint8))
+    # blocks that no sequence has, and those that hold none of the rows
+    changed = torch.ones(st.num_blocks, dtype=torch.bool, device=DEV)
+    changed[st.block_table[:, t // 64:(t + rows - 1) // 64 + 1].flatten().long()] = False
+    for now, then in zip((st.k_pool, st.v_pool), pools):
+        codes = st.num_blocks * Hkv * 64 * D if dtype == T.TEMPO_E4M3 else now.numel()
+        a, b = (x.flatten()[:codes].view(st.num_blocks, -1).view(torch.uint8) for x in (now, then))
+        assert torch.equal(a[changed], b[changed])
+        if dtype == T.TEMPO_E4M3:
+            a, b = (x.flatten()[codes:].view(st.num_blocks, -1) for x in (now, then))
+            assert torch.equal(a[changed], b[changed])
