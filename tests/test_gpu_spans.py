@@ -596,3 +596,55 @@ def test_nothing_is_written_beside_answers_workspace_and_rows(dtype, Hq, Hkv, D,
         if dtype == T.TEMPO_E4M3:
             a, b = (x.flatten()[codes:].view(st.num_blocks, -1) for x in (now, then))
             assert torch.equal(a[changed], b[changed])
+
+
+@pytest.mark.parametrize("dtype", STORES)
+@pytest.mark.parametrize("Hq,Hkv,D,B,ragged", [(16, 8, 128, 200, False), (16, 8, 128, 230, True), (136, 8, 128, 180, False), (32, 8, 64, 330, False), (32, 8, 64, 260, True)])
+def test_many_workgroups_of_few_groups(dtype, Hq, Hkv, D, B, ragged):
+    """One or two wavefronts to a workgroup: steps that write their row, trees."""
+    rng = np.random.default_rng(B)
+    t, window, sinks, nodes = 130, 90, 3, 2
+    steps = pick_steps(rng, t, B, ragged)
+    st = make_store(99, dtype, B, Hq, Hkv, D, 32, t + nodes)
+    K, V = normal(99, 2, (B, t + nodes, Hkv, D)), normal(99, 3, (B, t + nodes, Hkv, D))
+    st.append_block(bf16(K), bf16(V), 0, t + nodes)
+    # the step's row is written anew
+    k, v, q = normal(100, 2, (B, Hkv, D)), normal(100, 3, (B, Hkv, D)), normal(100, 1, (B, Hq, D))
+    out = bf16(np.zeros(q.shape))
+    st.step_sinks(bf16(q), bf16(k), bf16(v), out, t, window, sinks, ints(steps) if ragged else None)
+    got, some = np64(out), [0, 1, B - 1] + [int(b) for b in rng.integers(0, B, 7)]
+    for b in some:
+        K[b, steps[b]], V[b, steps[b]] = k[b], v[b]
+        end = steps[b] + 1
+        near(dtype, got[b][None], q[b][None], K[b, :end], V[b, :end], sees_chain(steps[b], 1, window, sinks))
+    k_back, v_back = (np64(x) for x in st.gather(0, t + 1))
+    for b in some:
+        np.testing.assert_array_equal(k_back[b], kept(dtype, K[b, :t + 1]))
+        np.testing.assert_array_equal(v_back[b], kept(dtype, V[b, :t + 1]))
+    parents = np.tile([[-1, 0]], (B, 1))
+    parents[::2, 1] = -1
+    q = normal(101, 1, (B, nodes, Hq, D))
+    out = bf16(np.zeros(q.shape))
+    st.attend_tree(bf16(q), out, ints(parents), t, t_per_seq=ints(steps) if ragged else None)
+    got = np64(out)
+    for b in some:
+        end = steps[b] + nodes
+        near(dtype, got[b], q[b], K[b, :end], V[b, :end], sees_tree(steps[b], parents[b], 0, 0))
+
+
+@pytest.mark.parametrize("dtype", STORES)
+@pytest.mark.parametrize("Hq,Hkv,D,B,count,window", [(16, 8, 128, 6, 900, 40), (8, 8, 64, 8, 1300, 60), (40, 8, 128, 3, 500, 20), (32, 8, 64, 2, 2500, 30)])
+def test_long_prompts_of_short_windows(dtype, Hq, Hkv, D, B, count, window):
+    st = make_store(103, dtype, B, Hq, Hkv, D, 64, count - 1)
+    q, K, V = normal(103, 1, (B, count, Hq, D)), normal(103, 2, (B, count, Hkv, D)), normal(103, 3, (B, count, Hkv, D))
+    out = bf16(np.full(q.shape, UNTOUCHED))
+    n = np.full(B, count)
+    n[1] = count // 2 + 1
+    st.prefill_sinks(bf16(q), bf16(K), bf16(V), out, 0, count, window, 4, ints(n))
+    got = np64(out)
+    for b in (0, 1, B - 1):
+        assert (got[b, n[b]:] == UNTOUCHED).all()
+        for first in (0, n[b] // 2, n[b] - 150):  # (rows 150 at a time: what they see lies among the sinks and the keys near them)
+            rows = np.arange(first, min(first + 150, n[b]))
+            seen = sees_chain(0, int(rows[-1]) + 1, window, 4)[rows]
+            near(dtype, got[b, rows], q[b, rows], K[b, :rows[-1] + 1], V[b, :rows[-1] + 1], seen)
