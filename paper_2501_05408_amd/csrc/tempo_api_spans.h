@@ -108,10 +108,11 @@ double span_cost_us(const tempo_kv* kv, int64_t pairs, int64_t columns, int64_t 
 // Wavefronts that share few groups, if four to a workgroup would not fit the part at once: more workgroups side by side hide each other's
 // beginnings and ends better (us with 4 / 2 / 1: 3648 of 3 groups, 32 columns, 8 bits, D = 128 65 / 49 / 41; 720 of 4, bf16 28 / 20 / 23; 2048 of 3,
 // 16 columns, 8 bits 19.5 / 16.2 / 13.5; D = 64, 1944 of 10, 16 columns, 8 bits 33.5 / 24.6 / 25.7; 1008 of 4, bf16 16.1 / 13.6 / 15.6;
-// ragged 768 of 9, 32 columns, D = 128 19.0 / 22.5 / 30.4).
-int32_t few_waves(int64_t workgroups, int32_t groups, int D, int32_t tile, bool ragged) {
+// ragged 768 of 9, 32 columns, D = 128 19.0 / 22.5 / 30.4; steps, D = 128: 1024 of 5, 8 bits 23.8 / 20.8 / 20.0, 2048 of 3, bf16 30.8 / 29.0 / 28.6,
+// of 11 65 / 69 / 68, so that such, whose tiles share no keys, are taken up to 8 too).
+int32_t few_waves(int64_t workgroups, int32_t tiles, int32_t groups, int D, int32_t tile, bool ragged) {
   const int64_t room = kComputeUnits * (D == 128 ? (tile == 16 ? 12 : 8) : (tile == 16 ? 14 : 12));  // (D = 64, 16 columns: registers let in 16)
-  if (groups < 3 || groups > (ragged ? 8 : 12) || 4 * workgroups <= room) return 8;
+  if (groups < 3 || groups > (ragged || tiles == 1 ? 8 : 12) || 4 * workgroups <= room) return 8;
   return !ragged && groups <= 6 && 2 * workgroups > room ? 1 : 2;
 }
 
@@ -164,7 +165,7 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
   while ((groups + s.split_groups - 1) / s.split_groups > most) s.split_groups *= 2;
   s.splits = (groups + s.split_groups - 1) / s.split_groups;
   if (s.tile_columns <= 32 && s.splits == 1 && kv->dtype != TEMPO_F32) {
-    const int64_t waves = few_waves((int64_t)batch * kv->num_kv_heads * s.tiles, groups, kv->head_dim, s.tile_columns, ragged || counts);
+    const int64_t waves = few_waves((int64_t)batch * kv->num_kv_heads * s.tiles, s.tiles, groups, kv->head_dim, s.tile_columns, ragged || counts);
     s.waves = s.waves < waves ? s.waves : (int32_t)waves;
   }
   while (s.tile_columns <= 32 && s.waves > 1 && units_lds_bytes(s.waves, (int)(columns < 16 ? columns : 16), kv->head_dim) > kMaxUnitsLds) s.waves /= 2;
