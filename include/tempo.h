@@ -690,7 +690,7 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  * once they leave the window).  Step p sees
  *     keys j < sinks, and keys max(0, p-window+1) .. p               (window >= 1, sinks >= 0; keys are counted once)
  * with positions as they were written.  Linear stores (TEMPO_ERR_SHAPE on rings); q, out and rows are of the store's dtype, bf16 for
- * an 8-bit one.  A value inside the union of the ranges that is not finite may show in steps of the call that do not see it, in fp32 too.
+ * an 8-bit one.
  *
  * Constant memory: the table of a linear store may name a block more than once.  Blocks 0 .. sink_blocks-1 of a sequence are kept and
  * window_blocks further ones (tempo_sink_blocks) take the tiles behind them in turn,
@@ -756,7 +756,7 @@ int tempo_rope_prefill_sinks(const tempo_kv* kv, const tempo_rope* rope, const v
  * tempo_attn_tree       q, out device, [batch][nodes][Hq][D].  Node i sees steps 0 .. t-1, its ancestors and itself.  t = 0: no
  *                       step is cached.  With window >= 1 of these only those at a position above t + depth - window or below
  *                       `sinks` (window = 0: all, and sinks must be 0).  Stores, workspace and limits as for tempo_attn_sinks.
- *                       A value of a node that is not finite may show in nodes that do not see it.
+ *                       (A node's value that is not finite, in bf16 or 8 bits: as a step's of a call with several.)
  * tempo_kv_keep         the row at step t + i becomes what step t + kept[b][i] held before the call, keys and values, for
  *                       i = 0, 1, .. up to the first entry of kept (device, int32 [batch][count]) outside 0 .. nodes-1; other
  *                       rows stay as they are.  With the accepted path's node numbers, root first, the sequence goes on at step

@@ -79,6 +79,7 @@ MIN_OCCUPANCY = [
     ("attn_spansILi128E", 2),                  # sinks and trees, D = 128: two workgroups of four wavefronts to a unit, or one of eight
     ("attn_spans_wideILi128E", 2),             # the same, 128 columns: two workgroups to a unit, as its splits are planned
     ("attn_spans_wideILi64E", 3),              # D = 64: three
+    ("attn_spans_f32ILi128ELb0E", 3),          # sinks over an fp32 store, D = 128 (two: 539 -> 609 us for 2048 steps behind 2048 keys)
 ]
 
 

@@ -7,9 +7,12 @@
 // second product as they stand.  A tile of answers takes the dims 64h + 4n + e of lanes n, so that values too are read 16 bytes a lane
 // (read 4 bytes a lane, where they are used: 145 us for 111, 648 for 536).  All in fp32: for parity and for stores that were made in
 // it.  Blocks may be shorter than a group, so every row looks its block up.  A tile of columns streams its keys again, from L2.
+// A value that is not finite shows in the columns that see it, and in no other: in groups that some columns see less of than others such
+// values are taken for 0 and added to their columns behind the loop, where there are any (us, without / with the check: 2048 steps of
+// window 2048 536 / 538, of window 64 58.2 / 59.9; 8 trees of 16 nodes behind 4000 keys 114 / 115; 8 of 100 behind 500, D = 64, 63.3 / 65.5).
 // Bound by memory with few columns (16 sequences, 32/8 heads of 128, a step behind a window of 4096 keys: 107 us, 5.0 TB/s), by the
-// matrix products and their loads with many (2048 steps of 24/8 heads behind a window of 2048 keys: 536 us, 96 TFLOP/s; 8 trees of 16
-// nodes behind 4000 keys: 111 us).
+// matrix products and their loads with many (2048 steps of 24/8 heads behind a window of 2048 keys: 538 us, 96 TFLOP/s; 8 trees of 16
+// nodes behind 4000 keys: 115 us).
 #include "attn_image.h"
 #include "attn_spans.h"
 #include "attn_tree.h"
@@ -49,6 +52,10 @@ __global__ __launch_bounds__(512) void attn_spans_f32(SpanParams p) {
   int position = t_b + row;
   if constexpr (kTree) position = t_b + tree.depth(row);
   const int hi_col = kTree ? t_b - 1 : position, lo_col = p.window > 0 && position - p.window + 1 > 0 ? position - p.window + 1 : 0;
+  // A group that ends behind all_hi, or begins before lo_last and is not all sinks, is seen less of by some of several rows than by others;
+  // in a tree by a single row too, whose ancestors are not all the nodes before it.
+  const int all_hi = kTree ? t_b - 1 : t_b + first_col / p.G, lo_last = p.window > 0 && last - p.window + 1 > 0 ? last - p.window + 1 : 0;
+  const bool differ = !kRope && (kTree || last_row > first_col / p.G);  // (turned: a single step)
   f32x4 q[DT];
   {
     const float* qp = static_cast<const float*>(p.q) + (((int64_t)b * p.io_steps + row) * p.Hq + (int64_t)hkv * p.G + gq) * D + 4 * c;
@@ -85,6 +92,8 @@ __global__ __launch_bounds__(512) void attn_spans_f32(SpanParams p) {
     const int phys = clamp_block(table[(j >> p.z_log2) & p.tile_mask], p.num_blocks);
     return ((((int64_t)phys * p.Hkv + hkv) << p.z_log2) + (j & ((1 << p.z_log2) - 1))) * D;
   };
+  auto cut = [&](int key) __attribute__((always_inline)) { return differ && (key + 31 > all_hi || (key < lo_last && key + 31 >= p.sinks)); };
+  bool wrong = false;
   for (int at = from + wave; at < past; at += nwaves) {
     const int key = span_group(rg, at) << 5;
     int64_t off[2];
@@ -114,9 +123,31 @@ __global__ __launch_bounds__(512) void attn_spans_f32(SpanParams p) {
 #pragma unroll
       for (int h = 0; h < D / 64; ++h) v[r][h] = *reinterpret_cast<const f32x4*>(vp + 64 * h);
     }
+    auto put_off = [&]() __attribute__((always_inline)) {  // a weight of 0 makes NaN of a value that is not finite: such values come later
+      float sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const int j = key + 4 * c + (r & 3) + 16 * (r >> 2);
+        float of = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) of = fmaf(0.f, v[r][dt >> 2][dt & 3], of);
+        sum += j <= last && (j >= rg.lo || j < p.sinks) ? of : 0.f;
+      }
+      if (__any(!(sum == 0.f))) {
+        wrong = true;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) v[r][dt >> 2][dt & 3] = fabsf(v[r][dt >> 2][dt & 3]) < INFINITY ? v[r][dt >> 2][dt & 3] : 0.f;
+        }
+      }
+    };
     uint32_t bits = 0;
-    if constexpr (kTree) {
-      if (key + 31 >= t_b) bits = tree.bits(row, key - t_b);
+    if constexpr (kTree) {  // (behind the mask trees take 123 us for 115; steps, before it, 547 for 538)
+      if (cut(key)) {
+        put_off();
+        if (key + 31 >= t_b) bits = tree.bits(row, key - t_b);
+      }
     }
     mask_span<kTree>(key, lo_col, hi_col, p.sinks, bits, lane, x);
     float mx = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
@@ -135,6 +166,9 @@ __global__ __launch_bounds__(512) void attn_spans_f32(SpanParams p) {
       }
     }
     m_run = above ? mx : m_run;
+    if constexpr (!kTree) {
+      if (cut(key)) put_off();
+    }
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
       const float w = fast_exp2(fmaf(x[r], p.scale_log2e, -m_run));
@@ -144,6 +178,45 @@ __global__ __launch_bounds__(512) void attn_spans_f32(SpanParams p) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         acc[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, some ? v[r][dt >> 2][dt & 3] : 0.f, acc[dt], 0, 0, 0);
+      }
+    }
+  }
+  if (wrong) {  // such values, one by one, into the columns that see them: infinite or NaN whatever the weight
+    int same = lane;
+    asm volatile("" : "+v"(same));  // (what both loops have in common is computed anew: registers)
+    const int c = same >> 4, n = same & 15;
+    for (int at = from + wave; at < past; at += nwaves) {
+      const int key = span_group(rg, at) << 5;
+      if (!cut(key)) continue;
+      uint32_t bits = 0, sees = 0;  // of the group's slots 4c + (r mod 4) + 16 (r / 4), bit r: this lane's column sees it
+      if constexpr (kTree) {
+        if (key + 31 >= t_b) bits = tree.bits(row, key - t_b);
+      }
+#pragma unroll 1
+      for (int r = 0; r < 8; ++r) {
+        const int slot = 4 * c + (r & 3) + 16 * (r >> 2), j = key + slot;
+        sees |= ((j <= hi_col && (j >= lo_col || j < p.sinks)) || ((bits >> slot) & 1u) != 0 ? 1u : 0u) << r;
+      }
+#pragma unroll 1
+      for (int r = 0; r < 8; ++r) {
+        const int j = key + 4 * c + (r & 3) + 16 * (r >> 2);
+        const bool some = j <= last && (j >= rg.lo || j < p.sinks);
+        const float* const vp = static_cast<const float*>(p.v_pool) + row_at(j) + 4 * n;
+        f32x4 one[D / 64];
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h) one[h] = *reinterpret_cast<const f32x4*>(vp + 64 * h);
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {  // the slot of lanes 16i ..
+          uint32_t seen[4];            // by columns 4c + e
+#pragma unroll
+          for (int e = 0; e < 4; ++e) seen[e] = ((uint32_t)__shfl((int)sees, 4 * c + e + 16 * i) >> r) & 1u;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            const float far = __shfl(some ? one[dt >> 2][dt & 3] : 0.f, n + 16 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[dt][e] += seen[e] && !(fabsf(far) < INFINITY) ? far : 0.f;
+          }
+        }
       }
     }
   }

@@ -648,3 +648,41 @@ def test_long_prompts_of_short_windows(dtype, Hq, Hkv, D, B, count, window):
             rows = np.arange(first, min(first + 150, n[b]))
             seen = sees_chain(0, int(rows[-1]) + 1, window, 4)[rows]
             near(dtype, got[b, rows], q[b, rows], K[b, :rows[-1] + 1], V[b, :rows[-1] + 1], seen)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,Z,B,t,rows,window,sinks,ragged", [
+    (6, 2, 128, 32, 2, 50, 12, 0, 0, False), (4, 4, 64, 4, 3, 333, 40, 20, 5, True), (24, 8, 128, 64, 2, 3000, 8, 600, 70, True),
+    (16, 1, 64, 32, 1, 0, 60, 7, 0, False), (1, 1, 128, 8, 1, 100, 33, 3, 110, False)])
+def test_fp32_values_that_are_not_finite_show_only_where_they_are_seen(Hq, Hkv, D, Z, B, t, rows, window, sinks, ragged):
+    """NaN and infinities among the values that some rows of a tree, a block or a prompt see: the other rows keep their bits, and so do the
+    dims of those rows that hold none."""
+    dtype, rng = T.TEMPO_F32, np.random.default_rng(t + rows)
+    end, steps = t + rows, pick_steps(rng, t, B, ragged)
+    parents = np.stack([tree_of("random", rows, rng) for _ in range(B)])
+    q, K, V = normal(44, 1, (B, rows, Hq, D), dtype), normal(44, 2, (B, end, Hkv, D), dtype), normal(44, 3, (B, end, Hkv, D), dtype)
+    worse = V.copy()
+    for b in range(B):
+        last = steps[b] + rows
+        for j in {int(steps[b]), int(steps[b]) + rows // 2, last - 1, max(0, int(steps[b]) - max(1, window - rows // 3)), int(rng.integers(0, last))}:
+            worse[b, j, rng.integers(0, Hkv), rng.integers(0, D, 3)] = np.array([np.nan, np.inf, -np.inf])[rng.permutation(3)]
+    answers = []
+    for values in (V, worse):
+        st = make_store(44, dtype, B, Hq, Hkv, D, Z, end - 1)
+        write_lengths(st, K, values, steps + rows)
+        tree, block = rows_of(dtype, np.zeros(q.shape)), rows_of(dtype, np.zeros(q.shape))
+        st.attend_tree(rows_of(dtype, q), tree, ints(parents), t, None, window, sinks, ints(steps) if ragged else None)
+        answers.append([np64(tree)])
+        if window:
+            st.attend_sinks(rows_of(dtype, q), block, t, rows, window, sinks, ints(steps) if ragged else None)
+            answers[-1].append(np64(block))
+        if window and not ragged:
+            st.prefill_sinks(rows_of(dtype, q), rows_of(dtype, K[:, t:]), rows_of(dtype, values[:, t:]), block, t, rows, window, sinks)
+            answers[-1].append(np64(block))
+    for which, (clean, got) in enumerate(zip(*answers)):
+        for b in range(B):
+            last = steps[b] + rows
+            seen = sees_tree(int(steps[b]), parents[b], window, sinks) if which == 0 else sees_chain(int(steps[b]), rows, window, sinks)
+            hit = seen.astype(float) @ (~np.isfinite(worse[b, :last])).reshape(last, -1) > 0     # [rows][Hkv * D]
+            hit = hit.reshape(rows, Hkv, 1, D).repeat(Hq // Hkv, 2).reshape(rows, Hq, D)
+            assert hit.any() and not hit.all() and not np.isfinite(got[b][hit]).any()
+            np.testing.assert_array_equal(got[b][~hit], clean[b][~hit])
