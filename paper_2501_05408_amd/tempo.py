@@ -70,6 +70,7 @@ class tempo_rope_axes(ctypes.Structure):
         ("axes", ctypes.c_int32),
         ("axis_of_pair", ctypes.c_uint8 * 64),
     ]
+    pairs = None  # that a list from make_rope_axes() is for (None: filled by hand, all that are used)
 
 
 class TempoError(RuntimeError):
@@ -281,11 +282,22 @@ def make_rope(cos_table, sin_table, head_dim) -> tempo_rope:
 
 
 def make_rope_axes(axis_of_pair) -> tempo_rope_axes:
-    """The axis (0 .. 3) of each of the head_dim/2 rotated pairs."""
+    """The axis (0 .. 3) of each of the head_dim/2 rotated pairs; refused with tables of another head_dim."""
     axis_of_pair = [int(a) for a in axis_of_pair]
     if not 1 <= len(axis_of_pair) <= 64 or not all(0 <= a <= 255 for a in axis_of_pair):
         raise TempoError(TEMPO_ERR_SHAPE, "make_rope_axes")
-    return tempo_rope_axes(max(axis_of_pair) + 1, (ctypes.c_uint8 * 64)(*axis_of_pair))
+    rest = [255] * (64 - len(axis_of_pair))  # (no axis)
+    axes = tempo_rope_axes(max(axis_of_pair) + 1, (ctypes.c_uint8 * 64)(*axis_of_pair, *rest))
+    axes.pairs = len(axis_of_pair)
+    return axes
+
+
+def _axes(axes, rope, where):
+    if axes is None:
+        return None
+    if axes.pairs not in (None, rope.head_dim // 2):
+        raise TempoError(TEMPO_ERR_SHAPE, where)
+    return ctypes.byref(axes)
 
 
 def make_kv_layers(stores):
@@ -687,13 +699,13 @@ def tempo_kv_keep(layers, num_layers, batch, t, t_per_seq, nodes, kept, count, s
 
 
 def tempo_rope_rotate_at(rope, axes, positions, x, y, dtype, batch, count, heads, stream=None):
-    _check(load().tempo_rope_rotate_at(ctypes.byref(rope), None if axes is None else ctypes.byref(axes), _ptr(positions), _ptr(x), _ptr(y),
+    _check(load().tempo_rope_rotate_at(ctypes.byref(rope), _axes(axes, rope, "tempo_rope_rotate_at"), _ptr(positions), _ptr(x), _ptr(y),
                                        dtype, batch, count, heads, _stream(stream)), "tempo_rope_rotate_at")
 
 
 def tempo_rope_kv_append_at(kv, rope, axes, positions, k_raw, v_new, q_raw, q_out, batch, num_q_heads, t, t_per_seq, count,
                             count_per_seq=None, stream=None):
-    _check(load().tempo_rope_kv_append_at(ctypes.byref(kv), ctypes.byref(rope), None if axes is None else ctypes.byref(axes),
+    _check(load().tempo_rope_kv_append_at(ctypes.byref(kv), ctypes.byref(rope), _axes(axes, rope, "tempo_rope_kv_append_at"),
                                           _ptr(positions), _ptr(k_raw), _ptr(v_new), _ptr(q_raw), _ptr(q_out), batch, num_q_heads, t,
                                           _ptr(t_per_seq), count, _ptr(count_per_seq), _stream(stream)), "tempo_rope_kv_append_at")
 

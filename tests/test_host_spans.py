@@ -204,3 +204,18 @@ def test_positions_and_kept_rows_are_refused():
         assert keep([kv_desc(), other]) == shape
     assert keep(t=-1) == reach and keep(t=250) == reach and keep(t=2 ** 31 - 10) == reach and keep(t=250, nodes=1, count=7) == reach
     assert keep([kv_desc(ring=2)], nodes=129) == reach
+
+
+def test_axes_made_for_another_head_dim_are_refused():
+    """A list of 32 axes with tables of 64 pairs, and of 64 with tables of 32: by the binding, and a list that is too short by the library too."""
+    few, many = T.make_rope_axes([0] * 10 + [1] * 22), T.make_rope_axes([i % 3 for i in range(64)])
+    wide, narrow = T.tempo_rope(FAKE, FAKE, 1000, 128), T.tempo_rope(FAKE, FAKE, 1000, 64)
+    for axes, rope in ((few, wide), (many, narrow), (T.make_rope_axes([0]), wide)):
+        with pytest.raises(T.TempoError) as e:
+            T.tempo_rope_rotate_at(rope, axes, FAKE, FAKE, FAKE, T.TEMPO_BF16, 2, 5, 6, stream=FAKE)
+        assert e.value.status == T.TEMPO_ERR_SHAPE
+        with pytest.raises(T.TempoError) as e:
+            T.tempo_rope_kv_append_at(kv_desc(D=rope.head_dim), rope, axes, FAKE, FAKE, FAKE, None, None, 2, 0, 100, None, 5, stream=FAKE)
+        assert e.value.status == T.TEMPO_ERR_SHAPE
+    assert place(axes=few) == T.TEMPO_ERR_RANGE
+    assert T.load().tempo_rope_rotate_at(ctypes.byref(wide), ctypes.byref(few), FAKE, FAKE, FAKE, T.TEMPO_BF16, 2, 5, 6, None) == T.TEMPO_ERR_RANGE
