@@ -701,7 +701,7 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  * tempo_sink_blocks         *sink_blocks = ceil(sinks / Z); *window_blocks = the most tiles that the windows of `queries` consecutive
  *                           steps touch.  Host only; TEMPO_ERR_RANGE for window, Z or queries < 1, sinks < 0 or 2^31 tiles and more, TEMPO_ERR_NULL.
  * tempo_attn_sinks          `queries` consecutive steps t .. t+queries-1 (t_per_seq[b] ..; t their upper bound), which the store
- *                           holds: q, out device, [batch][queries][Hq][D].  Any number of steps.
+ *                           holds: q, out device, [batch][queries][Hq][D].  Any number of steps (limits below).
  * tempo_decode_step_sinks   one step whose row k_new, v_new (device, [batch][Hkv][D]) is written first; q, out [batch][Hq][D].
  * tempo_rope_decode_step_sinks  the same with q_raw and k_raw turned to position t (t_per_seq[b]), as tempo_rope_decode_step_*.
  * tempo_prefill_sinks, tempo_rope_prefill_sinks  steps t .. t+count-1: rows written, all steps answered, count_per_seq as for
@@ -711,7 +711,9 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  *                           without counts).
  * Workspaces: device, 256-byte aligned (TEMPO_ERR_WORKSPACE).  The size for max_t serves every step up to it; a loop over steps of an
  * endless conversation asks for it once, with the largest step: it does not grow beyond the window.  0 on bad arguments.
- * queries * num_q_heads <= 2^30, rows written batch * count * Hkv * D < 2^31 (TEMPO_ERR_SHAPE).
+ * Of one call (TEMPO_ERR_SHAPE): queries (count) <= 2^24, queries * num_q_heads <= 2^29, of an fp32 store 2^26, batch * num_kv_heads *
+ * ceil(queries * group / 16) < 2^31, rows written batch * count * Hkv * D < 2^31.  The size for calls beyond these limits is 0, where it is
+ * asked for a number of queries.
  */
 int tempo_sink_blocks(int32_t window, int32_t sinks, int32_t Z, int32_t queries, int32_t* sink_blocks, int32_t* window_blocks);
 

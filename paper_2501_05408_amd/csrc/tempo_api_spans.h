@@ -11,13 +11,17 @@ struct SpanPlan {
   int32_t tile_columns, tiles, split_groups, splits, waves;
 };
 
-// Attention over spans is of linear stores.
+// Attention over spans is of linear stores.  A launch of so many rows fits whatever the plan: less than 2^31 threads along the grid's first
+// axis (tiles of 128 columns and 256 threads, which span_plan() takes where narrower ones would not fit; fp32: 16 columns, 256
+// threads at least) and workgroups, which are numbered in 32 bits.
 int check_span_store(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows) {
   int rc = check_layout(kv);
   if (rc != TEMPO_OK) return rc;
   if (kv->ring_blocks != 0) return TEMPO_ERR_SHAPE;
   if ((rc = check_heads(kv, batch, Hq)) != TEMPO_OK) return rc;
-  if (rows < 1 || rows > (1 << 24) || (int64_t)rows * Hq > (1 << 30)) return TEMPO_ERR_SHAPE;
+  if (rows < 1 || rows > (1 << 24) || (int64_t)rows * Hq > (kv->dtype == TEMPO_F32 ? 1 << 26 : 1 << 29)) return TEMPO_ERR_SHAPE;
+  const int64_t columns = (int64_t)rows * (Hq / kv->num_kv_heads);
+  if ((int64_t)batch * kv->num_kv_heads * ((columns + 15) / 16) > INT32_MAX) return TEMPO_ERR_SHAPE;
   return TEMPO_OK;
 }
 
@@ -127,6 +131,7 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
   int32_t groups = 0;
   double least = -1.0;
   for (int32_t tile = 16; tile <= 128; tile = tile == 16 ? 32 : 4 * tile) {
+    if (tile < 128 && kv->dtype != TEMPO_F32 && (columns + tile - 1) / tile * kv->num_kv_heads * 512 > INT32_MAX) continue;
     int32_t tile_rows = (tile + G - 2) / G + 1;
     tile_rows = tree || tile_rows > rows ? rows : tile_rows;
     const int32_t here = span_groups_bound(t, rows, tile_rows, window, sinks);
@@ -168,6 +173,7 @@ SpanPlan span_plan(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, 
     const int64_t waves = few_waves((int64_t)batch * kv->num_kv_heads * s.tiles, s.tiles, groups, kv->head_dim, s.tile_columns, ragged || counts);
     s.waves = s.waves < waves ? s.waves : (int32_t)waves;
   }
+  while (s.waves > 4 && s.tile_columns <= 32 && (int64_t)kv->num_kv_heads * s.tiles * 64 * s.waves > INT32_MAX) s.waves /= 2;
   while (s.tile_columns <= 32 && s.waves > 1 && units_lds_bytes(s.waves, (int)(columns < 16 ? columns : 16), kv->head_dim) > kMaxUnitsLds) s.waves /= 2;
   return s;
 }
@@ -213,9 +219,8 @@ int attend_spans(const tempo_kv* kv, const void* q, void* out, const int32_t* pa
 int check_span_workspace(const tempo_kv* kv, int32_t batch, int32_t Hq, int32_t rows, int32_t t, bool ragged, bool counts, int32_t window,
                          int32_t sinks, bool tree, const void* workspace, size_t workspace_bytes, SpanPlan* plan) {
   const SpanPlan s = *plan = span_plan(kv, batch, Hq, rows, t, ragged, counts, window, sinks, tree);
-  // workgroups: along the grid's first axis, and all of them (numbered in 32 bits)
-  const int64_t first = (int64_t)kv->num_kv_heads * s.tiles;
-  if (first * 512 > INT32_MAX || first * batch * s.splits > INT32_MAX || s.splits > 65535) return TEMPO_ERR_SHAPE;
+  const int64_t first = (int64_t)kv->num_kv_heads * s.tiles;  // workgroups along the grid's first axis
+  if (first * (s.tile_columns > 32 ? 256 : 64 * s.waves) > INT32_MAX || first * batch * s.splits > INT32_MAX || s.splits > 65535) return TEMPO_ERR_SHAPE;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TEMPO_ERR_WORKSPACE;
   return workspace_bytes < span_bytes(kv, batch, Hq, rows, s) ? TEMPO_ERR_WORKSPACE : TEMPO_OK;
 }

@@ -247,3 +247,36 @@ def test_a_pool_twice_among_the_layers_is_refused(lib):
         layers = T.make_kv_layers([one, T.make_kv(k, v, AT, 100, 50, 64, 8, 128, T.TEMPO_BF16)])
         assert lib.tempo_kv_keep(layers, 2, 4, 90, None, 20, AT, 6, None) == T.TEMPO_ERR_SHAPE
     assert taken(lib) == []
+
+
+@pytest.mark.parametrize("dtype", STORES)
+def test_calls_up_to_their_documented_limit_are_launched(lib, dtype):
+    """Steps, heads and batches at the limits of one call and one beyond: launched, in a grid that fits, or refused with a size of 0."""
+    most = 1 << (26 if dtype == T.TEMPO_F32 else 29)
+
+    def call(batch, Hkv, G, D, rows, window, sinks, t=0):
+        kv = store(Hkv, D, 256, 1 << 24, dtype)
+        nbytes = lib.tempo_attn_sinks_workspace_bytes(ctypes.byref(kv), batch, Hkv * G, rows, t, window, sinks)
+        lib.host_launches_take()
+        status = lib.tempo_attn_sinks(ctypes.byref(kv), AT, AT, batch, Hkv * G, rows, t, None, window, sinks, 0.1, AT, nbytes, None)
+        got = taken(lib)
+        assert (status == T.TEMPO_OK) == bool(got) == (nbytes > 0) and status in (T.TEMPO_OK, T.TEMPO_ERR_SHAPE)
+        for name, f in got[:1]:
+            tiles = Hkv * ((rows * G + f["tile"] - 1) // f["tile"])
+            assert tiles * 64 * f["waves"] < 2 ** 31 and tiles * batch * f["splits"] < 2 ** 31 and f["splits"] < 65536
+        return status
+
+    heads = [(1, 1), (8, 1), (1, 128), (8, 16), (500, 128), (65535, 1), (1000, 3)]
+    for (Hkv, G), D, (window, sinks) in itertools.product(heads, (64, 128), ((1, 0), (1, 4), (300, 4), (5000, 33))):
+        rows = most // (Hkv * G)
+        if rows <= 1 << 24:
+            assert call(1, Hkv, G, D, rows, window, sinks) == T.TEMPO_OK
+            assert call(1, Hkv, G, D, rows + 1, window, sinks) == T.TEMPO_ERR_SHAPE
+        else:
+            assert call(1, Hkv, G, D, 1 << 24, window, sinks) == T.TEMPO_OK
+            assert call(1, Hkv, G, D, (1 << 24) + 1, window, sinks) == T.TEMPO_ERR_SHAPE
+    # workgroups of a batch
+    for batch, Hkv, G, rows in ((65535, 32767, 1, 1), (65535, 8, 1, 65536), (60000, 8, 16, 4400)):
+        fits = batch * Hkv * ((rows * G + 15) // 16) < 2 ** 31
+        assert call(batch, Hkv, G, 64, rows, 300, 4) == (T.TEMPO_OK if fits else T.TEMPO_ERR_SHAPE)
+    assert call(65535, 8, 1, 64, 65520, 300, 4) == T.TEMPO_OK and call(65535, 8, 1, 64, 65537, 300, 4) == T.TEMPO_ERR_SHAPE
