@@ -15,12 +15,28 @@ from . import tempo as T
 _TORCH_DTYPE = {T.TEMPO_BF16: torch.bfloat16, T.TEMPO_F32: torch.float32, T.TEMPO_E4M3: torch.bfloat16}
 
 
+def _turns(table, num_blocks):
+    """Of a block table whose sequences name blocks more than once, what tells calls whose steps meet in a block: for every such sequence
+    (its first tile whose block comes again, the first tile whose block was there before, the least distance of two in one block)."""
+    table = table.clamp(0, num_blocks - 1)  # (as the library does)
+    order = torch.argsort(table, dim=1, stable=True)
+    sorted_ = table.gather(1, order)
+    again = sorted_[:, 1:] == sorted_[:, :-1]
+    found = set()
+    for b in torch.nonzero(again.any(1)).flatten().tolist():
+        before, behind = order[b, :-1][again[b]], order[b, 1:][again[b]]
+        found.add((int(before.min()), int(behind.min()), int((behind - before).min())))
+    return found
+
+
 class BlockStore:
     """A paged key/value pool (the paper's block store, Section 6) for `batch`
     sequences, plus the workspace the attention entry points need.
 
     block_table: int32 tensor [batch][max_blocks_per_seq] (tile n -> physical
-    block); by default sequence b owns blocks b*max_blocks_per_seq + n.
+    block); by default sequence b owns blocks b*max_blocks_per_seq + n.  A sequence may name a
+    block more than once (sinks_table()): the calls over windows with sinks, trees, placed and kept
+    rows then refuse steps that would meet in a block (TempoError, TEMPO_ERR_RANGE).
     fill: "nan" poisons the pool so that any read outside the visible range shows.
     dtype T.TEMPO_E4M3: rows are kept in 8 bits with a scale each; pools are flat uint8 tensors of
     T.tempo_kv_pool_bytes(kv) bytes, everything else is bf16.
@@ -55,6 +71,9 @@ class BlockStore:
         if block_table is None:
             block_table = torch.arange(batch * self.max_blocks_per_seq, dtype=torch.int32).reshape(
                 batch, self.max_blocks_per_seq)
+            self._turns = set()
+        else:
+            self._turns = _turns(block_table, self.num_blocks) if not ring_blocks else set()
         self.block_table = block_table.to(device=self.device, dtype=torch.int32).contiguous()
         assert tuple(self.block_table.shape) == (batch, self.max_blocks_per_seq)
         self.kv = T.make_kv(self.k_pool, self.v_pool, self.block_table, self.num_blocks,
@@ -271,13 +290,22 @@ class BlockStore:
     @staticmethod
     def sinks_table(batch, max_t, block_size, window, sinks, queries=1):
         """(block table, number of blocks) for BlockStore(block_table=, num_blocks=): sequences of up to max_t steps, in calls of up to
-        `queries`, that keep their first `sinks` keys and a window in blocks that are used in turn."""
+        `queries`, that keep their first `sinks` keys and a window in blocks that are used in turn.  (Calls of more steps are refused where
+        a block would come again within them.)"""
         first, turn = T.tempo_sink_blocks(window, sinks, block_size, queries)
         columns = max_t // block_size + 1
         own = min(columns, first + turn)
         n = torch.arange(columns)
         n = torch.where(n < first, n, first + (n - first) % turn) if own < columns else n
         return (n[None] + own * torch.arange(batch)[:, None]).to(torch.int32), batch * own
+
+    def _meet(self, where, t, rows, window=1, sinks=0):
+        """Refuses a call that writes or reads steps t .. t+rows-1, their windows (0: all before) and the sinks, where two of them have one slot."""
+        last = t + rows - 1
+        span = min(last + 1, window + rows - 1) if window else last + 1
+        for shared, again, apart in self._turns:
+            if last >= again * self.Z and (span > apart * self.Z or sinks > shared * self.Z):
+                raise T.TempoError(T.TEMPO_ERR_RANGE, f"{where}: steps of the call meet in a block of the table")
 
     def _spans_ws(self, nbytes):
         if nbytes == 0:
@@ -290,6 +318,7 @@ class BlockStore:
 
     def attend_sinks(self, q, out, t, queries, window, sinks, t_per_seq=None, scale=None):
         """Steps t .. t+queries-1 over their window and the first `sinks` keys; q, out [batch][queries][Hq][D]."""
+        self._meet("attend_sinks", t, queries, window, sinks)
         ws, nbytes = self._spans_ws(T.tempo_attn_sinks_workspace_bytes(self.kv, self.batch, self.Hq, queries, self._last_first_step(queries),
                                                                        window, sinks))
         T.tempo_attn_sinks(self.kv, q, out, self.batch, self.Hq, queries, t, t_per_seq, window, sinks,
@@ -298,6 +327,7 @@ class BlockStore:
 
     def step_sinks(self, q, k_new, v_new, out, t, window, sinks, t_per_seq=None, scale=None, rope=False):
         """Append step t and attend over its window and the first `sinks` keys.  rope=True: q and k_new arrive unrotated."""
+        self._meet("step_sinks", t, 1, window, sinks)
         ws, nbytes = self._spans_ws(T.tempo_attn_sinks_workspace_bytes(self.kv, self.batch, self.Hq, 1, self._last_first_step(1), window, sinks))
         s = self.scale if scale is None else scale
         if rope:
@@ -309,6 +339,7 @@ class BlockStore:
 
     def prefill_sinks(self, q, k_new, v_new, out, t, count, window, sinks, count_per_seq=None, scale=None, rope=False):
         """Write steps t .. t+count-1 and answer them over their windows and the first `sinks` keys."""
+        self._meet("prefill_sinks", t, count, window, sinks)
         ws, nbytes = self._spans_ws(T.tempo_prefill_sinks_workspace_bytes(self.kv, self.batch, self.Hq, min(self.max_t, 2 ** 31 - 256)))
         s = self.scale if scale is None else scale
         if rope:
@@ -326,6 +357,7 @@ class BlockStore:
 
     def attend_tree(self, q, out, parents, t, nodes_per_seq=None, window=0, sinks=0, t_per_seq=None, scale=None):
         """The nodes of a tree, whose rows lie at steps t .. t+nodes-1; q, out [batch][nodes][Hq][D]."""
+        self._meet("attend_tree", t, parents.shape[1], window, sinks)
         nodes = parents.shape[1]
         ws, nbytes = self._spans_ws(T.tempo_attn_tree_workspace_bytes(self.kv, self.batch, self.Hq, nodes, self._last_first_step(nodes),
                                                                       window, sinks))
@@ -336,12 +368,14 @@ class BlockStore:
     def keep(self, kept, t, nodes, t_per_seq=None, layers=None):
         """The rows t + kept[b][i] (int32 [batch][count]; up to the first negative one) become rows t + i; layers: the stores of all
         layers (this one among them), which share the block table."""
+        self._meet("keep", t, max(nodes, kept.shape[1]))
         kvs = T.make_kv_layers([s.kv for s in layers] if layers else [self.kv])
         T.tempo_kv_keep(kvs, len(kvs), self.batch, t, t_per_seq, nodes, kept, kept.shape[1])
 
     def rope_append_at(self, positions, k_raw, v_new, t, q_raw=None, q_out=None, t_per_seq=None, count_per_seq=None, axes=None):
         """Rows [batch][count][Hkv][D] to steps t .., keys turned to positions [batch][count][axes] (set_rope tables); queries
         [batch][count][Hq][D] turned into q_out."""
+        self._meet("rope_append_at", t, k_raw.shape[1])
         T.tempo_rope_kv_append_at(self.kv, self.rope, axes, positions, k_raw, v_new, q_raw, q_out, self.batch, self.Hq, t, t_per_seq,
                                   k_raw.shape[1], count_per_seq)
         return q_out
