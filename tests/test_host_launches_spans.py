@@ -10,6 +10,7 @@ import numpy as np
 import pytest
 
 from paper_2501_05408_amd import tempo as T
+from spans_cases import WIDE
 from spans_reference import sees_chain, sees_tree
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -280,3 +281,33 @@ def test_calls_up_to_their_documented_limit_are_launched(lib, dtype):
         fits = batch * Hkv * ((rows * G + 15) // 16) < 2 ** 31
         assert call(batch, Hkv, G, 64, rows, 300, 4) == (T.TEMPO_OK if fits else T.TEMPO_ERR_SHAPE)
     assert call(65535, 8, 1, 64, 65520, 300, 4) == T.TEMPO_OK and call(65535, 8, 1, 64, 65537, 300, 4) == T.TEMPO_ERR_SHAPE
+
+
+def test_the_calls_whose_wide_answers_are_tested_go_wide(lib):
+    """The cases of test_gpu_spans_wide.py, and that they take in what that kernel has: tiles of 64 to 128 columns, one range and many, steps and
+    trees, both stores and head lengths, a window and a range more than 64 tiles long."""
+    seen = set()
+    for dtype, what, Hq, Hkv, D, Z, B, t, rows, window, sinks, ragged, counts in WIDE:
+        kv = store(Hkv, D, Z, (t + rows) // Z + 1, dtype)
+        lib.host_launches_take()
+        at, n, ref, size = AT if ragged else None, AT if counts else None, ctypes.byref(kv), 1 << 40
+        if what == "tree":
+            assert lib.tempo_attn_tree(ref, AT, AT, AT, n, B, Hq, rows, t, at, window, sinks, 0.1, AT, size, None) == T.TEMPO_OK
+        elif what == "block":
+            assert lib.tempo_attn_sinks(ref, AT, AT, B, Hq, rows, t, at, window, sinks, 0.1, AT, size, None) == T.TEMPO_OK
+        else:
+            assert lib.tempo_prefill_sinks(ref, AT, AT, AT, AT, B, Hq, t, rows, n, window, sinks, 0.1, AT, size, None) == T.TEMPO_OK
+        launches = dict(taken(lib))
+        f = launches["spans_wide"]
+        split, one_range = f["splits"] > 1, f["split_groups"] // (Z // 32)
+        seen |= {(dtype, D, what, split), (dtype, D, f["tile"]), (dtype, what, rows > 64, window > 0)}
+        if sinks and (t - window) // Z > 64:
+            seen.add((dtype, D, "far"))
+        if not split and one_range > 64:
+            seen.add((dtype, D, "long"))
+    for dtype, D in itertools.product((T.TEMPO_BF16, T.TEMPO_E4M3), (64, 128)):
+        assert {(dtype, D, "far"), (dtype, D, "long"), (dtype, D, 128)} <= seen
+        assert {(dtype, D, "prompt", False), (dtype, D, "prompt", True), (dtype, D, "tree", False)} <= seen
+    assert {(T.TEMPO_BF16, 128, 64), (T.TEMPO_BF16, 128, 96), (T.TEMPO_E4M3, 128, 96), (T.TEMPO_E4M3, 64, 96)} <= seen
+    for dtype in (T.TEMPO_BF16, T.TEMPO_E4M3):
+        assert {(dtype, 128, "tree", True), (dtype, "tree", True, False), (dtype, "tree", True, True), (dtype, "tree", False, False)} <= seen
