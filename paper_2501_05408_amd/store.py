@@ -310,7 +310,8 @@ class BlockStore:
     def _spans_ws(self, nbytes):
         if nbytes == 0:
             raise T.TempoError(T.TEMPO_ERR_SHAPE, "workspace of the attention over spans")
-        ws = self._kept_ws("_span_ws", nbytes)
+        # (a prompt of all steps needs the most)
+        ws = self._kept_ws("_span_ws", nbytes, lambda: T.tempo_prefill_sinks_workspace_bytes(self.kv, self.batch, self.Hq, min(self.max_t, 2 ** 31 - 256)))
         return ws, ws.numel()
 
     def _last_first_step(self, rows):

@@ -279,3 +279,21 @@ def test_steps_that_meet_in_a_block_are_refused(monkeypatch):
     # sequences that share a block with each other, or have one each, are nothing to refuse
     st = BlockStore(2, 4, 2, 64, 32, 127, T.TEMPO_BF16, device="cpu", num_blocks=7, block_table=torch.tensor([[0, 1, 2, 3], [0, 4, 5, 6]]))
     st.attend_tree(None, None, torch.zeros((2, 9), dtype=torch.int32), 100)
+
+
+def test_workspaces_of_spans_do_not_grow_beyond_a_prompts(monkeypatch):
+    import torch
+    from paper_2501_05408_amd.store import BlockStore
+    given = []
+    for name in ("tempo_attn_sinks", "tempo_prefill_sinks", "tempo_attn_tree"):
+        monkeypatch.setattr(T, name, lambda *a, **k: given.append(a[-1]))
+    for B, Hq, Hkv, D, max_t in ((1, 8, 2, 64, 3000), (4, 24, 8, 128, 2000), (2, 4, 4, 64, 100)):
+        st = BlockStore(B, Hq, Hkv, D, 64, max_t, T.TEMPO_BF16, device="cpu")
+        most = T.tempo_prefill_sinks_workspace_bytes(st.kv, B, Hq, st.max_t)
+        given.clear()
+        for rows in (1, 2, 5, 9, 20, 50, 90):
+            st.attend_sinks(None, None, 0, rows, 2000, 4)
+            st.attend_tree(None, None, torch.zeros((B, rows), dtype=torch.int32), 0)
+            assert max(given) <= most
+        st.prefill_sinks(None, None, None, None, 0, 100, 50, 4)
+        assert given[-1] == most and len(st._span_ws) <= 20
