@@ -695,8 +695,10 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  * Constant memory: the table of a linear store may name a block more than once.  Blocks 0 .. sink_blocks-1 of a sequence are kept and
  * window_blocks further ones (tempo_sink_blocks) take the tiles behind them in turn,
  *     table[n] = n < sink_blocks ? own[n] : own[sink_blocks + (n - sink_blocks) mod window_blocks],
- * so that a conversation of any length lives in sink_blocks + window_blocks blocks.  What one call writes and what it reads must lie
- * in blocks of their own then: the sizes that tempo_sink_blocks gives for its `queries` steps do that.  (Longer prompts by several calls.)
+ * so that a conversation lives in sink_blocks + window_blocks blocks however long it gets.  (Its table has an entry for every tile all the same,
+ * and positions stay those of the steps: the rotary calls need angle tables as long as it.)  What one call writes and what it reads must lie
+ * in blocks of their own then, which nothing here can check: the sizes that tempo_sink_blocks gives for its `queries` steps do that.  (Longer
+ * prompts by several calls.)
  *
  * tempo_sink_blocks         *sink_blocks = ceil(sinks / Z); *window_blocks = the most tiles that the windows of `queries` consecutive
  *                           steps touch.  Host only; TEMPO_ERR_RANGE for window, Z or queries < 1, sinks < 0 or 2^31 tiles and more, TEMPO_ERR_NULL.
@@ -709,8 +711,8 @@ int tempo_decode_step_selected(const tempo_kv* kv, void* bounds, const void* q, 
  *                           as they are there).  Answers are those of single steps.  `out` must not alias k_new or v_new.
  *                           Rows of an fp32 store are not turned here (tempo_rope_prefill_sinks: TEMPO_ERR_DTYPE, but for one step
  *                           without counts).
- * Workspaces: device, 256-byte aligned (TEMPO_ERR_WORKSPACE).  The size for max_t serves every step up to it; a loop over steps of an
- * endless conversation asks for it once, with the largest step: it does not grow beyond the window.  0 on bad arguments.
+ * Workspaces: device, 256-byte aligned (TEMPO_ERR_WORKSPACE).  The size for max_t serves every step up to it; a loop over steps of a
+ * long conversation asks for it once, with the largest step: it does not grow beyond the window.  0 on bad arguments.
  * Of one call (TEMPO_ERR_SHAPE): queries (count) <= 2^24, queries * num_q_heads <= 2^29, of an fp32 store 2^26, batch * num_kv_heads *
  * ceil(queries * group / 16) < 2^31, rows written batch * count * Hkv * D < 2^31.  The size for calls beyond these limits is 0, where it is
  * asked for a number of queries.

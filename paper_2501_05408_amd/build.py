@@ -77,7 +77,7 @@ MIN_OCCUPANCY = [
     ("attn_unitsILi128ELb1ELb0ELb0ELi1E", 3),  # 8-bit decode kernel, D = 128: its plans expect three wavefronts to a SIMD
     ("attn_prefill_bf16ILi128E", 2),           # prompt kernel, D = 128: two wavefronts of 32 columns per SIMD
     ("attn_spansILi128E", 2),                  # sinks and trees, D = 128: two workgroups of four wavefronts to a unit, or one of eight
-    ("attn_spans_wideILi128E", 2),             # the same, 128 columns: two workgroups to a unit, as its splits are planned
+    ("attn_spans_wideILi128E", 2),             # the same, 128 columns: two workgroups to a unit by registers, as its splits are planned
     ("attn_spans_wideILi64E", 3),              # D = 64: three
     ("attn_spans_f32ILi128ELb0E", 3),          # sinks over an fp32 store, D = 128 (two: 539 -> 609 us for 2048 steps behind 2048 keys)
 ]

@@ -2,10 +2,15 @@
 //
 // The rows, what they see and how their groups are numbered: attn_spans.hip.  The products as in attn_prefill_bf16.hip: 32 columns
 // to a wavefront as the columns of 32x32x16 products (logits = K Q^T, answers = V^T P^T, so that a lane's logits, weights, sum and
-// accumulators are of one column), every group of 32 slots staged in LDS once for the workgroup's NW wavefronts, four groups deep,
-// the logits of a group computed an iteration ahead of its weights.  What differs: rows see sinks, windows and ancestors; a group
-// of an 8-bit store is turned into bf16 on its way into LDS, by the wavefront that fetched the piece (a quarter of the group each),
-// instead of by every wavefront that reads it.
+// accumulators are of one column), every group of 32 slots staged in LDS once for the workgroup's NW wavefronts, the logits of a group
+// computed an iteration ahead of its weights.  What differs: rows see sinks, windows and ancestors; tiles of 64 to 128 columns (even ones: a
+// wavefront beyond its tile's columns copies, and meets the others); and how groups come into LDS:
+//   bf16    copied straight into the image that the products read, four buffers: three groups in flight, one read.
+//   8 bits  copied as they lie (codes and scale bytes) into three buffers of their own, and turned from there into bf16 images, three as
+//           well, by the wavefront that copied the piece (a quarter of the group each), two groups ahead of the logits.
+// LDS of a workgroup, D = 128: bf16 64 KiB, 8 bits 72.75, and the bits of a tree (up to 11 KiB).  Two to a unit, as the splits are planned
+// (wide_split_groups()), but for 8-bit trees of more than 206 nodes, one: us, 4 trees of 206 / 208 nodes of 32/4 heads behind 7000 keys
+// 158 / 220, bf16 133 / 134.
 #include "attn_bf16_columns32.h"
 #include "attn_spans.h"
 #include "attn_tree.h"

@@ -45,8 +45,9 @@ constexpr int64_t kSpanPartials = 131072;  // partials (of a (row, head) and spl
 
 // Groups of a split of the kernel for many columns: a time model as make_plan()'s, in nanoseconds.  A workgroup of 128 columns costs
 // kWideFixedNs before its first group and behind its last one, hidden behind others only in part; a group, with two or three
-// workgroups to a unit (what registers and LDS let in), 560 ns of the unit's time at D = 128 and 420 at 64, with one 720 and 540.
-// The combine reads and writes a partial per (row, head) and split.  Of a ragged batch's workgroups about half exist.
+// workgroups to a unit (what registers and LDS let in; 8-bit trees of more than 206 nodes at D = 128, one, are not told apart), 560 ns of
+// the unit's time at D = 128 and 420 at 64, with one 720 and 540.  The combine reads and writes a partial per (row, head) and split.  Of a
+// ragged batch's workgroups about half exist.  (Against lengths of a quarter to four times, over 56675 drawn calls of all tiles: 1.1%.)
 constexpr double kWideFixedNs = 8000.0, kWideCombineNs = 4000.0, kWidePartialBytesPerNs = 5000.0;
 
 int32_t wide_split_groups(int64_t units, int32_t groups, int D, int64_t rows, bool ragged, int64_t most) {
@@ -86,7 +87,9 @@ int32_t whole_groups(const tempo_kv* kv) {
 // 16 of 4000, 96 columns 127 / 92 / 67; 32/8 heads of 64, 8 bits, 48 of 1000, 60 columns 27 / 22 / 31; 188 columns 66 / 53 / 46.
 // Of a batch whose sequences have steps, or trees, of their own, about half of the longest are taken to be there, though a range
 // that is not split takes as long as the longest (16 trees of up to 32 nodes behind up to 4000 keys, 24/8 heads of 128, 8 bits,
-// 16 / 32 / 128: 35 / 30 / 44; bf16 61 / 44 / 36).
+// 16 / 32 / 128: 35 / 30 / 44; bf16 61 / 44 / 36).  A group of 8 bits under 32 columns at D = 128 takes a fifth longer where a unit has more
+// than one workgroup (its codes are turned by every wavefront, beside the other's): of 8376 drawn calls of that kind this decides 761, which
+// are 14% (128 columns taken) and 7% (16) faster for it.  Against the best of the three, over 56675 drawn calls: 1.6% on the mean.
 double span_cost_us(const tempo_kv* kv, int64_t pairs, int64_t columns, int64_t rows_heads, int32_t tile, int32_t groups, bool ragged, bool counts) {
   const bool k8 = kv->dtype == TEMPO_E4M3, narrow = kv->head_dim == 64;
   const int at = (k8 ? 2 : 0) + (narrow ? 1 : 0);
